@@ -1,0 +1,152 @@
+/*
+ * lamb_ops.h -- C ABI of the operators around the optimizer step, for AMD
+ * Instinct MI355X (gfx950): Newton-Schulz orthogonalization and the Muon step
+ * for a model's matrices, softmax cross entropy against a vocabulary table with
+ * its gradients, and a token table's lookup with its gradient. Same library,
+ * status codes and conventions as lamb_mi355x.h: pointers are device pointers
+ * unless marked host; the caller owns every tensor; arguments are validated on
+ * the host before any HIP call; work is enqueued on `stream` and nothing is
+ * synchronised, allocated or copied to the host (plan creation and destruction
+ * aside); lamb_last_error() describes a failure. Nothing throws.
+ */
+#ifndef LAMB_OPS_H
+#define LAMB_OPS_H
+
+#include <stddef.h>
+#include <stdint.h>
+
+#include "lamb_mi355x.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Element types of an operator's tensors. */
+typedef enum lamb_dtype {
+    LAMB_DTYPE_F32 = 0,
+    LAMB_DTYPE_BF16 = 1, /* raw 16-bit patterns */
+    LAMB_DTYPE_I32 = 2,  /* token ids */
+    LAMB_DTYPE_I64 = 3   /* token ids */
+} lamb_dtype;
+
+/*
+ * How the products of the Newton-Schulz iteration round their operands.
+ *  LAMB_NS_HALF   to one 16-bit float (11 significant bits). The result is about
+ *                 1.3e-3 off (2-norm, relative) for matrices of independent
+ *                 entries and up to 7e-3 for ones whose singular values span
+ *                 many decades: the rounding of a bf16 result is 1.7e-3.
+ *  LAMB_NS_SPLIT  to the sum of two (22 bits), three products for one: errors as
+ *                 of fp32 arithmetic.
+ */
+typedef enum lamb_ns_precision { LAMB_NS_HALF = 0, LAMB_NS_SPLIT = 1 } lamb_ns_precision;
+
+/*
+ * The iteration: X = G / (||G||_F + eps), then `steps` times
+ *   A = X X^T (or X^T X, on the shorter side),  X <- (a I + b A + c A A) X.
+ * steps 1 to 64, eps >= 0 (with eps = 0 a zero matrix gives NaN), and a, b, c such
+ * that no singular value that starts in [0, 1] passes 2.75, nor the polynomial
+ * 7.75, on the way (LAMB_EINVAL): the iteration's 16-bit numbers hold no more.
+ */
+typedef struct lamb_ns_params {
+    int32_t steps;
+    float a, b, c;
+    float eps;
+    int32_t reserved; /* must be 0 */
+} lamb_ns_params;
+
+/* 5 steps of (3.4445, -4.7750, 2.0315), eps 1e-7. */
+LAMB_API lamb_status lamb_ns_params_init(lamb_ns_params *params);
+
+/*
+ * One matrix to orthogonalize, row-major with rows `*_stride` elements apart
+ * (>= cols). rows and cols 1 to 2^20, aligned to their element. A row or column
+ * vector is a matrix of short side 1. No output may overlap an input of the plan
+ * or another output, but for an input that has the output's address, type and
+ * stride (in place).
+ */
+typedef struct lamb_matrix {
+    const void *in;
+    void *out;
+    int64_t rows, cols;
+    int64_t in_stride, out_stride;
+} lamb_matrix;
+
+/* A list of matrices that are worked on together, with their workspace: about
+ * 4 bytes per element and 4 per entry of the short sides' squares (twice that
+ * with LAMB_NS_SPLIT). One call may be in flight per plan; not thread-safe. */
+typedef struct lamb_ns_plan lamb_ns_plan;
+
+/*
+ * `matrices` (host) has n >= 1 entries; in_dtype and out_dtype are
+ * LAMB_DTYPE_F32 or LAMB_DTYPE_BF16; precision is a lamb_ns_precision.
+ */
+LAMB_API lamb_status lamb_ortho_plan_create(const lamb_matrix *matrices, int32_t n,
+                                            int32_t in_dtype, int32_t out_dtype,
+                                            int32_t precision, lamb_ns_plan **out);
+
+/* Every out becomes the iteration's result for its in. A matrix that holds a NaN
+ * or an infinity becomes NaN; the others are not touched by it. */
+LAMB_API lamb_status lamb_orthogonalize(lamb_ns_plan *plan, const lamb_ns_params *params,
+                                        void *stream);
+
+/*
+ * One matrix of a Muon step: contiguous, row-major. x fp32 parameters and m fp32
+ * momentum are updated in place, g (fp32 or bf16, one type per plan) is read. The
+ * conventions of lamb_tensor hold, and its alignment (16 bytes).
+ */
+typedef struct lamb_muon_tensor {
+    float *x;
+    const void *g;
+    float *m;
+    int64_t rows, cols;
+    int32_t wd;       /* 1: weight decay applies to this matrix */
+    int32_t reserved; /* must be 0 */
+} lamb_muon_tensor;
+
+LAMB_API lamb_status lamb_muon_plan_create(const lamb_muon_tensor *tensors, int32_t n,
+                                           int32_t g_dtype, int32_t precision,
+                                           lamb_ns_plan **out);
+
+/* The factor s of the update: LAMB_MUON_RMS 0.2 sqrt(max(rows, cols)), which gives
+ * the update an Adam step's root mean square; LAMB_MUON_SPECTRAL
+ * sqrt(max(1, rows / cols)); LAMB_MUON_UNIT 1. */
+typedef enum lamb_muon_scale {
+    LAMB_MUON_RMS = 0,
+    LAMB_MUON_SPECTRAL = 1,
+    LAMB_MUON_UNIT = 2
+} lamb_muon_scale;
+
+typedef struct lamb_muon_hparams {
+    lamb_ns_params ns;
+    float lr;            /* >= 0                                                 */
+    float momentum;      /* in [0, 1)                                            */
+    float weight_decay;  /* >= 0, decoupled: x <- (1 - lr weight_decay) x first   */
+    float grad_scale;    /* > 0: every gradient element is multiplied by it       */
+    int32_t nesterov;    /* 0 or 1                                               */
+    int32_t scale;       /* a lamb_muon_scale                                    */
+    int32_t skip_nonfinite; /* 1: a step whose scaled gradient holds a NaN or an
+                               infinity anywhere changes nothing                 */
+    int32_t reserved;    /* must be 0                                            */
+} lamb_muon_hparams;
+
+/* lr 1e-3, momentum 0.95, Nesterov, no decay, LAMB_MUON_RMS, grad_scale 1. */
+LAMB_API lamb_status lamb_muon_hparams_init(lamb_muon_hparams *hp);
+
+/*
+ * g' = grad_scale g;  m <- momentum m + (1 - momentum) g';
+ * u = momentum m + (1 - momentum) g' (Nesterov) or m;  O = the iteration's result for u;
+ * x <- (1 - lr weight_decay wd) x - lr s O.
+ * nonfinite_out (device int32, may be NULL) receives 1 when skip_nonfinite held the
+ * step back, else 0.
+ */
+LAMB_API lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void *stream,
+                                    int32_t *nonfinite_out);
+
+/* Frees either kind of plan; NULL is fine. Waits for the device. */
+LAMB_API lamb_status lamb_ns_plan_destroy(lamb_ns_plan *plan);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* LAMB_OPS_H */

@@ -1,0 +1,306 @@
+// A workgroup's tile of a matrix product D = A B^T on the matrix cores, from
+// 16-bit operands into fp32 accumulators. Device code shared by the kernels of
+// the Newton-Schulz products and of the cross entropy. Not installed.
+//
+// Each operand is one of two kinds, so that no kernel needs a transposed copy:
+//  rows     its rows are D's rows (or columns) and the summed index k runs along
+//           a row: element (i, k) at i * ld + k
+//  columns  its rows are k: element (i, k) at k * ld + i
+// LDS holds a ring of stages, each some values of k of both operands; the loads of
+// all but one run while that one is computed on. Global memory goes
+// there directly (16 bytes a lane), so no register holds data in flight; what
+// lies outside an operand is given an offset past the buffer's length, which the
+// load unit answers with zeros.
+//
+// LDS is written in lane order, so the order of a stage is set by which 16-byte
+// piece each lane asks for. Pieces are swapped within a row (rows: row_slot) or in
+// pairs (columns: column_slot) such that the lanes served together in a fragment
+// read touch every bank once.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace lamb_mi355x {
+
+using half8 = _Float16 __attribute__((ext_vector_type(8)));
+using bf8 = __bf16 __attribute__((ext_vector_type(8)));
+using short4v = short __attribute__((ext_vector_type(4)));
+using short8v = short __attribute__((ext_vector_type(8)));
+using float4v = float __attribute__((ext_vector_type(4)));
+using int4v = int __attribute__((ext_vector_type(4)));
+
+constexpr int kBufferWord3 = 0x00027000;  // raw 32-bit buffer, gfx9
+constexpr int kBufferBytes = 0x7ffffff0;  // a voffset with the sign bit set is outside
+constexpr int kOutside = int(0x80000000u);
+
+#define LAMB_LDS __attribute__((address_space(3)))
+
+struct HalfMath {
+    using Elem = _Float16;
+    static __device__ float4v mma(short8v a, short8v b, float4v c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8, a),
+                                                      __builtin_bit_cast(half8, b), c, 0, 0, 0);
+    }
+};
+
+struct Bf16Math {
+    using Elem = __bf16;
+    static __device__ float4v mma(short8v a, short8v b, float4v c) {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8, a),
+                                                       __builtin_bit_cast(bf8, b), c, 0, 0, 0);
+    }
+};
+
+// An operand of one tile: `base` at the tile's first row (rows) or column
+// (columns) and k = 0, `ld` in bytes, `extent` the rows or columns from there on
+// that exist (columns: in multiples of 8).
+struct Operand {
+    const char *base;
+    int64_t ld;
+    int32_t extent;
+};
+
+// Tile shape: BM x BN by WM x WN waves of 64, STAGES stages of DEPTH values of k
+// each; PARTS 2 for operands that are each the sum of two parts.
+template <int BM_, int BN_, int WM_, int WN_, int DEPTH_, int STAGES_, int PARTS_>
+struct TileShape {
+    static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+    static constexpr int DEPTH = DEPTH_, STAGES = STAGES_, PARTS = PARTS_;
+    static constexpr int kWaves = WM * WN;
+    static constexpr int kThreads = kWaves * 64;
+    static constexpr int MI = BM / WM / 16, NI = BN / WN / 16;
+    static constexpr int kA = BM * DEPTH, kB = BN * DEPTH;  // a part's 16-bit elements
+    static constexpr int kStage = (kA + kB) * PARTS;
+    static constexpr int kLds = kStage * STAGES;
+    static constexpr int kLoads = kStage / 8 / kThreads;  // a lane's loads per stage
+    // workgroups per CU that LDS allows
+    static constexpr int kPerCu = 160 * 1024 / (kLds * 2);
+    static_assert(DEPTH % 32 == 0 && STAGES >= 2 && kPerCu >= 1 && kLoads * (STAGES - 2) < 64, "");
+};
+
+// Bank swizzle of a `rows` stage: 8 rows at the same k get different banks.
+template <int DEPTH>
+__device__ inline int row_slot(int row) {
+    return DEPTH == 64 ? row & 7 : (row >> 1) & 3;
+}
+
+// Bank swizzle of a `columns` stage: rows of k that one fragment read touches
+// (8 q + j, q = 0, 1 together, j = 0..3) get different slots.
+__device__ inline int column_slot(int k) { return (k & 3) | ((k >> 1) & 4); }
+
+// `v`, the same on every lane, in a scalar register that a scalar instruction wrote. A
+// vector instruction's scalar result must not be read by a load within 5 wait states;
+// the compiler sees to that for its own loads, but not for load_to_lds.
+__device__ inline int scalar(int v) {
+    int s;
+    asm volatile("s_mov_b32 %0, %1" : "=s"(s) : "s"(__builtin_amdgcn_readfirstlane(v)));
+    return s;
+}
+
+// 16 bytes a lane from rsrc + off to LDS at `lds` + 16 lane; rsrc's words and lds have
+// been through scalar(). The builtin for this makes the compiler wait for every load
+// in flight before the next LDS read, which would end the overlap of a stage's loads
+// with the stage before; written out, the waiting is tile_product's. The load has no
+// register result, so nothing can be reused under it. (M0 needs one wait state.)
+__device__ inline void load_to_lds(int4v rsrc, int off, int lds) {
+    asm volatile("s_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds"
+                 :
+                 : "v"(off), "s"(rsrc), "{m0}"(lds));
+}
+
+// One operand's share of a stage: EXT rows (or columns) by DEPTH.
+template <int EXT, int DEPTH, int WAVES, bool COLUMNS>
+struct StageLoader {
+    static constexpr int kLoads = EXT * DEPTH / 8 / 64 / WAVES;
+    static_assert(kLoads >= 1 && kLoads * 512 * WAVES == EXT * DEPTH, "whole waves of 16 bytes");
+    static constexpr int kPieces = COLUMNS ? EXT / 8 : DEPTH / 8;  // 16-byte pieces of a stage row
+    static constexpr int kSlots = EXT / 16 < 8 ? EXT / 16 - 1 : 7;  // columns: swap within these
+    static constexpr int kNext = COLUMNS ? 64 / kPieces : 0;  // k from one load to the next
+    int offset[kLoads];  // from the operand's base at the stage's first k
+    int first_k;         // the lane's k in the stage, of its first load
+
+    __device__ void init(const Operand &op, int wave, int lane) {
+#pragma unroll
+        for (int t = 0; t < kLoads; ++t) {
+            const int at = (wave * kLoads + t) * 64 + lane;  // piece of the stage
+            const int row = at / kPieces, p = at % kPieces;
+            if (COLUMNS) {
+                const int col = ((((p >> 1) ^ (column_slot(row) & kSlots)) << 1) | (p & 1)) * 8;
+                offset[t] = col < op.extent ? int(row * op.ld) + col * 2 : kOutside;
+                if (t == 0)
+                    first_k = row;
+            } else {
+                const int k = (p ^ row_slot<DEPTH>(row)) * 8;
+                offset[t] = row < op.extent ? int(row * op.ld) + k * 2 : kOutside;
+                if (t == 0)
+                    first_k = k;  // the same of every load: rows 64 / kPieces apart
+            }
+        }
+    }
+
+    // `src` at the stage's first k, of which `left` remain (none or less: zeros).
+    __device__ void issue(const char *src, int64_t left, const short *stage, int wave) const {
+        const uint64_t at = reinterpret_cast<uint64_t>(src);
+        const int4v rsrc = {scalar(int(at)), scalar(int(at >> 32) & 0xffff), kBufferBytes,
+                            kBufferWord3};
+        const int lds = scalar(int(uintptr_t((LAMB_LDS const short *)stage)) + wave * kLoads * 1024);
+        const bool whole = left >= DEPTH;
+#pragma unroll
+        for (int t = 0; t < kLoads; ++t) {
+            const int off = whole || first_k + t * kNext < left ? offset[t] : kOutside;
+            load_to_lds(rsrc, off, lds + t * 1024);
+        }
+    }
+};
+
+// The fragment of rows first .. first + 15 for k = 32 step + 8 (lane / 16) + 0..7.
+template <int EXT, int DEPTH, bool COLUMNS>
+__device__ inline short8v read_fragment(const short *stage, int first, int step, int lane) {
+    if (COLUMNS) {
+        constexpr int kSlots = EXT / 16 < 8 ? EXT / 16 - 1 : 7;
+        const int k = step * 32 + (lane >> 4) * 8 + ((lane >> 2) & 3);
+        short8v both;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int kk = k + 4 * h;
+            const int pair = (first >> 4) ^ (column_slot(kk) & kSlots);
+            const short4v v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (LAMB_LDS short4v *)(stage + kk * EXT + pair * 16 + (lane & 3) * 4));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) both[4 * h + j] = v[j];
+        }
+        return both;
+    }
+    const int row = first + (lane & 15);
+    const int piece = (step * 4 + (lane >> 4)) ^ row_slot<DEPTH>(row);
+    return *(const short8v *)(stage + row * DEPTH + piece * 8);
+}
+
+// Before a stage is read its loads have landed (every wave waits for its own, of
+// which OPEN later ones may still run, then all meet); the same meeting says that the
+// stage before has been read. The stages' addresses went to the loads, so the
+// compiler takes them as written here.
+template <int OPEN>
+__device__ inline void meet() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(OPEN) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Computes on stages 0 .. count - 1. issue(stage) starts the next one's loads (zeros
+// past the end, so that every turn has the same number of loads in flight). On
+// return no load runs and all of LDS may be written.
+template <class Shape, class Issue, class Compute>
+__device__ inline void run_stages(int32_t count, const short *lds, Issue issue, Compute compute) {
+#pragma unroll
+    for (int s = 0; s < Shape::STAGES - 1; ++s) issue(lds + s * Shape::kStage);
+    const short *reads = lds, *writes = lds + (Shape::STAGES - 1) * Shape::kStage;
+    const short *end = lds + Shape::kLds;
+    auto next = [&](const short *p) {
+        p += Shape::kStage;
+        return p == end ? lds : p;
+    };
+    for (int32_t it = 0; it < count; ++it) {
+        meet<(Shape::STAGES - 2) * Shape::kLoads>();
+        issue(writes);
+        compute(reads);
+        reads = next(reads);
+        writes = next(writes);
+    }
+    meet<0>();
+}
+
+// acc[i][j][r] += D at row 16 i + lane % 16 and column 16 j + 4 (lane / 16) + r of
+// the wave's part, over `depth` values of k.
+//
+// With two parts, `low_a` and `low_b` bytes apart, it sums the products high low, low
+// high and high high. A matrix instruction rounds each of its products to the
+// accumulator's last place, which costs a chain over k = 1024 about 1e-6; so 32 values
+// of k are summed from 0, small products first, and added to the accumulator in one
+// rounding.
+template <class Math, class Shape, bool COLS_A, bool COLS_B>
+__device__ inline void tile_product(float4v (&acc)[Shape::MI][Shape::NI], const short *lds,
+                                    const Operand &a, const Operand &b, int64_t depth,
+                                    int64_t low_a = 0, int64_t low_b = 0) {
+    constexpr int D = Shape::DEPTH, kA = Shape::kA, kB = Shape::kB;
+    constexpr bool kSplit = Shape::PARTS == 2;
+    const int lane = threadIdx.x & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wm = wave / Shape::WN, wn = wave % Shape::WN;
+    StageLoader<Shape::BM, D, Shape::kWaves, COLS_A> la;
+    StageLoader<Shape::BN, D, Shape::kWaves, COLS_B> lb;
+    la.init(a, wave, lane);
+    lb.init(b, wave, lane);
+    const int64_t step_a = COLS_A ? a.ld * D : D * 2;
+    const int64_t step_b = COLS_B ? b.ld * D : D * 2;
+    int32_t left = int32_t(depth);
+    const char *pa = a.base, *pb = b.base;
+    auto issue = [&](const short *s) {
+        la.issue(pa, left, s, wave);
+        if (kSplit)
+            la.issue(pa + low_a, left, s + kA, wave);
+        lb.issue(pb, left, s + Shape::PARTS * kA, wave);
+        if (kSplit)
+            lb.issue(pb + low_b, left, s + 2 * kA + kB, wave);
+        left -= D;
+        if (left > 0) {
+            pa += step_a;
+            pb += step_b;
+        }
+    };
+    auto read_a = [&](const short *s, int i, int step) {
+        return read_fragment<Shape::BM, D, COLS_A>(s, (wm * Shape::MI + i) * 16, step, lane);
+    };
+    auto read_b = [&](const short *s, int j, int step) {
+        return read_fragment<Shape::BN, D, COLS_B>(s + Shape::PARTS * kA,
+                                                   (wn * Shape::NI + j) * 16, step, lane);
+    };
+    auto compute = [&](const short *s) {
+#pragma unroll
+        for (int step = 0; step < D / 32; ++step) {
+            short8v fb[Shape::PARTS][Shape::NI];
+#pragma unroll
+            for (int p = 0; p < Shape::PARTS; ++p)
+#pragma unroll
+                for (int j = 0; j < Shape::NI; ++j) fb[p][j] = read_b(s + p * kB, j, step);
+#pragma unroll
+            for (int i = 0; i < Shape::MI; ++i) {
+                const short8v hi = read_a(s, i, step);
+                if (!kSplit) {
+#pragma unroll
+                    for (int j = 0; j < Shape::NI; ++j)
+                        acc[i][j] = Math::mma(fb[0][j], hi, acc[i][j]);
+                    continue;
+                }
+                const short8v lo = read_a(s + kA, i, step);
+                float4v part[Shape::NI];
+#pragma unroll
+                for (int j = 0; j < Shape::NI; ++j) part[j] = Math::mma(fb[0][j], lo, float4v{});
+#pragma unroll
+                for (int j = 0; j < Shape::NI; ++j)
+                    part[j] = Math::mma(fb[kSplit][j], hi, part[j]);
+#pragma unroll
+                for (int j = 0; j < Shape::NI; ++j) part[j] = Math::mma(fb[0][j], hi, part[j]);
+#pragma unroll
+                for (int j = 0; j < Shape::NI; ++j)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) acc[i][j][r] += part[j][r];
+            }
+        }
+    };
+    run_stages<Shape>(int32_t((depth + D - 1) / D), lds, issue, compute);
+}
+
+// The lane's first value of acc in the tile.
+template <class Shape>
+struct Place {
+    int row, col;
+    __device__ Place() {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        row = wave / Shape::WN * (Shape::BM / Shape::WM) + (lane & 15);
+        col = wave % Shape::WN * (Shape::BN / Shape::WN) + 4 * (lane >> 4);
+    }
+};
+
+}  // namespace lamb_mi355x

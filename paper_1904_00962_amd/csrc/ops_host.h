@@ -1,0 +1,50 @@
+// Host-side helpers shared by the entry points of include/lamb_ops.h. Not
+// installed.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+#include <stdint.h>
+
+#include <exception>
+#include <new>
+#include <vector>
+
+#include "lamb_host.h"
+#include "lamb_ops.h"
+
+namespace lamb_mi355x {
+
+constexpr int kXcds = 8;  // accelerator dies, each with its own L2; blocks go to them in turn
+
+// Workgroup b of `n` runs on die b % kXcds. Gives each die a run of consecutive
+// items, so that tiles that read the same operand rows share an L2.
+template <class T>
+std::vector<T> spread_over_dies(const std::vector<T> &items) {
+    const size_t n = items.size(), each = n / kXcds, more = n % kXcds;
+    std::vector<T> out(n);
+    for (size_t b = 0; b < n; ++b) {
+        const size_t die = b % kXcds, at = b / kXcds;
+        out[b] = items[die * each + (die < more ? die : more) + at];
+    }
+    return out;
+}
+
+// Runs an entry point's body; what it throws becomes a status.
+template <class F>
+lamb_status guarded(F body) noexcept {
+    try {
+        return body();
+    } catch (const std::bad_alloc &) {
+        return fail(LAMB_ENOMEM, "host allocation failed");
+    } catch (const std::exception &e) {
+        return fail(LAMB_EINVAL, "%s", e.what());
+    }
+}
+
+inline bool aligned_to(const void *p, uintptr_t bytes) {
+    return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0;
+}
+
+inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+
+}  // namespace lamb_mi355x

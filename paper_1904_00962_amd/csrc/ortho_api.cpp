@@ -1,0 +1,516 @@
+// Host side of the Newton-Schulz entry points of include/lamb_ops.h: plans
+// (validation, tile lists, workspace) and the launches of a call.
+#include <math.h>
+
+#include <algorithm>
+
+#include "ops_host.h"
+#include "ortho_internal.h"
+
+using namespace lamb_mi355x;
+
+struct lamb_ns_plan {
+    int device = 0;
+    bool muon = false, bf16_in = false, split = false;
+    NsKind kind = kNsBf16Out;
+    int shape = 0;
+    int32_t n = 0, blocks = 0, n_sym = 0, n_update = 0;
+    void *block = nullptr;  // every device buffer of the plan
+    NsMatrix *matrices = nullptr;
+    int32_t *block_matrix = nullptr;
+    NsTile *sym_tiles = nullptr, *update_tiles = nullptr;
+    double *partials = nullptr;
+    uint32_t *flag = nullptr;  // see launch_ns_check
+};
+
+namespace {
+
+constexpr int64_t kMaxSide = int64_t(1) << 20;
+
+// The bounds of lamb_ns_params: where singular values that start in [0, 1] go.
+lamb_status check_params(const lamb_ns_params &p) {
+    if (p.reserved != 0)
+        return fail(LAMB_EINVAL, "ns.reserved must be 0");
+    if (p.steps < 1 || p.steps > 64)
+        return fail(LAMB_EINVAL, "ns.steps = %d, need 1 to 64", p.steps);
+    if (!std::isfinite(p.a) || !std::isfinite(p.b) || !std::isfinite(p.c))
+        return fail(LAMB_EINVAL, "ns coefficients must be finite");
+    if (!(p.eps >= 0.0f) || !std::isfinite(p.eps))
+        return fail(LAMB_EINVAL, "ns.eps = %g, need finite and >= 0", double(p.eps));
+    const double a = p.a, b = p.b, c = p.c;
+    double top = 1.0;
+    for (int k = 0; k < p.steps; ++k) {
+        // extremes over t = s^2 in [0, top^2] of p(t) = a + b t + c t^2 and of
+        // s p(s^2): the ends and the roots of the derivatives
+        const double end = top * top;
+        double largest_p = 0.0, largest_x = 0.0;
+        auto look = [&](double t) {
+            if (!(t >= 0.0 && t <= end))
+                return;
+            const double v = a + t * (b + t * c);
+            largest_p = std::max(largest_p, std::fabs(v));
+            largest_x = std::max(largest_x, std::sqrt(t) * std::fabs(v));
+        };
+        look(0.0);
+        look(end);
+        if (c != 0.0) {
+            look(-b / (2.0 * c));
+            const double d = 9.0 * b * b - 20.0 * a * c;  // a + 3 b t + 5 c t^2 = 0
+            if (d >= 0.0) {
+                look((-3.0 * b + std::sqrt(d)) / (10.0 * c));
+                look((-3.0 * b - std::sqrt(d)) / (10.0 * c));
+            }
+        } else if (b != 0.0) {
+            look(-a / (3.0 * b));
+        }
+        // the last result is not an operand again, but is held to the same bound
+        if (!(largest_p <= kNsLargest) || !(largest_x <= kNsLargestX))
+            return fail(LAMB_EINVAL,
+                        "ns coefficients %g, %g, %g let the polynomial reach %.3g (at most %g) or a "
+                        "singular value %.3g (at most %g) in step %d",
+                        a, b, c, largest_p, kNsLargest, largest_x, kNsLargestX, k + 1);
+        top = largest_x;
+    }
+    return LAMB_OK;
+}
+
+lamb_status check_ranges(std::vector<BufferRange> &ranges) {
+    std::sort(ranges.begin(), ranges.end(), [](const BufferRange &p, const BufferRange &q) {
+        return p.lo != q.lo ? p.lo < q.lo : p.hi < q.hi;
+    });
+    // an input may share memory with other inputs, a written buffer with nothing
+    uintptr_t in_hi = 0, out_hi = 0;
+    int32_t in_of = 0, out_of = 0;
+    for (const BufferRange &r : ranges) {
+        const bool written = r.what[0] != 'i' && r.what[0] != 'g';
+        if (r.lo < out_hi || (written && r.lo < in_hi))
+            return fail(LAMB_EOVERLAP, "matrix %d %s overlaps a buffer of matrix %d", r.tensor,
+                        r.what, r.lo < out_hi ? out_of : in_of);
+        if (written && r.hi > out_hi)
+            out_hi = r.hi, out_of = r.tensor;
+        if (!written && r.hi > in_hi)
+            in_hi = r.hi, in_of = r.tensor;
+    }
+    return LAMB_OK;
+}
+
+// A product takes the largest tiles that still fill the device: kFill workgroups.
+// Split products have no large shape.
+constexpr int64_t kFill = 512;
+
+int pick_shape(const std::vector<NsMatrix> &matrices, bool split) {
+    for (int shape = split ? kNsSmall : kNsLarge; shape > kNsTiny; --shape) {
+        int64_t tiles = 0;
+        for (const NsMatrix &m : matrices)
+            tiles += (round_up(m.rows, ns_tile_rows(shape)) / ns_tile_rows(shape)) *
+                     (round_up(m.cols, ns_tile_cols(shape)) / ns_tile_cols(shape));
+        if (tiles >= kFill)
+            return shape;
+    }
+    return kNsTiny;
+}
+
+template <class F>
+void for_tiles(int32_t rows, int32_t cols, int shape, F f) {
+    const int64_t h = ns_tile_rows(shape), w = ns_tile_cols(shape);
+    for (int32_t r = 0; r * h < rows; ++r)
+        for (int32_t c = 0; c * w < cols; ++c) f(r, c);
+}
+
+// Fills in sizes, tiles and workspace; `matrices` has its user's fields set.
+lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
+    plan->n = int32_t(matrices.size());
+    plan->shape = pick_shape(matrices, plan->split);
+    const int64_t tile_rows = ns_tile_rows(plan->shape), tile_cols = ns_tile_cols(plan->shape);
+
+    // Longest products first, so that the last workgroups are short ones.
+    std::vector<int32_t> order(matrices.size());
+    for (size_t i = 0; i < order.size(); ++i) order[i] = int32_t(i);
+    auto side = [&](int32_t i) { return std::min(matrices[i].rows, matrices[i].cols); };
+    auto longest = [&](int32_t i) { return std::max(matrices[i].rows, matrices[i].cols); };
+
+    std::vector<NsTile> sym, update;
+    std::vector<int32_t> block_matrix;
+    int64_t elems = 0, blocks = 0;  // workspace, in 16-bit elements
+    std::vector<int64_t> at_x(matrices.size()), at_gram(matrices.size());
+    const int parts = plan->split ? 2 : 1;
+    for (size_t i = 0; i < matrices.size(); ++i) {
+        NsMatrix &m = matrices[i];
+        m.tall = m.rows > m.cols;
+        m.side = std::min(m.rows, m.cols);
+        m.ld = int32_t(round_up(m.cols, 8));
+        m.side_ld = int32_t(round_up(m.side, 8));
+        m.x_low = round_up(int64_t(m.rows) * m.ld, 64);
+        m.gram_low = round_up(int64_t(m.side) * m.side_ld, 64);
+        at_x[i] = elems;
+        elems += 2 * parts * m.x_low;
+        at_gram[i] = elems;
+        elems += 2 * parts * m.gram_low;
+        const int64_t units = int64_t(m.rows) * (m.ld / 8);
+        const int64_t count = (units + kNsBlockUnits - 1) / kNsBlockUnits;
+        if (blocks + count > INT32_MAX)
+            return fail(LAMB_EINVAL, "the matrices hold too many elements for one plan");
+        m.first_block = int32_t(blocks);
+        m.blocks = int32_t(count);
+        blocks += count;
+        block_matrix.insert(block_matrix.end(), size_t(count), int32_t(i));
+    }
+    plan->blocks = int32_t(blocks);
+    std::stable_sort(order.begin(), order.end(),
+                     [&](int32_t p, int32_t q) { return longest(p) > longest(q); });
+    for (int32_t i : order)
+        for_tiles(side(i), side(i), plan->shape, [&](int32_t r, int32_t c) {
+            if (c * tile_cols < (r + 1) * tile_rows)  // not wholly above the diagonal
+                sym.push_back(NsTile{i, r, c});
+        });
+    std::stable_sort(order.begin(), order.end(),
+                     [&](int32_t p, int32_t q) { return side(p) > side(q); });
+    for (int32_t i : order)
+        for_tiles(matrices[i].rows, matrices[i].cols, plan->shape,
+                  [&](int32_t r, int32_t c) { update.push_back(NsTile{i, r, c}); });
+    if (sym.size() > INT32_MAX || update.size() > INT32_MAX)
+        return fail(LAMB_EINVAL, "the matrices take too many tiles for one plan");
+    sym = spread_over_dies(sym);
+    update = spread_over_dies(update);
+    plan->n_sym = int32_t(sym.size());
+    plan->n_update = int32_t(update.size());
+
+    size_t bytes = 0;
+    auto take = [&](size_t size) {
+        const size_t at = bytes;
+        bytes += size_t(round_up(int64_t(size), 256));
+        return at;
+    };
+    const size_t o_work = take(size_t(elems) * 2);
+    const size_t o_matrices = take(matrices.size() * sizeof(NsMatrix));
+    const size_t o_blocks = take(block_matrix.size() * 4);
+    const size_t o_sym = take(sym.size() * sizeof(NsTile));
+    const size_t o_update = take(update.size() * sizeof(NsTile));
+    const size_t o_partials = take(size_t(blocks) * 8);
+    const size_t o_flag = take(8);
+    hipError_t err = hipGetDevice(&plan->device);
+    if (err != hipSuccess)
+        return fail_hip(err, "hipGetDevice");
+    err = hipMalloc(&plan->block, bytes);
+    if (err != hipSuccess) {
+        plan->block = nullptr;
+        (void)hipGetLastError();
+        return fail(LAMB_ENOMEM, "hipMalloc of %zu bytes: %s", bytes, hipGetErrorString(err));
+    }
+    char *base = static_cast<char *>(plan->block);
+    uint16_t *work = reinterpret_cast<uint16_t *>(base + o_work);
+    for (size_t i = 0; i < matrices.size(); ++i) {
+        NsMatrix &m = matrices[i];
+        m.x[0] = work + at_x[i];
+        m.x[1] = m.x[0] + parts * m.x_low;
+        m.gram = work + at_gram[i];
+        m.poly = m.gram + parts * m.gram_low;
+    }
+    plan->matrices = reinterpret_cast<NsMatrix *>(base + o_matrices);
+    plan->block_matrix = reinterpret_cast<int32_t *>(base + o_blocks);
+    plan->sym_tiles = reinterpret_cast<NsTile *>(base + o_sym);
+    plan->update_tiles = reinterpret_cast<NsTile *>(base + o_update);
+    plan->partials = reinterpret_cast<double *>(base + o_partials);
+    plan->flag = reinterpret_cast<uint32_t *>(base + o_flag);
+    auto up = [&](void *to, const void *from, size_t size) {
+        if (err == hipSuccess)
+            err = hipMemcpy(to, from, size, hipMemcpyHostToDevice);
+    };
+    up(plan->matrices, matrices.data(), matrices.size() * sizeof(NsMatrix));
+    up(plan->block_matrix, block_matrix.data(), block_matrix.size() * 4);
+    up(plan->sym_tiles, sym.data(), sym.size() * sizeof(NsTile));
+    up(plan->update_tiles, update.data(), update.size() * sizeof(NsTile));
+    const uint32_t zero[2] = {};
+    up(plan->flag, zero, sizeof zero);
+    if (err != hipSuccess)
+        return fail_hip(err, "hipMemcpy");
+    return LAMB_OK;
+}
+
+struct DeviceScope {
+    int previous = -1;
+    explicit DeviceScope(int device) {
+        if (hipGetDevice(&previous) == hipSuccess && previous != device)
+            (void)hipSetDevice(device);
+        else
+            previous = -1;
+    }
+    ~DeviceScope() {
+        if (previous >= 0)
+            (void)hipSetDevice(previous);
+    }
+};
+
+lamb_status run(lamb_ns_plan *plan, const lamb_ns_params &ns, NsStep step, uint32_t *flag,
+                int32_t *nonfinite_out, hipStream_t stream) {
+    step.a = ns.a;
+    step.b = ns.b;
+    step.c = ns.c;
+    step.eps = ns.eps;
+    hipError_t err = launch_ns_norms(plan->matrices, plan->block_matrix, plan->blocks, plan->muon,
+                                     plan->bf16_in, step, plan->partials, flag, nonfinite_out,
+                                     stream);
+    if (err == hipSuccess)
+        err = launch_ns_convert(plan->matrices, plan->block_matrix, plan->blocks, plan->muon,
+                                plan->bf16_in, plan->split, step, plan->partials, flag, stream);
+    for (int32_t k = 0; k < ns.steps && err == hipSuccess; ++k) {
+        const int parity = k & 1;
+        err = launch_ns_gram(plan->matrices, plan->sym_tiles, plan->n_sym, plan->shape,
+                             plan->split, parity, stream);
+        if (err == hipSuccess)
+            err = launch_ns_poly(plan->matrices, plan->sym_tiles, plan->n_sym, plan->shape,
+                                 plan->split, step, stream);
+        if (err == hipSuccess)
+            err = launch_ns_update(plan->matrices, plan->update_tiles, plan->n_update, plan->shape,
+                                   plan->split, parity, k + 1 == ns.steps, plan->kind, step, flag,
+                                   stream);
+    }
+    if (err != hipSuccess)
+        return fail_hip(err, "kernel launch");
+    return LAMB_OK;
+}
+
+lamb_status check_side(int32_t i, int64_t rows, int64_t cols) {
+    if (rows < 1 || rows > kMaxSide || cols < 1 || cols > kMaxSide)
+        return fail(LAMB_EINVAL, "matrix %d is %lld x %lld, need 1 to 2^20 each", i,
+                    static_cast<long long>(rows), static_cast<long long>(cols));
+    return LAMB_OK;
+}
+
+lamb_status finish(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices, lamb_ns_plan **out) {
+    const lamb_status st = guarded([&] { return build(plan, matrices); });
+    if (st != LAMB_OK) {
+        if (plan->block)
+            (void)hipFree(plan->block);
+        delete plan;
+        return st;
+    }
+    *out = plan;
+    return LAMB_OK;
+}
+
+lamb_status check_precision(int32_t precision) {
+    if (precision != LAMB_NS_HALF && precision != LAMB_NS_SPLIT)
+        return fail(LAMB_EINVAL, "unknown precision %d", precision);
+    return LAMB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+lamb_status lamb_ns_params_init(lamb_ns_params *params) {
+    if (!params)
+        return fail(LAMB_ENULL, "params must not be NULL");
+    *params = lamb_ns_params{5, 3.4445f, -4.7750f, 2.0315f, 1e-7f, 0};
+    return LAMB_OK;
+}
+
+lamb_status lamb_muon_hparams_init(lamb_muon_hparams *hp) {
+    if (!hp)
+        return fail(LAMB_ENULL, "hparams must not be NULL");
+    *hp = lamb_muon_hparams{};
+    (void)lamb_ns_params_init(&hp->ns);
+    hp->lr = 1e-3f;
+    hp->momentum = 0.95f;
+    hp->grad_scale = 1.0f;
+    hp->nesterov = 1;
+    hp->scale = LAMB_MUON_RMS;
+    return LAMB_OK;
+}
+
+lamb_status lamb_ortho_plan_create(const lamb_matrix *matrices, int32_t n, int32_t in_dtype,
+                                   int32_t out_dtype, int32_t precision, lamb_ns_plan **out) {
+    if (!out)
+        return fail(LAMB_ENULL, "out must not be NULL");
+    *out = nullptr;
+    if (!matrices)
+        return fail(LAMB_ENULL, "matrices must not be NULL");
+    if (n < 1)
+        return fail(LAMB_EINVAL, "n = %d, need >= 1", n);
+    if ((in_dtype != LAMB_DTYPE_F32 && in_dtype != LAMB_DTYPE_BF16) ||
+        (out_dtype != LAMB_DTYPE_F32 && out_dtype != LAMB_DTYPE_BF16))
+        return fail(LAMB_EINVAL, "matrices are float32 or bfloat16");
+    lamb_status st = check_precision(precision);
+    if (st != LAMB_OK)
+        return st;
+    return guarded([&]() -> lamb_status {
+        const int64_t in_size = in_dtype == LAMB_DTYPE_BF16 ? 2 : 4;
+        const int64_t out_size = out_dtype == LAMB_DTYPE_BF16 ? 2 : 4;
+        std::vector<NsMatrix> list;
+        std::vector<BufferRange> ranges;
+        for (int32_t i = 0; i < n; ++i) {
+            const lamb_matrix &t = matrices[i];
+            if (!t.in || !t.out)
+                return fail(LAMB_ENULL, "matrix %d: in and out must not be NULL", i);
+            lamb_status s = check_side(i, t.rows, t.cols);
+            if (s != LAMB_OK)
+                return s;
+            if (t.in_stride < t.cols || t.out_stride < t.cols || t.in_stride > kMaxNumel ||
+                t.out_stride > kMaxNumel)
+                return fail(LAMB_EINVAL, "matrix %d: a row stride is below its %lld columns", i,
+                            static_cast<long long>(t.cols));
+            if (!aligned_to(t.in, uintptr_t(in_size)) || !aligned_to(t.out, uintptr_t(out_size)))
+                return fail(LAMB_EALIGN, "matrix %d: a pointer is not aligned to its elements", i);
+            const uintptr_t in = reinterpret_cast<uintptr_t>(t.in);
+            const uintptr_t to = reinterpret_cast<uintptr_t>(t.out);
+            const uintptr_t in_len = uintptr_t((t.rows - 1) * t.in_stride + t.cols) *
+                                     uintptr_t(in_size);
+            const uintptr_t out_len = uintptr_t((t.rows - 1) * t.out_stride + t.cols) *
+                                      uintptr_t(out_size);
+            const bool in_place = in == to && in_dtype == out_dtype && t.in_stride == t.out_stride;
+            if (!in_place)
+                ranges.push_back(BufferRange{in, in + in_len, i, "in"});
+            ranges.push_back(BufferRange{to, to + out_len, i, "out"});
+            NsMatrix m{};
+            m.in = t.in;
+            m.out = t.out;
+            m.rows = int32_t(t.rows);
+            m.cols = int32_t(t.cols);
+            m.in_stride = t.in_stride;
+            m.out_stride = t.out_stride;
+            m.vector = aligned_to(t.in, 16) && aligned_to(t.out, 16) &&
+                       t.in_stride * in_size % 16 == 0 && t.out_stride * out_size % 16 == 0;
+            list.push_back(m);
+        }
+        lamb_status s = check_ranges(ranges);
+        if (s != LAMB_OK)
+            return s;
+        lamb_ns_plan *plan = new lamb_ns_plan;
+        plan->bf16_in = in_dtype == LAMB_DTYPE_BF16;
+        plan->split = precision == LAMB_NS_SPLIT;
+        plan->kind = out_dtype == LAMB_DTYPE_BF16 ? kNsBf16Out : kNsF32Out;
+        return finish(plan, list, out);
+    });
+}
+
+lamb_status lamb_muon_plan_create(const lamb_muon_tensor *tensors, int32_t n, int32_t g_dtype,
+                                  int32_t precision, lamb_ns_plan **out) {
+    if (!out)
+        return fail(LAMB_ENULL, "out must not be NULL");
+    *out = nullptr;
+    if (!tensors)
+        return fail(LAMB_ENULL, "tensors must not be NULL");
+    if (n < 1)
+        return fail(LAMB_EINVAL, "n = %d, need >= 1", n);
+    if (g_dtype != LAMB_DTYPE_F32 && g_dtype != LAMB_DTYPE_BF16)
+        return fail(LAMB_EINVAL, "gradients are float32 or bfloat16");
+    lamb_status st = check_precision(precision);
+    if (st != LAMB_OK)
+        return st;
+    return guarded([&]() -> lamb_status {
+        std::vector<NsMatrix> list;
+        std::vector<BufferRange> ranges;
+        for (int32_t i = 0; i < n; ++i) {
+            const lamb_muon_tensor &t = tensors[i];
+            if (!t.x || !t.g || !t.m)
+                return fail(LAMB_ENULL, "matrix %d: x, g and m must not be NULL", i);
+            lamb_status s = check_side(i, t.rows, t.cols);
+            if (s != LAMB_OK)
+                return s;
+            if (t.wd != 0 && t.wd != 1)
+                return fail(LAMB_EINVAL, "matrix %d: wd must be 0 or 1", i);
+            if (t.reserved != 0)
+                return fail(LAMB_EINVAL, "matrix %d: reserved field must be 0", i);
+            if (!aligned_to(t.x, 16) || !aligned_to(t.g, 16) || !aligned_to(t.m, 16))
+                return fail(LAMB_EALIGN, "matrix %d: every buffer must be 16-byte aligned", i);
+            const uintptr_t numel = uintptr_t(t.rows) * uintptr_t(t.cols);
+            auto add = [&](const void *p, uintptr_t bytes, const char *what) {
+                const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+                ranges.push_back(BufferRange{lo, lo + bytes, i, what});
+            };
+            add(t.x, numel * 4, "x");
+            add(t.g, numel * (g_dtype == LAMB_DTYPE_BF16 ? 2 : 4), "g");
+            add(t.m, numel * 4, "m");
+            NsMatrix m{};
+            m.in = t.g;
+            m.out = t.x;
+            m.m = t.m;
+            m.rows = int32_t(t.rows);
+            m.cols = int32_t(t.cols);
+            m.in_stride = m.out_stride = t.cols;
+            m.vector = t.cols % 8 == 0;
+            m.wd = t.wd;
+            list.push_back(m);
+        }
+        lamb_status s = check_ranges(ranges);
+        if (s != LAMB_OK)
+            return s;
+        lamb_ns_plan *plan = new lamb_ns_plan;
+        plan->muon = true;
+        plan->bf16_in = g_dtype == LAMB_DTYPE_BF16;
+        plan->split = precision == LAMB_NS_SPLIT;
+        plan->kind = kNsMuon;
+        return finish(plan, list, out);
+    });
+}
+
+lamb_status lamb_orthogonalize(lamb_ns_plan *plan, const lamb_ns_params *params, void *stream) {
+    if (!plan || !params)
+        return fail(LAMB_ENULL, "plan and params must not be NULL");
+    if (plan->muon)
+        return fail(LAMB_EPLAN, "the plan was created for lamb_muon_step");
+    lamb_status st = check_params(*params);
+    if (st != LAMB_OK)
+        return st;
+    DeviceScope scope(plan->device);
+    return run(plan, *params, NsStep{}, nullptr, nullptr, static_cast<hipStream_t>(stream));
+}
+
+lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void *stream_in,
+                           int32_t *nonfinite_out) {
+    if (!plan || !hp)
+        return fail(LAMB_ENULL, "plan and hparams must not be NULL");
+    if (!plan->muon)
+        return fail(LAMB_EPLAN, "the plan was created for lamb_orthogonalize");
+    lamb_status st = check_params(hp->ns);
+    if (st != LAMB_OK)
+        return st;
+    if (!std::isfinite(hp->lr) || hp->lr < 0.0f)
+        return fail(LAMB_EINVAL, "lr = %g, need finite and >= 0", double(hp->lr));
+    if (!(hp->momentum >= 0.0f && hp->momentum < 1.0f))
+        return fail(LAMB_EINVAL, "momentum = %g outside [0, 1)", double(hp->momentum));
+    if (!std::isfinite(hp->weight_decay) || hp->weight_decay < 0.0f)
+        return fail(LAMB_EINVAL, "weight_decay = %g, need finite and >= 0",
+                    double(hp->weight_decay));
+    if (!std::isfinite(hp->grad_scale) || hp->grad_scale <= 0.0f)
+        return fail(LAMB_EINVAL, "grad_scale = %g, need finite and > 0", double(hp->grad_scale));
+    if ((hp->nesterov | hp->skip_nonfinite) & ~1)
+        return fail(LAMB_EINVAL, "nesterov and skip_nonfinite must be 0 or 1");
+    if (hp->scale < LAMB_MUON_RMS || hp->scale > LAMB_MUON_UNIT)
+        return fail(LAMB_EINVAL, "unknown scale %d", hp->scale);
+    if (hp->reserved != 0)
+        return fail(LAMB_EINVAL, "hparams.reserved must be 0");
+    hipStream_t stream = static_cast<hipStream_t>(stream_in);
+    DeviceScope scope(plan->device);
+    NsStep step{};
+    step.momentum = hp->momentum;
+    step.one_minus = float(1.0 - double(hp->momentum));
+    step.grad_scale = hp->grad_scale;
+    step.decay = float(1.0 - double(hp->lr) * double(hp->weight_decay));
+    step.lr = hp->lr;
+    step.nesterov = hp->nesterov;
+    step.scale = hp->scale;
+    uint32_t *flag = nullptr;
+    if (hp->skip_nonfinite) {
+        const hipError_t err = launch_ns_check(plan->matrices, plan->block_matrix, plan->blocks,
+                                               plan->bf16_in, hp->grad_scale, plan->flag, stream);
+        if (err != hipSuccess)
+            return fail_hip(err, "kernel launch");
+        flag = plan->flag;
+    }
+    return run(plan, hp->ns, step, flag, nonfinite_out, stream);
+}
+
+lamb_status lamb_ns_plan_destroy(lamb_ns_plan *plan) {
+    if (!plan)
+        return LAMB_OK;
+    DeviceScope scope(plan->device);
+    const hipError_t err = hipFree(plan->block);
+    delete plan;
+    if (err != hipSuccess)
+        return fail_hip(err, "hipFree");
+    return LAMB_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,89 @@
+// Layout shared by the kernels of the Newton-Schulz products (ortho_kernels.hip)
+// and their host side (ortho_api.cpp). Not installed; the public interface is
+// include/lamb_ops.h.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+#include <stdint.h>
+
+namespace lamb_mi355x {
+
+// X, A and P are held as 16-bit floats times kNsScale. Their entries are at most
+// their largest singular value, which the host keeps under kNsLargest for P and
+// kNsLargestX for X, so kNsScale times that stays below the format's 65504; and
+// an entry of 2^-14, about the smallest of a 16384 x 16384 matrix, is still a normal
+// number with a normal low part.
+constexpr float kNsScale = 8192.0f;
+constexpr double kNsLargest = 7.75, kNsLargestX = 2.75;
+
+// Elements per workgroup of the elementwise passes, in units of 8 columns.
+constexpr int kNsBlock = 256;
+constexpr int kNsUnits = 4;  // units per thread
+constexpr int kNsBlockUnits = kNsBlock * kNsUnits;
+
+// One matrix. `tall`: rows > cols, and A = X^T X, X <- X P; else A = X X^T, X <- P X.
+struct NsMatrix {
+    const void *in;     // orthogonalize: the input; Muon: the gradient
+    void *out;          // orthogonalize: the output; Muon: the parameters x
+    float *m;           // Muon: the momentum
+    uint16_t *x[2];     // X of even and odd iterations, [rows][ld]; low parts x_low further
+    uint16_t *gram;     // A, [side][side_ld]; low parts gram_low further
+    uint16_t *poly;     // P, likewise
+    int64_t in_stride, out_stride;
+    int64_t x_low, gram_low;
+    int32_t rows, cols, ld, side, side_ld, tall;
+    int32_t first_block, blocks;  // its workgroups of the elementwise passes
+    int32_t vector;               // rows of in, out and m allow 16-byte accesses
+    int32_t wd;                   // Muon: decay applies
+};
+static_assert(sizeof(NsMatrix) == 128, "NsMatrix layout");
+
+// One tile of a product.
+struct NsTile {
+    int32_t matrix;
+    int32_t row, col;  // in tiles
+};
+
+// Tile shapes of the products, rows by columns.
+enum NsShape : int32_t { kNsTiny = 0, kNsSmall = 1, kNsLarge = 2 };
+constexpr int32_t ns_tile_rows(int32_t shape) { return 64 << shape; }
+constexpr int32_t ns_tile_cols(int32_t shape) { return shape == kNsTiny ? 64 : 128; }
+
+enum NsKind : int32_t { kNsBf16Out = 0, kNsF32Out = 1, kNsMuon = 2 };
+
+struct NsStep {
+    float a, b, c;
+    float eps;
+    // Muon
+    float momentum, one_minus;  // m <- momentum m + one_minus grad_scale g
+    float grad_scale;
+    float decay;                // x <- decay x - lr s O (decay 1 where the mask is off)
+    float lr;
+    int32_t nesterov;
+    int32_t scale;              // a lamb_muon_scale
+};
+
+// Elementwise passes over `blocks` workgroups (block_matrix: each one's matrix).
+// `flag` non-null: a skip_nonfinite step. The check raises flag[0], the norm pass
+// obeys it and copies it to flag[1], which the last update obeys, and the convert
+// pass clears it for the next step; nothing depends on a host counter.
+hipError_t launch_ns_check(const NsMatrix *matrices, const int32_t *block_matrix, int32_t blocks,
+                           bool bf16_in, float grad_scale, uint32_t *flag, hipStream_t stream);
+hipError_t launch_ns_norms(const NsMatrix *matrices, const int32_t *block_matrix, int32_t blocks,
+                           bool muon, bool bf16_in, const NsStep &step, double *partials,
+                           uint32_t *flag, int32_t *nonfinite_out, hipStream_t stream);
+hipError_t launch_ns_convert(const NsMatrix *matrices, const int32_t *block_matrix,
+                             int32_t blocks, bool muon, bool bf16_in, bool split,
+                             const NsStep &step, const double *partials, uint32_t *flag,
+                             hipStream_t stream);
+// Products over `n` tiles of shape `shape`.
+hipError_t launch_ns_gram(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
+                          bool split, int parity, hipStream_t stream);
+hipError_t launch_ns_poly(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
+                          bool split, const NsStep &step, hipStream_t stream);
+// `last`: the result goes to `out` as `kind` says, else to the other X.
+hipError_t launch_ns_update(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
+                            bool split, int parity, bool last, NsKind kind, const NsStep &step,
+                            const uint32_t *flag, hipStream_t stream);
+
+}  // namespace lamb_mi355x

@@ -27,7 +27,7 @@ from __future__ import annotations
 
 from typing import Optional, Sequence, Tuple
 
-from . import _lib
+from . import _lib, _ops
 
 
 def _torch():
@@ -331,3 +331,95 @@ class LARS(_LayerwiseOptimizer):
         self._t = int(state["step"])
         for dst, src in zip(self.m, state["m"]):
             dst.copy_(src)
+
+
+class Muon:
+    """Momentum whose direction is orthogonalized by Newton-Schulz products, for a
+    model's matrices (vectors and token tables are better served by ``LAMB``).
+
+    Per matrix: m <- momentum m + (1 - momentum) g; u = momentum m + (1 - momentum) g
+    (``nesterov``) or m; O = u with its singular values moved towards 1
+    (``ops.Orthogonalizer``); x <- (1 - lr weight_decay) x - lr s O. ``scale`` picks s:
+    "rms" 0.2 sqrt(max(rows, cols)), which gives O an Adam step's root mean square and
+    so lets its learning rate be used; "spectral" sqrt(max(1, rows / cols)); "unit" 1.
+
+    ``params`` are contiguous float32 tensors of two or more dimensions, seen as
+    [shape[0], rest]; ``grads`` as for ``LAMB``. ``m``: momentum buffers to use (one
+    contiguous float32 tensor per parameter; default: new ones, zero). ``wd_mask``:
+    which matrices decay (default: all). ``precision``: "split" keeps the products at
+    fp32's accuracy; "half" is about three times faster and moves the direction by
+    1e-3 to 7e-3, less than bfloat16 products do. ``grad_scale``, ``skip_nonfinite`` and
+    ``schedule`` as for ``LAMB``; a skipped step sets ``found_nonfinite``.
+    """
+
+    def __init__(self, params: Sequence, grads: Sequence, lr: float = 1e-3,
+                 momentum: float = 0.95, weight_decay: float = 0.0, nesterov: bool = True,
+                 scale: str = "rms", steps: int = 5,
+                 coefficients: Tuple[float, float, float] = (3.4445, -4.7750, 2.0315),
+                 eps: float = 1e-7, precision: str = "split", m: Optional[Sequence] = None,
+                 wd_mask: Optional[Sequence[bool]] = None, grad_scale: float = 1.0,
+                 skip_nonfinite: bool = False, schedule=None):
+        torch = _torch()
+        self.params = list(params)
+        self.grads = list(grads)
+        g_dtype, self.device = _check_tensors(self.params, self.grads)
+        for i, p in enumerate(self.params):
+            if p.dim() < 2:
+                raise ValueError("parameter %d has %d dimensions; Muon steps matrices"
+                                 % (i, p.dim()))
+        if scale not in _ops.SCALES:
+            raise ValueError("scale must be one of %s" % (tuple(_ops.SCALES),))
+        if precision not in _ops.PRECISIONS:
+            raise ValueError("precision must be one of %s" % (tuple(_ops.PRECISIONS),))
+        self.m = ([torch.zeros_like(p) for p in self.params] if m is None else list(m))
+        if len(self.m) != len(self.params):
+            raise ValueError("need one momentum buffer per parameter tensor")
+        for i, (p, t) in enumerate(zip(self.params, self.m)):
+            if t.dtype != torch.float32 or t.device != self.device or not t.is_contiguous():
+                raise TypeError("momentum %d must be a contiguous float32 tensor on %s"
+                                % (i, self.device))
+            if t.numel() != p.numel():
+                raise ValueError("momentum %d has %d elements, parameter %d"
+                                 % (i, t.numel(), p.numel()))
+        self.wd_mask = ([True] * len(self.params) if wd_mask is None
+                        else [bool(w) for w in wd_mask])
+        if len(self.wd_mask) != len(self.params):
+            raise ValueError("wd_mask needs one entry per tensor")
+        self.lr = float(lr)
+        self.schedule = [tuple(s) for s in schedule] if schedule else None
+        self.found_nonfinite = torch.zeros(1, dtype=torch.int32, device=self.device)
+        ns = _ops.lamb_ns_params_init(steps=int(steps), a=coefficients[0], b=coefficients[1],
+                                      c=coefficients[2], eps=eps)
+        self.hparams = _ops.lamb_muon_hparams_init(
+            ns, momentum=momentum, weight_decay=weight_decay, nesterov=int(bool(nesterov)),
+            scale=scale, grad_scale=grad_scale, skip_nonfinite=int(bool(skip_nonfinite)))
+        rows = [(p.data_ptr(), g.data_ptr(), t.data_ptr(), p.shape[0], p.numel() // p.shape[0],
+                 int(w)) for p, g, t, w in zip(self.params, self.grads, self.m, self.wd_mask)]
+        with torch.cuda.device(self.device):
+            self.plan = _ops.lamb_muon_plan_create(
+                rows, _ops.LAMB_DTYPE_BF16 if g_dtype == torch.bfloat16 else _ops.LAMB_DTYPE_F32,
+                _ops.PRECISIONS[precision])
+        self.t = 0
+
+    def step(self, lr: Optional[float] = None) -> None:
+        """One step on the current stream. ``t`` counts the calls, skipped steps among
+        them."""
+        self.t += 1
+        if lr is None:
+            lr = _lib.lamb_lr_at(self.schedule, self.t) if self.schedule else self.lr
+        self.hparams.lr = lr
+        stream = _torch().cuda.current_stream(self.device).cuda_stream
+        _ops.lamb_muon_step(self.plan, self.hparams, stream,
+                            self.found_nonfinite.data_ptr() if self.hparams.skip_nonfinite else 0)
+
+    def state_dict(self):
+        return {"step": self.t, "m": [m.clone() for m in self.m]}
+
+    def load_state_dict(self, state) -> None:
+        _check_state(state, {"m": self.m})
+        self.t = int(state["step"])
+        for dst, src in zip(self.m, state["m"]):
+            dst.copy_(src.reshape(dst.shape))
+
+    def close(self) -> None:
+        self.plan.close()
