@@ -145,6 +145,65 @@ LAMB_API lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams 
 /* Frees either kind of plan; NULL is fine. Waits for the device. */
 LAMB_API lamb_status lamb_ns_plan_destroy(lamb_ns_plan *plan);
 
+/*
+ * Softmax cross entropy of hidden states against a vocabulary table:
+ * logits = hidden table^T, loss_i = logsumexp(logits_i) - logits_i[target_i].
+ * hidden [tokens][dim] and table [vocab][dim] are bfloat16, rows `*_stride` elements
+ * apart (>= dim), 2-byte aligned. They are read in place where rows are 16-byte
+ * aligned and dim is a multiple of 8; else the table is copied to the workspace first.
+ * targets: LAMB_DTYPE_I32 or _I64. A token whose target is ignore_index does not
+ * count: its loss and gradient are 0 and nothing that its row holds reaches any
+ * result. Any other target outside [0, vocab) makes that token's loss and lse NaN, and
+ * with them the mean and the gradients.
+ * tokens 0 to 2^24, vocab 1 to 2^24, dim 1 to 2^16.
+ */
+typedef struct lamb_xent {
+    const void *hidden;
+    const void *table;
+    const void *targets;
+    int64_t hidden_stride, table_stride;
+    int64_t tokens, vocab, dim;
+    int64_t ignore_index;
+    int32_t target_dtype;
+    int32_t reserved; /* must be 0 */
+} lamb_xent;
+
+/* Bytes of device workspace (256-byte aligned) that a forward and a backward call need;
+ * host only. The backward holds a piece of the vocabulary's softmax, at most about
+ * 128 MiB, beside the hidden states and their gradient in fp32. */
+LAMB_API lamb_status lamb_xent_workspace(const lamb_xent *xent, size_t *forward_bytes,
+                                         size_t *backward_bytes);
+
+/*
+ * loss and lse: device float[tokens], fp32 (lse is what the backward needs). mean:
+ * device float, the sum of the losses over the number of tokens that count (0 when
+ * none does), or NULL.
+ */
+LAMB_API lamb_status lamb_xent_forward(const lamb_xent *xent, float *loss, float *lse, float *mean,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Gradients of grad_scale grad_loss times the mean (`mean` 1) or the sum (0) of the
+ * losses, given the forward's lse. grad_loss: device float, or NULL for 1.
+ * grad_hidden: bfloat16 [tokens][dim], or NULL. grad_table: [vocab][dim] of
+ * grad_table_dtype (LAMB_DTYPE_F32 or _BF16), written, or added to (`add_table` 1);
+ * NULL for none.
+ */
+typedef struct lamb_xent_grads {
+    const float *grad_loss;
+    void *grad_hidden;
+    void *grad_table;
+    int64_t grad_hidden_stride, grad_table_stride;
+    int32_t grad_table_dtype;
+    int32_t add_table;
+    int32_t mean;
+    float grad_scale;
+} lamb_xent_grads;
+
+LAMB_API lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
+                                        const lamb_xent_grads *grads, void *workspace,
+                                        size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

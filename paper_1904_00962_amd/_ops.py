@@ -29,7 +29,8 @@ SCALES = {"rms": LAMB_MUON_RMS, "spectral": LAMB_MUON_SPECTRAL, "unit": LAMB_MUO
 # Every symbol include/lamb_ops.h declares (checked by the test suite).
 EXPORTS = ("lamb_ns_params_init", "lamb_ortho_plan_create", "lamb_orthogonalize",
            "lamb_muon_plan_create", "lamb_muon_hparams_init", "lamb_muon_step",
-           "lamb_ns_plan_destroy")
+           "lamb_ns_plan_destroy", "lamb_xent_workspace", "lamb_xent_forward",
+           "lamb_xent_backward")
 
 
 class lamb_ns_params(ctypes.Structure):
@@ -56,6 +57,23 @@ class lamb_muon_hparams(ctypes.Structure):
                 ("skip_nonfinite", ctypes.c_int32), ("reserved", ctypes.c_int32)]
 
 
+class lamb_xent(ctypes.Structure):
+    _fields_ = [("hidden", ctypes.c_void_p), ("table", ctypes.c_void_p),
+                ("targets", ctypes.c_void_p), ("hidden_stride", ctypes.c_int64),
+                ("table_stride", ctypes.c_int64), ("tokens", ctypes.c_int64),
+                ("vocab", ctypes.c_int64), ("dim", ctypes.c_int64),
+                ("ignore_index", ctypes.c_int64), ("target_dtype", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
+
+
+class lamb_xent_grads(ctypes.Structure):
+    _fields_ = [("grad_loss", ctypes.c_void_p), ("grad_hidden", ctypes.c_void_p),
+                ("grad_table", ctypes.c_void_p), ("grad_hidden_stride", ctypes.c_int64),
+                ("grad_table_stride", ctypes.c_int64), ("grad_table_dtype", ctypes.c_int32),
+                ("add_table", ctypes.c_int32), ("mean", ctypes.c_int32),
+                ("grad_scale", ctypes.c_float)]
+
+
 _lib_ops: Optional[ctypes.CDLL] = None
 
 
@@ -66,6 +84,7 @@ def load() -> ctypes.CDLL:
         return _lib_ops
     lib = _lib.load()
     i32, vp, P = ctypes.c_int32, ctypes.c_void_p, ctypes.POINTER
+    size = ctypes.c_size_t
     lib.lamb_ns_params_init.argtypes = [P(lamb_ns_params)]
     lib.lamb_ortho_plan_create.argtypes = [P(lamb_matrix), i32, i32, i32, i32, P(vp)]
     lib.lamb_orthogonalize.argtypes = [vp, P(lamb_ns_params), vp]
@@ -73,6 +92,9 @@ def load() -> ctypes.CDLL:
     lib.lamb_muon_hparams_init.argtypes = [P(lamb_muon_hparams)]
     lib.lamb_muon_step.argtypes = [vp, P(lamb_muon_hparams), vp, vp]
     lib.lamb_ns_plan_destroy.argtypes = [vp]
+    lib.lamb_xent_workspace.argtypes = [P(lamb_xent), P(size), P(size)]
+    lib.lamb_xent_forward.argtypes = [P(lamb_xent), vp, vp, vp, vp, size, vp]
+    lib.lamb_xent_backward.argtypes = [P(lamb_xent), vp, P(lamb_xent_grads), vp, size, vp]
     for name in EXPORTS:
         getattr(lib, name).restype = ctypes.c_int
     _lib_ops = lib
@@ -152,3 +174,25 @@ def lamb_muon_step(plan: NsPlan, hp: lamb_muon_hparams, stream: int = 0,
                    nonfinite_out: int = 0) -> None:
     _check(load().lamb_muon_step(_vp(plan.handle), ctypes.byref(hp), _vp(stream),
                                  _vp(nonfinite_out)), "lamb_muon_step")
+
+
+def lamb_xent_workspace(xent: lamb_xent) -> Tuple[int, int]:
+    """Bytes that a forward and a backward call need."""
+    a, b = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(load().lamb_xent_workspace(ctypes.byref(xent), ctypes.byref(a), ctypes.byref(b)),
+           "lamb_xent_workspace")
+    return a.value, b.value
+
+
+def lamb_xent_forward(xent: lamb_xent, loss: int, lse: int, mean: int, workspace: int,
+                      workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().lamb_xent_forward(ctypes.byref(xent), _vp(loss), _vp(lse), _vp(mean),
+                                    _vp(workspace), workspace_bytes, _vp(stream)),
+           "lamb_xent_forward")
+
+
+def lamb_xent_backward(xent: lamb_xent, lse: int, grads: lamb_xent_grads, workspace: int,
+                       workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().lamb_xent_backward(ctypes.byref(xent), _vp(lse), ctypes.byref(grads),
+                                     _vp(workspace), workspace_bytes, _vp(stream)),
+           "lamb_xent_backward")

@@ -5,6 +5,7 @@
 #include <hip/hip_runtime_api.h>
 #include <stdint.h>
 
+#include <algorithm>
 #include <exception>
 #include <new>
 #include <vector>
@@ -46,5 +47,39 @@ inline bool aligned_to(const void *p, uintptr_t bytes) {
 }
 
 inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
+
+// Memory that a call reads or writes, for the overlap check.
+struct Span {
+    uintptr_t lo, hi;
+    bool written;
+    int32_t index;
+    const char *what;
+};
+
+inline Span span_of(const void *p, uint64_t bytes, bool written, int32_t index, const char *what) {
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
+    return Span{lo, lo + uintptr_t(bytes), written, index, what};
+}
+
+// Written memory overlaps nothing; what is only read may overlap. Sorts the spans.
+inline lamb_status check_spans(Span *spans, size_t n) {
+    std::sort(spans, spans + n, [](const Span &p, const Span &q) {
+        return p.lo != q.lo ? p.lo < q.lo : p.hi < q.hi;
+    });
+    const Span *read = nullptr, *wrote = nullptr;  // the furthest-reaching so far
+    for (size_t i = 0; i < n; ++i) {
+        const Span &s = spans[i];
+        const Span *other = wrote && s.lo < wrote->hi               ? wrote
+                            : s.written && read && s.lo < read->hi ? read
+                                                                    : nullptr;
+        if (other && s.hi > s.lo)
+            return fail(LAMB_EOVERLAP, "%s (%d) overlaps %s (%d)", s.what, s.index, other->what,
+                        other->index);
+        const Span *&far = s.written ? wrote : read;
+        if (!far || s.hi > far->hi)
+            far = &s;
+    }
+    return LAMB_OK;
+}
 
 }  // namespace lamb_mi355x

@@ -26,6 +26,7 @@ struct lamb_ns_plan {
 namespace {
 
 constexpr int64_t kMaxSide = int64_t(1) << 20;
+constexpr int64_t kMaxStride = int64_t(1) << 40;
 
 // The bounds of lamb_ns_params: where singular values that start in [0, 1] go.
 lamb_status check_params(const lamb_ns_params &p) {
@@ -70,26 +71,6 @@ lamb_status check_params(const lamb_ns_params &p) {
                         "singular value %.3g (at most %g) in step %d",
                         a, b, c, largest_p, kNsLargest, largest_x, kNsLargestX, k + 1);
         top = largest_x;
-    }
-    return LAMB_OK;
-}
-
-lamb_status check_ranges(std::vector<BufferRange> &ranges) {
-    std::sort(ranges.begin(), ranges.end(), [](const BufferRange &p, const BufferRange &q) {
-        return p.lo != q.lo ? p.lo < q.lo : p.hi < q.hi;
-    });
-    // an input may share memory with other inputs, a written buffer with nothing
-    uintptr_t in_hi = 0, out_hi = 0;
-    int32_t in_of = 0, out_of = 0;
-    for (const BufferRange &r : ranges) {
-        const bool written = r.what[0] != 'i' && r.what[0] != 'g';
-        if (r.lo < out_hi || (written && r.lo < in_hi))
-            return fail(LAMB_EOVERLAP, "matrix %d %s overlaps a buffer of matrix %d", r.tensor,
-                        r.what, r.lo < out_hi ? out_of : in_of);
-        if (written && r.hi > out_hi)
-            out_hi = r.hi, out_of = r.tensor;
-        if (!written && r.hi > in_hi)
-            in_hi = r.hi, in_of = r.tensor;
     }
     return LAMB_OK;
 }
@@ -338,7 +319,7 @@ lamb_status lamb_ortho_plan_create(const lamb_matrix *matrices, int32_t n, int32
         const int64_t in_size = in_dtype == LAMB_DTYPE_BF16 ? 2 : 4;
         const int64_t out_size = out_dtype == LAMB_DTYPE_BF16 ? 2 : 4;
         std::vector<NsMatrix> list;
-        std::vector<BufferRange> ranges;
+        std::vector<Span> spans;
         for (int32_t i = 0; i < n; ++i) {
             const lamb_matrix &t = matrices[i];
             if (!t.in || !t.out)
@@ -346,22 +327,19 @@ lamb_status lamb_ortho_plan_create(const lamb_matrix *matrices, int32_t n, int32
             lamb_status s = check_side(i, t.rows, t.cols);
             if (s != LAMB_OK)
                 return s;
-            if (t.in_stride < t.cols || t.out_stride < t.cols || t.in_stride > kMaxNumel ||
-                t.out_stride > kMaxNumel)
-                return fail(LAMB_EINVAL, "matrix %d: a row stride is below its %lld columns", i,
+            if (t.in_stride < t.cols || t.out_stride < t.cols || t.in_stride > kMaxStride ||
+                t.out_stride > kMaxStride)
+                return fail(LAMB_EINVAL, "matrix %d: a row stride is below its %lld columns, or above 2^40", i,
                             static_cast<long long>(t.cols));
             if (!aligned_to(t.in, uintptr_t(in_size)) || !aligned_to(t.out, uintptr_t(out_size)))
                 return fail(LAMB_EALIGN, "matrix %d: a pointer is not aligned to its elements", i);
-            const uintptr_t in = reinterpret_cast<uintptr_t>(t.in);
-            const uintptr_t to = reinterpret_cast<uintptr_t>(t.out);
-            const uintptr_t in_len = uintptr_t((t.rows - 1) * t.in_stride + t.cols) *
-                                     uintptr_t(in_size);
-            const uintptr_t out_len = uintptr_t((t.rows - 1) * t.out_stride + t.cols) *
-                                      uintptr_t(out_size);
-            const bool in_place = in == to && in_dtype == out_dtype && t.in_stride == t.out_stride;
+            const int64_t in_len = ((t.rows - 1) * t.in_stride + t.cols) * in_size;
+            const int64_t out_len = ((t.rows - 1) * t.out_stride + t.cols) * out_size;
+            const bool in_place =
+                t.in == t.out && in_dtype == out_dtype && t.in_stride == t.out_stride;
             if (!in_place)
-                ranges.push_back(BufferRange{in, in + in_len, i, "in"});
-            ranges.push_back(BufferRange{to, to + out_len, i, "out"});
+                spans.push_back(span_of(t.in, in_len, false, i, "in"));
+            spans.push_back(span_of(t.out, out_len, true, i, "out"));
             NsMatrix m{};
             m.in = t.in;
             m.out = t.out;
@@ -373,7 +351,7 @@ lamb_status lamb_ortho_plan_create(const lamb_matrix *matrices, int32_t n, int32
                        t.in_stride * in_size % 16 == 0 && t.out_stride * out_size % 16 == 0;
             list.push_back(m);
         }
-        lamb_status s = check_ranges(ranges);
+        lamb_status s = check_spans(spans.data(), spans.size());
         if (s != LAMB_OK)
             return s;
         lamb_ns_plan *plan = new lamb_ns_plan;
@@ -400,7 +378,7 @@ lamb_status lamb_muon_plan_create(const lamb_muon_tensor *tensors, int32_t n, in
         return st;
     return guarded([&]() -> lamb_status {
         std::vector<NsMatrix> list;
-        std::vector<BufferRange> ranges;
+        std::vector<Span> spans;
         for (int32_t i = 0; i < n; ++i) {
             const lamb_muon_tensor &t = tensors[i];
             if (!t.x || !t.g || !t.m)
@@ -414,14 +392,10 @@ lamb_status lamb_muon_plan_create(const lamb_muon_tensor *tensors, int32_t n, in
                 return fail(LAMB_EINVAL, "matrix %d: reserved field must be 0", i);
             if (!aligned_to(t.x, 16) || !aligned_to(t.g, 16) || !aligned_to(t.m, 16))
                 return fail(LAMB_EALIGN, "matrix %d: every buffer must be 16-byte aligned", i);
-            const uintptr_t numel = uintptr_t(t.rows) * uintptr_t(t.cols);
-            auto add = [&](const void *p, uintptr_t bytes, const char *what) {
-                const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-                ranges.push_back(BufferRange{lo, lo + bytes, i, what});
-            };
-            add(t.x, numel * 4, "x");
-            add(t.g, numel * (g_dtype == LAMB_DTYPE_BF16 ? 2 : 4), "g");
-            add(t.m, numel * 4, "m");
+            const uint64_t numel = uint64_t(t.rows) * uint64_t(t.cols);
+            spans.push_back(span_of(t.x, numel * 4, true, i, "x"));
+            spans.push_back(span_of(t.g, numel * (g_dtype == LAMB_DTYPE_BF16 ? 2 : 4), false, i, "g"));
+            spans.push_back(span_of(t.m, numel * 4, true, i, "m"));
             NsMatrix m{};
             m.in = t.g;
             m.out = t.x;
@@ -433,7 +407,7 @@ lamb_status lamb_muon_plan_create(const lamb_muon_tensor *tensors, int32_t n, in
             m.wd = t.wd;
             list.push_back(m);
         }
-        lamb_status s = check_ranges(ranges);
+        lamb_status s = check_spans(spans.data(), spans.size());
         if (s != LAMB_OK)
             return s;
         lamb_ns_plan *plan = new lamb_ns_plan;

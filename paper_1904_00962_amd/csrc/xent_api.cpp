@@ -1,0 +1,310 @@
+// Host side of the cross entropy of include/lamb_ops.h: validation, the workspace's
+// layout and the launches of a call.
+#include <math.h>
+
+#include "ops_host.h"
+#include "xent_internal.h"
+
+using namespace lamb_mi355x;
+
+namespace {
+
+constexpr int64_t kMaxTokens = int64_t(1) << 24, kMaxVocab = int64_t(1) << 24,
+                  kMaxDim = int64_t(1) << 16, kMaxStride = int64_t(1) << 40,
+                  kMaxReadStride = int64_t(1) << 21;  // a tile's rows within 32-bit offsets
+// A piece of the vocabulary's softmax: written once and read twice, so kept within
+// the 256 MiB last-level cache.
+constexpr int64_t kPieceBytes = int64_t(128) << 20;
+constexpr int64_t kPieceAlign = 256;
+constexpr int64_t kFill = 512;  // workgroups that fill the device (two on each CU)
+
+lamb_status check(const lamb_xent *x) {
+    if (!x)
+        return fail(LAMB_ENULL, "xent must not be NULL");
+    if (x->reserved != 0)
+        return fail(LAMB_EINVAL, "xent.reserved must be 0");
+    if (x->tokens < 0 || x->tokens > kMaxTokens || x->vocab < 1 || x->vocab > kMaxVocab ||
+        x->dim < 1 || x->dim > kMaxDim)
+        return fail(LAMB_EINVAL,
+                    "tokens %lld, vocab %lld, dim %lld: need 0 to 2^24, 1 to 2^24, 1 to 2^16",
+                    (long long)x->tokens, (long long)x->vocab, (long long)x->dim);
+    if (x->target_dtype != LAMB_DTYPE_I32 && x->target_dtype != LAMB_DTYPE_I64)
+        return fail(LAMB_EINVAL, "targets are int32 or int64");
+    if (!x->table || (x->tokens && (!x->hidden || !x->targets)))
+        return fail(LAMB_ENULL, "hidden, table and targets must not be NULL");
+    if (x->hidden_stride < x->dim || x->table_stride < x->dim || x->hidden_stride > kMaxStride ||
+        x->table_stride > kMaxStride)
+        return fail(LAMB_EINVAL, "a row stride is below dim, or above 2^40");
+    if (!aligned_to(x->hidden, 2) || !aligned_to(x->table, 2) ||
+        !aligned_to(x->targets, x->target_dtype == LAMB_DTYPE_I64 ? 8 : 4))
+        return fail(LAMB_EALIGN, "a pointer is not aligned to its elements");
+    return LAMB_OK;
+}
+
+bool in_place(const void *p, int64_t stride, int64_t dim) {
+    return dim % 8 == 0 && stride % 8 == 0 && stride <= kMaxReadStride && aligned_to(p, 16);
+}
+
+int64_t count_tiles(int64_t rows, int64_t cols, int shape) {
+    return round_up(rows, xent_rows(shape)) / xent_rows(shape) *
+           (round_up(cols, xent_cols(shape)) / xent_cols(shape));
+}
+
+// The largest tiles that fill the device and whose last row of tiles wastes at most
+// half of the work.
+int pick_shape(int64_t rows, int64_t cols) {
+    for (int shape = kXentLarge; shape > kXentTiny; --shape)
+        if (count_tiles(rows, cols, shape) >= kFill &&
+            2 * round_up(rows, xent_rows(shape)) <= 3 * round_up(rows, 64))
+            return shape;
+    return kXentTiny;
+}
+
+struct Layout {
+    int64_t ld = 0;
+    bool copy_table = false;
+    int logits_shape = 0, probs_shape = 0, hidden_shape = 0, table_shape = 0;
+    int32_t parts = 0, splits = 1;
+    int64_t piece = 0;
+    // offsets, and the end
+    size_t kept = 0, source = 0, target = 0, packed = 0, table = 0, parts_at = 0, at_target = 0,
+           probs = 0, partial = 0, forward = 0, backward = 0;
+};
+
+Layout layout_of(const lamb_xent &x) {
+    Layout l;
+    l.ld = round_up(x.dim, 8);
+    l.copy_table = !in_place(x.table, x.table_stride, x.dim);
+    size_t at = 0;
+    auto take = [&](int64_t bytes) {
+        const size_t start = at;
+        at += size_t(round_up(bytes, 256));
+        return start;
+    };
+    l.kept = take(4);
+    l.source = take(4 * x.tokens);
+    l.target = take(4 * x.tokens);
+    l.packed = take(2 * x.tokens * l.ld);
+    l.table = take(l.copy_table ? 2 * x.vocab * l.ld : 0);
+    const size_t common = at;
+    l.logits_shape = pick_shape(x.tokens, x.vocab);
+    l.parts = int32_t(round_up(x.vocab, xent_cols(l.logits_shape)) / xent_cols(l.logits_shape)) *
+              kXentColumnWaves;
+    l.parts_at = take(int64_t(l.parts) * x.tokens * 8);
+    l.at_target = take(4 * x.tokens);
+    l.forward = at;
+    at = common;
+    // equal pieces, whole multiples of a tile
+    const int64_t rows = x.tokens ? x.tokens : 1;
+    const int64_t most = std::max<int64_t>(kPieceAlign, kPieceBytes / 2 / rows);
+    const int64_t pieces = (x.vocab + most - 1) / most;
+    l.piece = std::min(round_up((x.vocab + pieces - 1) / pieces, kPieceAlign), round_up(x.vocab, 8));
+    l.probs_shape = pick_shape(x.tokens, l.piece);
+    l.table_shape = pick_shape(l.piece, x.dim);
+    l.hidden_shape = pick_shape(x.tokens, x.dim);
+    // few rows: the piece's columns are split over workgroups, 512 each at least
+    const int64_t tiles = std::max<int64_t>(1, count_tiles(x.tokens, x.dim, l.hidden_shape));
+    l.splits = int32_t(std::max<int64_t>(
+        1, std::min((kFill + tiles - 1) / tiles, l.piece / 512)));
+    l.probs = take(2 * x.tokens * l.piece);
+    l.partial = take(int64_t(l.splits) * x.tokens * l.ld * 4);
+    l.backward = at;
+    return l;
+}
+
+// The packed rows and the table as the kernels read them.
+lamb_status begin(const lamb_xent &x, const Layout &l, char *work, float *loss, float *lse,
+                  void *grad_hidden, int64_t grad_stride, XentArgs *args, hipStream_t stream) {
+    XentPack pack{};
+    pack.hidden = static_cast<const uint16_t *>(x.hidden);
+    pack.stride = x.hidden_stride;
+    pack.targets = x.targets;
+    pack.wide = x.target_dtype == LAMB_DTYPE_I64;
+    pack.vector = aligned_to(x.hidden, 16) && x.hidden_stride % 8 == 0;
+    pack.ignore = x.ignore_index;
+    pack.dim = int32_t(x.dim);
+    pack.ld = int32_t(l.ld);
+    pack.vocab = int32_t(x.vocab);
+    pack.tokens = int32_t(x.tokens);
+    pack.packed = reinterpret_cast<uint16_t *>(work + l.packed);
+    pack.kept = reinterpret_cast<int32_t *>(work + l.kept);
+    pack.source = reinterpret_cast<int32_t *>(work + l.source);
+    pack.target = reinterpret_cast<int32_t *>(work + l.target);
+    pack.loss = loss;
+    pack.lse = lse;
+    pack.grad_hidden = static_cast<uint16_t *>(grad_hidden);
+    pack.grad_stride = grad_stride;
+    hipError_t err = launch_xent_pack(pack, stream);
+    *args = XentArgs{};
+    args->hidden = pack.packed;
+    args->ld = l.ld;
+    args->table = static_cast<const uint16_t *>(x.table);
+    args->table_ld = x.table_stride;
+    if (l.copy_table) {
+        uint16_t *copy = reinterpret_cast<uint16_t *>(work + l.table);
+        if (err == hipSuccess)
+            err = launch_xent_copy(args->table, x.table_stride, copy, int32_t(x.dim),
+                                   int32_t(l.ld), x.vocab, stream);
+        args->table = copy;
+        args->table_ld = l.ld;
+    }
+    args->dim = int32_t(x.dim);
+    args->vocab = int32_t(x.vocab);
+    args->tokens = int32_t(x.tokens);
+    args->kept = pack.kept;
+    args->source = pack.source;
+    args->target = pack.target;
+    return err == hipSuccess ? LAMB_OK : fail_hip(err, "kernel launch");
+}
+
+lamb_status check_workspace(const void *workspace, size_t bytes, size_t need) {
+    if (!workspace)
+        return fail(LAMB_ENULL, "workspace must not be NULL");
+    if (!aligned_to(workspace, 256))
+        return fail(LAMB_EALIGN, "the workspace must be 256-byte aligned");
+    if (bytes < need)
+        return fail(LAMB_EINVAL, "the workspace has %zu bytes, the call needs %zu", bytes, need);
+    return LAMB_OK;
+}
+
+uint64_t rows_bytes(int64_t rows, int64_t stride, int64_t cols, int64_t size) {
+    return rows ? uint64_t((rows - 1) * stride + cols) * uint64_t(size) : 0;
+}
+
+}  // namespace
+
+extern "C" {
+
+lamb_status lamb_xent_workspace(const lamb_xent *xent, size_t *forward_bytes,
+                                size_t *backward_bytes) {
+    const lamb_status st = check(xent);
+    if (st != LAMB_OK)
+        return st;
+    const Layout l = layout_of(*xent);
+    if (forward_bytes)
+        *forward_bytes = l.forward;
+    if (backward_bytes)
+        *backward_bytes = l.backward;
+    return LAMB_OK;
+}
+
+lamb_status lamb_xent_forward(const lamb_xent *xent, float *loss, float *lse, float *mean,
+                              void *workspace, size_t workspace_bytes, void *stream_in) {
+    lamb_status st = check(xent);
+    if (st != LAMB_OK)
+        return st;
+    const lamb_xent &x = *xent;
+    if (x.tokens && (!loss || !lse))
+        return fail(LAMB_ENULL, "loss and lse must not be NULL");
+    if (!aligned_to(loss, 4) || !aligned_to(lse, 4) || !aligned_to(mean, 4))
+        return fail(LAMB_EALIGN, "a pointer is not aligned to its elements");
+    const Layout l = layout_of(x);
+    st = check_workspace(workspace, workspace_bytes, l.forward);
+    if (st != LAMB_OK)
+        return st;
+    const int64_t id = x.target_dtype == LAMB_DTYPE_I64 ? 8 : 4;
+    Span spans[] = {
+        span_of(x.hidden, rows_bytes(x.tokens, x.hidden_stride, x.dim, 2), false, 0, "hidden"),
+        span_of(x.table, rows_bytes(x.vocab, x.table_stride, x.dim, 2), false, 0, "table"),
+        span_of(x.targets, uint64_t(x.tokens * id), false, 0, "targets"),
+        span_of(loss, uint64_t(x.tokens) * 4, true, 0, "loss"),
+        span_of(lse, uint64_t(x.tokens) * 4, true, 0, "lse"),
+        span_of(mean, mean ? 4 : 0, true, 0, "mean"),
+        span_of(workspace, l.forward, true, 0, "workspace")};
+    st = check_spans(spans, sizeof spans / sizeof spans[0]);
+    if (st != LAMB_OK)
+        return st;
+    hipStream_t stream = static_cast<hipStream_t>(stream_in);
+    char *work = static_cast<char *>(workspace);
+    XentArgs args;
+    st = begin(x, l, work, loss, lse, nullptr, 0, &args, stream);
+    if (st != LAMB_OK)
+        return st;
+    hipError_t err = hipSuccess;
+    if (x.tokens) {
+        float2 *parts = reinterpret_cast<float2 *>(work + l.parts_at);
+        float *at_target = reinterpret_cast<float *>(work + l.at_target);
+        err = launch_xent_logits(args, l.logits_shape, parts, at_target, stream);
+        if (err == hipSuccess)
+            err = launch_xent_reduce(args, l.parts, parts, at_target, loss, lse, stream);
+    }
+    if (err == hipSuccess && mean)
+        err = launch_xent_mean(loss, args.tokens, args.kept, mean, stream);
+    return err == hipSuccess ? LAMB_OK : fail_hip(err, "kernel launch");
+}
+
+lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
+                               const lamb_xent_grads *grads, void *workspace,
+                               size_t workspace_bytes, void *stream_in) {
+    lamb_status st = check(xent);
+    if (st != LAMB_OK)
+        return st;
+    const lamb_xent &x = *xent;
+    if (!grads || (x.tokens && !lse))
+        return fail(LAMB_ENULL, "lse and grads must not be NULL");
+    const lamb_xent_grads &g = *grads;
+    if ((g.add_table | g.mean) & ~1)
+        return fail(LAMB_EINVAL, "grads.add_table and grads.mean must be 0 or 1");
+    if (!std::isfinite(g.grad_scale))
+        return fail(LAMB_EINVAL, "grads.grad_scale = %g must be finite", double(g.grad_scale));
+    const bool bf16 = g.grad_table_dtype == LAMB_DTYPE_BF16;
+    if (g.grad_table && !bf16 && g.grad_table_dtype != LAMB_DTYPE_F32)
+        return fail(LAMB_EINVAL, "grad_table is float32 or bfloat16");
+    if ((g.grad_hidden && (g.grad_hidden_stride < x.dim || g.grad_hidden_stride > kMaxStride)) ||
+        (g.grad_table && (g.grad_table_stride < x.dim || g.grad_table_stride > kMaxStride)))
+        return fail(LAMB_EINVAL, "a row stride is below dim, or above 2^40");
+    if (!aligned_to(g.grad_loss, 4) || !aligned_to(lse, 4) || !aligned_to(g.grad_hidden, 2) ||
+        !aligned_to(g.grad_table, bf16 ? 2 : 4))
+        return fail(LAMB_EALIGN, "a pointer is not aligned to its elements");
+    const Layout l = layout_of(x);
+    st = check_workspace(workspace, workspace_bytes, l.backward);
+    if (st != LAMB_OK)
+        return st;
+    const int64_t id = x.target_dtype == LAMB_DTYPE_I64 ? 8 : 4;
+    Span spans[] = {
+        span_of(x.hidden, rows_bytes(x.tokens, x.hidden_stride, x.dim, 2), false, 0, "hidden"),
+        span_of(x.table, rows_bytes(x.vocab, x.table_stride, x.dim, 2), false, 0, "table"),
+        span_of(x.targets, uint64_t(x.tokens * id), false, 0, "targets"),
+        span_of(lse, uint64_t(x.tokens) * 4, false, 0, "lse"),
+        span_of(g.grad_loss, g.grad_loss ? 4 : 0, false, 0, "grad_loss"),
+        span_of(g.grad_hidden,
+                g.grad_hidden ? rows_bytes(x.tokens, g.grad_hidden_stride, x.dim, 2) : 0, true, 0,
+                "grad_hidden"),
+        span_of(g.grad_table,
+                g.grad_table ? rows_bytes(x.vocab, g.grad_table_stride, x.dim, bf16 ? 2 : 4) : 0,
+                true, 0, "grad_table"),
+        span_of(workspace, l.backward, true, 0, "workspace")};
+    st = check_spans(spans, sizeof spans / sizeof spans[0]);
+    if (st != LAMB_OK)
+        return st;
+    hipStream_t stream = static_cast<hipStream_t>(stream_in);
+    char *work = static_cast<char *>(workspace);
+    XentArgs args;
+    st = begin(x, l, work, nullptr, nullptr, g.grad_hidden, g.grad_hidden_stride, &args, stream);
+    if (st != LAMB_OK)
+        return st;
+    float *partial = reinterpret_cast<float *>(work + l.partial);
+    hipError_t err = hipSuccess;
+    for (int64_t first = 0; first < x.vocab && err == hipSuccess; first += l.piece) {
+        XentPiece piece{};
+        piece.first = int32_t(first);
+        piece.count = int32_t(std::min(l.piece, x.vocab - first));
+        piece.ld = int32_t(round_up(piece.count, 8));
+        piece.probs = reinterpret_cast<uint16_t *>(work + l.probs);
+        if (x.tokens)
+            err = launch_xent_probs(args, l.probs_shape, piece, lse, stream);
+        if (err == hipSuccess && x.tokens && g.grad_hidden)
+            err = launch_xent_hidden(args, l.hidden_shape, piece, l.splits, first > 0, partial,
+                                     stream);
+        if (err == hipSuccess && g.grad_table)
+            err = launch_xent_table(args, l.table_shape, piece, g.grad_loss, g.grad_scale, g.mean,
+                                    bf16, g.add_table, g.grad_table, g.grad_table_stride, stream);
+    }
+    if (err == hipSuccess && x.tokens && g.grad_hidden)
+        err = launch_xent_hidden_out(args, l.splits, partial, g.grad_loss, g.grad_scale, g.mean,
+                                     static_cast<uint16_t *>(g.grad_hidden), g.grad_hidden_stride,
+                                     stream);
+    return err == hipSuccess ? LAMB_OK : fail_hip(err, "kernel launch");
+}
+
+}  // extern "C"

@@ -1,0 +1,86 @@
+// Layout shared by the kernels of the cross entropy (xent_kernels.hip) and their
+// host side (xent_api.cpp). Not installed; the public interface is
+// include/lamb_ops.h.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+#include <stdint.h>
+
+namespace lamb_mi355x {
+
+// Tile shapes, rows by columns.
+enum XentShape : int32_t { kXentTiny = 0, kXentSmall = 1, kXentLarge = 2 };
+constexpr int32_t xent_rows(int32_t shape) { return 64 << shape; }
+constexpr int32_t xent_cols(int32_t shape) { return shape == kXentTiny ? 64 : 128; }
+constexpr int32_t kXentColumnWaves = 2;  // waves across a tile's columns, in every shape
+
+constexpr int kPackTokens = 64;   // tokens per workgroup of the packing pass
+constexpr int kReduceTokens = 16;  // tokens per workgroup of the logsumexp pass
+
+// What every pass of a call reads. `hidden` is the packed copy of the tokens that
+// count, rows `ld` apart with zeros from dim to ld; `table` the caller's, or a copy
+// laid out likewise.
+struct XentArgs {
+    const uint16_t *hidden;
+    const uint16_t *table;
+    int64_t ld, table_ld;
+    int32_t dim, vocab, tokens;
+    const int32_t *kept;    // tokens that count
+    const int32_t *source;  // packed row -> token
+    const int32_t *target;  // packed row -> target, -1 where it is outside the vocabulary
+};
+
+struct XentPack {
+    const uint16_t *hidden;
+    int64_t stride;
+    const void *targets;
+    int32_t wide;  // targets are 64-bit
+    int32_t vector;
+    int64_t ignore;
+    int32_t dim, ld, vocab, tokens;
+    uint16_t *packed;
+    int32_t *kept, *source, *target;
+    float *loss, *lse;           // forward: of the tokens that do not count, 0
+    uint16_t *grad_hidden;       // backward: likewise, rows grad_stride apart
+    int64_t grad_stride;
+};
+
+// Copies the rows of the tokens that count together, in their order.
+hipError_t launch_xent_pack(const XentPack &args, hipStream_t stream);
+// dst[r][0 .. ld) = src[r][0 .. dim) and zeros, `rows` rows.
+hipError_t launch_xent_copy(const uint16_t *src, int64_t stride, uint16_t *dst, int32_t dim,
+                            int32_t ld, int64_t rows, hipStream_t stream);
+// Logits of all of the vocabulary, tile by tile: each tile column's wave halves'
+// maximum and sum of exponentials, parts[part][token], and the targets' logits.
+hipError_t launch_xent_logits(const XentArgs &args, int shape, float2 *parts, float *at_target,
+                              hipStream_t stream);
+hipError_t launch_xent_reduce(const XentArgs &args, int32_t n_parts, const float2 *parts,
+                              const float *at_target, float *loss, float *lse,
+                              hipStream_t stream);
+// mean = sum of the losses over the count of tokens (0 without any).
+hipError_t launch_xent_mean(const float *loss, int32_t tokens, const int32_t *kept, float *mean,
+                            hipStream_t stream);
+
+// One piece of the vocabulary: rows [first, first + count) of the table; probs is
+// [tokens][ld] with zeros from count to ld.
+struct XentPiece {
+    int32_t first, count, ld;
+    uint16_t *probs;
+};
+
+// probs = softmax - one at the target, in bf16.
+hipError_t launch_xent_probs(const XentArgs &args, int shape, const XentPiece &piece,
+                             const float *lse, hipStream_t stream);
+// partial[split] (tokens x dim, fp32) = or += probs' share of the piece times the table.
+hipError_t launch_xent_hidden(const XentArgs &args, int shape, const XentPiece &piece,
+                              int32_t splits, bool add, float *partial, hipStream_t stream);
+// The sum over the splits, scaled, to the tokens' rows of grad_hidden.
+hipError_t launch_xent_hidden_out(const XentArgs &args, int32_t splits, const float *partial,
+                                  const float *grad_loss, float grad_scale, bool mean,
+                                  uint16_t *grad_hidden, int64_t stride, hipStream_t stream);
+// grad_table's rows of the piece = (or +=) scale probs^T hidden.
+hipError_t launch_xent_table(const XentArgs &args, int shape, const XentPiece &piece,
+                             const float *grad_loss, float grad_scale, bool mean, bool bf16_out,
+                             bool add, void *grad_table, int64_t stride, hipStream_t stream);
+
+}  // namespace lamb_mi355x

@@ -1,6 +1,8 @@
 """Operators around the optimizer step, over torch tensors on an MI355X.
 
-  Orthogonalizer   lists of matrices made orthogonal by Newton-Schulz products
+  Orthogonalizer            lists of matrices made orthogonal by Newton-Schulz products
+  linear_cross_entropy      softmax cross entropy against a vocabulary table, and
+  linear_cross_entropy_grad its gradients, without keeping the logits
 
 PyTorch supplies device memory and the current stream only; the work is the HIP
 library's (``_ops``). Argument errors raise ``ValueError`` or ``TypeError`` here,
@@ -101,3 +103,107 @@ class Orthogonalizer:
 
     def close(self) -> None:
         self.plan.close()
+
+
+def _rows(name, t, dtype, device=None):
+    """A 2-D tensor whose rows are contiguous: its row stride."""
+    _on_gpu(name, t, device)
+    if t.dtype != dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    if t.dim() != 2:
+        raise ValueError("%s must have two dimensions" % name)
+    if t.shape[1] > 1 and t.stride(1) != 1:
+        raise ValueError("%s: the elements of a row must be adjacent" % name)
+    # the stride of a single row means nothing; an expanded row's is 0
+    if t.shape[0] <= 1:
+        return t.shape[1]
+    return t.stride(0)
+
+
+def _ids(name, t, device):
+    torch = _torch()
+    _on_gpu(name, t, device)
+    if t.dtype not in (torch.int32, torch.int64):
+        raise TypeError("%s must be int32 or int64, got %s" % (name, t.dtype))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return _ops.LAMB_DTYPE_I64 if t.dtype == torch.int64 else _ops.LAMB_DTYPE_I32
+
+
+def _xent(hidden, table, targets, ignore_index):
+    torch = _torch()
+    stride = _rows("hidden", hidden, torch.bfloat16)
+    table_stride = _rows("table", table, torch.bfloat16, hidden.device)
+    code = _ids("targets", targets, hidden.device)
+    if hidden.shape[1] != table.shape[1]:
+        raise ValueError("hidden has %d columns, the table %d" % (hidden.shape[1], table.shape[1]))
+    if targets.dim() != 1 or targets.shape[0] != hidden.shape[0]:
+        raise ValueError("need one target per row of hidden")
+    return _ops.lamb_xent(hidden.data_ptr() or None, table.data_ptr() or None,
+                          targets.data_ptr() or None, stride, table_stride, hidden.shape[0],
+                          table.shape[0], hidden.shape[1], int(ignore_index), code, 0)
+
+
+def _workspace(bytes_, device):
+    return _torch().empty(bytes_, dtype=_torch().uint8, device=device)
+
+
+def linear_cross_entropy(hidden, table, targets, *, ignore_index: int = -100):
+    """(mean, loss, lse) of softmax cross entropy with logits hidden table^T, fp32.
+
+    ``hidden`` [tokens, dim] and ``table`` [vocab, dim] are bfloat16 with contiguous
+    rows, ``targets`` int32 or int64. Tokens whose target is ``ignore_index`` do not
+    count: loss 0, and the mean is over the others (0 without any). A target outside
+    the vocabulary gives NaN. ``lse`` is what :func:`linear_cross_entropy_grad` needs.
+    """
+    torch = _torch()
+    x = _xent(hidden, table, targets, ignore_index)
+    need, _ = _ops.lamb_xent_workspace(x)
+    out = torch.empty(2, hidden.shape[0], dtype=torch.float32, device=hidden.device)
+    mean = torch.empty((), dtype=torch.float32, device=hidden.device)
+    work = _workspace(need, hidden.device)
+    with torch.cuda.device(hidden.device):
+        _ops.lamb_xent_forward(x, out[0].data_ptr(), out[1].data_ptr(), mean.data_ptr(),
+                               work.data_ptr(), need, _stream(hidden.device))
+    return mean, out[0], out[1]
+
+
+def linear_cross_entropy_grad(hidden, table, targets, lse, grad_hidden=None, grad_table=None, *,
+                              ignore_index: int = -100, reduction: str = "mean",
+                              grad_loss=None, grad_scale: float = 1.0,
+                              accumulate: bool = False) -> None:
+    """Gradients of ``grad_scale`` x ``grad_loss`` x the mean or the sum (``reduction``)
+    of the losses: into ``grad_hidden`` (bfloat16, like hidden) and ``grad_table``
+    (bfloat16 or float32, like the table), either of them optional; ``accumulate`` adds
+    to what ``grad_table`` holds. ``grad_loss``: a float32 tensor of one element on the
+    device (default 1). ``lse`` is the forward's."""
+    torch = _torch()
+    x = _xent(hidden, table, targets, ignore_index)
+    device = hidden.device
+    if lse.dtype != torch.float32 or lse.shape != targets.shape or not lse.is_contiguous():
+        raise ValueError("lse must be the forward's")
+    _on_gpu("lse", lse, device)
+    if reduction not in ("mean", "sum"):
+        raise ValueError("reduction must be 'mean' or 'sum'")
+    g = _ops.lamb_xent_grads(mean=int(reduction == "mean"), grad_scale=float(grad_scale),
+                             add_table=int(bool(accumulate)))
+    if grad_loss is not None:
+        _on_gpu("grad_loss", grad_loss, device)
+        if grad_loss.dtype != torch.float32 or grad_loss.numel() != 1:
+            raise TypeError("grad_loss must be one float32 element")
+        g.grad_loss = grad_loss.data_ptr()
+    if grad_hidden is not None:
+        g.grad_hidden_stride = _rows("grad_hidden", grad_hidden, torch.bfloat16, device)
+        if grad_hidden.shape != hidden.shape:
+            raise ValueError("grad_hidden must have hidden's shape")
+        g.grad_hidden = grad_hidden.data_ptr() or None
+    if grad_table is not None:
+        g.grad_table_dtype = _float_code(grad_table.dtype)
+        g.grad_table_stride = _rows("grad_table", grad_table, grad_table.dtype, device)
+        if grad_table.shape != table.shape:
+            raise ValueError("grad_table must have the table's shape")
+        g.grad_table = grad_table.data_ptr()
+    _, need = _ops.lamb_xent_workspace(x)
+    work = _workspace(need, device)
+    with torch.cuda.device(device):
+        _ops.lamb_xent_backward(x, lse.data_ptr(), g, work.data_ptr(), need, _stream(device))

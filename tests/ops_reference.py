@@ -42,3 +42,26 @@ def relative(a, b):
     n = float(torch.linalg.vector_norm(b))
     d = float(torch.linalg.vector_norm(a - b))
     return d / n if n else d
+
+
+def cross_entropy(hidden, table, targets, ignore=-100, reduction="mean"):
+    """(mean, loss, grad_hidden, grad_table, size_hidden, size_table): the sizes are the
+    gradients' sums with every term's magnitude, what their rounding errors go by."""
+    h, w = hidden.double(), table.double()
+    keep = targets != ignore
+    rows = keep.nonzero()[:, 0]
+    h, t = h[rows], targets[rows].long()
+    z = h @ w.t().contiguous()
+    top = z.max(dim=1, keepdim=True).values if len(rows) else z[:, :1]
+    lse = torch.log(torch.exp(z - top).sum(dim=1, keepdim=True)) + top
+    loss = torch.zeros(len(targets), dtype=torch.float64, device=hidden.device)
+    loss[rows] = (lse - z.gather(1, t[:, None]))[:, 0]
+    count = max(1, len(rows))
+    q = torch.exp(z - lse)
+    q.scatter_add_(1, t[:, None], torch.full_like(lse, -1.0))
+    if reduction == "mean":
+        q = q / count
+    gh, sh = torch.zeros_like(hidden.double()), torch.zeros_like(hidden.double())
+    gh[rows], sh[rows] = q @ w, q.abs() @ w.abs()
+    qt = q.t().contiguous()
+    return loss.sum() / count, loss, gh, qt @ h, sh, qt.abs() @ h.abs()
