@@ -204,6 +204,40 @@ LAMB_API lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
                                         const lamb_xent_grads *grads, void *workspace,
                                         size_t workspace_bytes, void *stream);
 
+/*
+ * Rows of a token table: out[i] = scale table[ids[i]]. table [vocab][dim] and out
+ * [tokens][dim] are float32 or bfloat16 each, rows `*_stride` elements apart (>= dim;
+ * out's rows do not overlap), aligned to their elements. ids: LAMB_DTYPE_I32 or _I64.
+ * The row of an id outside [0, vocab) becomes NaN. tokens 0 to 2^24, vocab 1 to 2^24,
+ * dim 1 to 2^16.
+ */
+typedef struct lamb_embed {
+    const void *ids;
+    int64_t tokens, vocab, dim;
+    int32_t id_dtype;
+    float scale;
+} lamb_embed;
+
+LAMB_API lamb_status lamb_embed_forward(const lamb_embed *embed, const void *table,
+                                        int64_t table_stride, int32_t table_dtype, void *out,
+                                        int64_t out_stride, int32_t out_dtype, void *stream);
+
+/*
+ * The table's gradient: grad_table[v] = (or, with `add` 1, +=) scale times the sum of
+ * grad_out[i] over the tokens with ids[i] = v, in the tokens' order and in fp32: the
+ * same inputs give the same bits. Tokens whose id is outside the table or equals
+ * padding_id (-1 for none) add nothing. Without `add` every row is written; with it,
+ * only rows that tokens name are touched. lamb_embed_workspace gives the device
+ * workspace's bytes (256-byte aligned; host only).
+ */
+LAMB_API lamb_status lamb_embed_workspace(const lamb_embed *embed, size_t *bytes);
+
+LAMB_API lamb_status lamb_embed_backward(const lamb_embed *embed, const void *grad_out,
+                                         int64_t grad_out_stride, int32_t grad_out_dtype,
+                                         void *grad_table, int64_t grad_table_stride,
+                                         int32_t grad_table_dtype, int64_t padding_id, int32_t add,
+                                         void *workspace, size_t workspace_bytes, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

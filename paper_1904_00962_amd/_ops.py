@@ -30,7 +30,8 @@ SCALES = {"rms": LAMB_MUON_RMS, "spectral": LAMB_MUON_SPECTRAL, "unit": LAMB_MUO
 EXPORTS = ("lamb_ns_params_init", "lamb_ortho_plan_create", "lamb_orthogonalize",
            "lamb_muon_plan_create", "lamb_muon_hparams_init", "lamb_muon_step",
            "lamb_ns_plan_destroy", "lamb_xent_workspace", "lamb_xent_forward",
-           "lamb_xent_backward")
+           "lamb_xent_backward", "lamb_embed_forward", "lamb_embed_workspace",
+           "lamb_embed_backward")
 
 
 class lamb_ns_params(ctypes.Structure):
@@ -74,6 +75,11 @@ class lamb_xent_grads(ctypes.Structure):
                 ("grad_scale", ctypes.c_float)]
 
 
+class lamb_embed(ctypes.Structure):
+    _fields_ = [("ids", ctypes.c_void_p), ("tokens", ctypes.c_int64), ("vocab", ctypes.c_int64),
+                ("dim", ctypes.c_int64), ("id_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 _lib_ops: Optional[ctypes.CDLL] = None
 
 
@@ -95,6 +101,11 @@ def load() -> ctypes.CDLL:
     lib.lamb_xent_workspace.argtypes = [P(lamb_xent), P(size), P(size)]
     lib.lamb_xent_forward.argtypes = [P(lamb_xent), vp, vp, vp, vp, size, vp]
     lib.lamb_xent_backward.argtypes = [P(lamb_xent), vp, P(lamb_xent_grads), vp, size, vp]
+    i64 = ctypes.c_int64
+    lib.lamb_embed_forward.argtypes = [P(lamb_embed), vp, i64, i32, vp, i64, i32, vp]
+    lib.lamb_embed_workspace.argtypes = [P(lamb_embed), P(size)]
+    lib.lamb_embed_backward.argtypes = [P(lamb_embed), vp, i64, i32, vp, i64, i32, i64, i32, vp,
+                                        size, vp]
     for name in EXPORTS:
         getattr(lib, name).restype = ctypes.c_int
     _lib_ops = lib
@@ -196,3 +207,27 @@ def lamb_xent_backward(xent: lamb_xent, lse: int, grads: lamb_xent_grads, worksp
     _check(load().lamb_xent_backward(ctypes.byref(xent), _vp(lse), ctypes.byref(grads),
                                      _vp(workspace), workspace_bytes, _vp(stream)),
            "lamb_xent_backward")
+
+
+def lamb_embed_forward(embed: lamb_embed, table: int, table_stride: int, table_dtype: int, out: int,
+                       out_stride: int, out_dtype: int, stream: int = 0) -> None:
+    _check(load().lamb_embed_forward(ctypes.byref(embed), _vp(table), table_stride, table_dtype,
+                                     _vp(out), out_stride, out_dtype, _vp(stream)),
+           "lamb_embed_forward")
+
+
+def lamb_embed_workspace(embed: lamb_embed) -> int:
+    n = ctypes.c_size_t()
+    _check(load().lamb_embed_workspace(ctypes.byref(embed), ctypes.byref(n)),
+           "lamb_embed_workspace")
+    return n.value
+
+
+def lamb_embed_backward(embed: lamb_embed, grad_out: int, grad_out_stride: int,
+                        grad_out_dtype: int, grad_table: int, grad_table_stride: int,
+                        grad_table_dtype: int, padding_id: int, add: int, workspace: int,
+                        workspace_bytes: int, stream: int = 0) -> None:
+    _check(load().lamb_embed_backward(ctypes.byref(embed), _vp(grad_out), grad_out_stride,
+                                      grad_out_dtype, _vp(grad_table), grad_table_stride,
+                                      grad_table_dtype, padding_id, add, _vp(workspace),
+                                      workspace_bytes, _vp(stream)), "lamb_embed_backward")

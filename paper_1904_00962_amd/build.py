@@ -20,11 +20,12 @@ LIBRARY = os.path.join(PKG, "liblamb_mi355x.so")
 SOURCES = [os.path.join(CSRC, "lamb_kernels.hip"), os.path.join(CSRC, "lamb_static.hip"),
            os.path.join(CSRC, "lamb_api.cpp"), os.path.join(CSRC, "ortho_kernels.hip"),
            os.path.join(CSRC, "ortho_api.cpp"), os.path.join(CSRC, "xent_kernels.hip"),
-           os.path.join(CSRC, "xent_api.cpp")]
+           os.path.join(CSRC, "xent_api.cpp"), os.path.join(CSRC, "embed_kernels.hip"),
+           os.path.join(CSRC, "embed_api.cpp")]
 HEADERS = [os.path.join(INCLUDE, "lamb_mi355x.h"), os.path.join(INCLUDE, "lamb_ops.h"),
            *[os.path.join(CSRC, name) for name in
              ("lamb_internal.h", "lamb_host.h", "ops_host.h", "mma_tile.h", "ortho_internal.h",
-              "xent_internal.h")]]
+              "xent_internal.h", "embed_internal.h")]]
 # Measurement only: streams with the kernels' access patterns (bench.py).
 PROBE_LIBRARY = os.path.join(PKG, "libstream_probe.so")
 PROBE_SOURCES = [os.path.join(CSRC, "stream_probe.hip")]

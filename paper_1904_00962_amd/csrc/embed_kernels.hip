@@ -1,0 +1,355 @@
+// Lookup of a token table's rows, and the table's gradient, for gfx950.
+//
+// The gradient of row v is the sum of the gradients of the tokens with id v, in the
+// tokens' order, in fp32: the tokens are sorted by id first, so that no two sums meet
+// in one address and every call gives the same bits.
+//
+// Sorting takes one launch. Each workgroup owns a range of ids and reads all ids twice:
+// once to count its own (per wave's share of the tokens) and the smaller ones, which
+// gives every id its place, and once to put its tokens there. The ids are read from L2.
+//
+// Summing cuts the sorted order, not the table, into equal chunks, so that a frequent
+// id (or a batch of padding) is spread over many waves. An id's tokens that lie within
+// a chunk are summed and written; what reaches over a chunk's ends goes to a partial
+// sum, and a second pass joins these. Rows without tokens are written as zeros by the
+// first pass, unless the gradient is added to what is there.
+#include <hip/hip_runtime.h>
+#include <math.h>
+
+#include "embed_internal.h"
+
+namespace lamb_mi355x {
+namespace {
+
+__device__ inline uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, __bf16(v)); }
+__device__ inline float widen(uint16_t v) { return __uint_as_float(uint32_t(v) << 16); }
+
+__device__ inline int64_t id_at(const EmbedArgs &a, int64_t i) {
+    return a.wide ? ((const int64_t *)a.ids)[i] : int64_t(((const int32_t *)a.ids)[i]);
+}
+
+// Eight elements from column c of a row, `n` of them inside it.
+template <bool BF16>
+__device__ inline void load8(const void *base, int64_t at, int n, bool vector, float (&v)[8]) {
+    if (BF16) {
+        const uint16_t *p = (const uint16_t *)base + at;
+        if (vector && n >= 8) {
+            const uint4 w = *(const uint4 *)p;
+            const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                v[2 * i] = __uint_as_float(u[i] << 16);
+                v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+            }
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? widen(p[i]) : 0.0f;
+    } else {
+        const float *p = (const float *)base + at;
+        if (vector && n >= 8) {
+            const float4 lo = *(const float4 *)p, hi = *(const float4 *)(p + 4);
+            v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w;
+            v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+    }
+}
+
+template <bool BF16>
+__device__ inline void store8(void *base, int64_t at, int n, bool vector, const float (&v)[8]) {
+    if (BF16) {
+        uint16_t *p = (uint16_t *)base + at;
+        if (vector && n >= 8) {
+            uint32_t u[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                u[i] = uint32_t(to_bf16(v[2 * i])) | uint32_t(to_bf16(v[2 * i + 1])) << 16;
+            *(uint4 *)p = make_uint4(u[0], u[1], u[2], u[3]);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n)
+                p[i] = to_bf16(v[i]);
+    } else {
+        float *p = (float *)base + at;
+        if (vector && n >= 8) {
+            *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
+            *(float4 *)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n)
+                p[i] = v[i];
+    }
+}
+
+template <bool TABLE_BF16, bool OUT_BF16>
+__global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, EmbedRows r) {
+    const uint32_t per_row = uint32_t(a.dim + 7) / 8;
+    const int64_t unit = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t units = a.tokens * per_row;
+    if (unit >= units)
+        return;
+    const int64_t token = units <= INT32_MAX ? int64_t(uint32_t(unit) / per_row) : unit / per_row;
+    const int c = int(unit - token * per_row) * 8;
+    const int n = a.dim - c;
+    const int64_t id = id_at(a, token);
+    float v[8];
+    if (id >= 0 && id < a.vocab) {
+        load8<TABLE_BF16>(r.table, id * r.table_stride + c, n, r.vector, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] *= a.scale;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = NAN;
+    }
+    store8<OUT_BF16>(r.out, token * r.out_stride + c, n, r.vector, v);
+}
+
+__global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(EmbedArgs a, int32_t ids,
+                                                                     int64_t skip, int32_t *order,
+                                                                     int32_t *sorted,
+                                                                     int32_t *first) {
+    extern __shared__ int32_t counts[];  // [kSortWaves][ids], then [kSortWaves]
+    int32_t *smaller = counts + kSortWaves * ids;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t low = int64_t(blockIdx.x) * ids;
+    for (int i = threadIdx.x; i < kSortWaves * ids; i += kSortWaves * 64) counts[i] = 0;
+    __syncthreads();
+    // this wave's share of the tokens, whole groups of 64
+    const int64_t groups = (a.tokens + 63) / 64;
+    const int64_t share = (groups + kSortWaves - 1) / kSortWaves * 64;
+    const int64_t begin = wave * share;
+    const int64_t end = begin + share < a.tokens ? begin + share : a.tokens;
+    int32_t before = 0;
+    for (int64_t i = begin + lane; i < end; i += 64) {
+        const int64_t id = id_at(a, i);
+        if (id == skip || id < 0 || id >= a.vocab)
+            continue;
+        before += id < low;
+        if (id >= low && id < low + ids)
+            atomicAdd(&counts[wave * ids + int(id - low)], 1);
+    }
+#pragma unroll
+    for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d);
+    if (lane == 0)
+        smaller[wave] = before;
+    __syncthreads();
+    // every (id, wave)'s first place: a scan over the ids, 64 at a time, by one wave
+    if (wave == 0) {
+        int32_t base = 0;
+        for (int w = 0; w < kSortWaves; ++w) base += smaller[w];
+        for (int g = 0; g < ids; g += 64) {
+            const int id = g + lane;
+            int32_t total = 0;
+            if (id < ids)
+                for (int w = 0; w < kSortWaves; ++w) total += counts[w * ids + id];
+            int32_t scan = total;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int32_t up = __shfl_up(scan, d);
+                scan += lane >= d ? up : 0;
+            }
+            int32_t place = base + scan - total;
+            if (id < ids) {
+                if (low + id < a.vocab)
+                    first[low + id] = place;
+                if (low + id == a.vocab - 1)
+                    first[a.vocab] = place + total;
+                for (int w = 0; w < kSortWaves; ++w) {
+                    const int32_t n = counts[w * ids + id];
+                    counts[w * ids + id] = place;
+                    place += n;
+                }
+            }
+            base += __shfl(scan, 63);
+        }
+    }
+    __syncthreads();
+    // Put the tokens in their places. Lanes with the same id take theirs in lane order,
+    // found id by id among the few lanes of a group that are in the range.
+    int32_t *mine = counts + wave * ids;
+    for (int64_t g = begin; g < end; g += 64) {
+        const int64_t i = g + lane;
+        const int64_t id = i < end ? id_at(a, i) : -1;
+        const bool inside = id >= low && id < low + ids && id < a.vocab && id != skip;
+        uint64_t todo = __ballot(inside);
+        const int local = int(id - low);
+        while (todo) {
+            const int leader = __ffsll((unsigned long long)todo) - 1;
+            const int which = __shfl(local, leader);
+            const uint64_t same = __ballot(inside && local == which);
+            const int32_t place = mine[which];
+            if (inside && local == which) {
+                const int32_t at = place + __popcll(same & ((uint64_t(1) << lane) - 1));
+                order[at] = int32_t(i);
+                sorted[at] = int32_t(id);
+            }
+            if (lane == leader)
+                mine[which] = place + __popcll(same);
+            todo &= ~same;
+        }
+    }
+}
+
+// Writes, or adds to, a finished row's eight columns.
+template <bool BF16>
+__device__ inline void finish(const EmbedArgs &a, const EmbedGrad &g, int64_t id, int c,
+                              float (&v)[8]) {
+    const int n = a.dim - c;
+    const int64_t at = id * g.table_stride + c;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= a.scale;
+    if (g.add) {
+        float old[8];
+        load8<BF16>(g.table, at, n, g.vector, old);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += old[i];
+    }
+    store8<BF16>(g.table, at, n, g.vector, v);
+}
+
+// Waves of the first `chunks` x (columns / kSumColumns) sum a chunk's columns; where the
+// gradient is not added, the waves after them write the rows without tokens.
+template <bool ROWS_BF16, bool TABLE_BF16>
+__global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedGrad g) {
+    const int lane = threadIdx.x & 63;
+    const int across = g.columns / kSumColumns;
+    const int64_t chunks = (a.tokens + kSumTokens - 1) / kSumTokens;
+    int64_t work = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    if (work >= chunks * across) {
+        work -= chunks * across;
+        if (g.add || work >= a.vocab || g.first[work] != g.first[work + 1])
+            return;
+        const float zero[8] = {};
+        for (int c = lane * 8; c < a.dim; c += 512)
+            store8<TABLE_BF16>(g.table, work * g.table_stride + c, a.dim - c, g.vector, zero);
+        return;
+    }
+    const int64_t chunk = work / across;
+    const int c = int(work % across) * kSumColumns + lane * 8;
+    const int32_t total = g.first[a.vocab];
+    const int32_t begin = int32_t(chunk) * kSumTokens;
+    const int32_t end = begin + kSumTokens < total ? begin + kSumTokens : total;
+    if (begin >= total)
+        return;
+    // lane t holds the chunk's t-th token and id
+    const int32_t at = begin + lane < end ? begin + lane : end - 1;
+    const int32_t token_of = g.order[at], id_of = g.sorted[at];
+    const int n = a.dim - c;
+    const int32_t id_before = begin > 0 ? g.sorted[begin - 1] : -1;
+    const int32_t id_after = end < total ? g.sorted[end] : -1;
+    float sum[8] = {};
+    constexpr int kAhead = 4;  // rows in flight
+    for (int t0 = 0; t0 < end - begin; t0 += kAhead) {
+        float row[kAhead][8];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int32_t token = __shfl(token_of, t0 + k);
+            if (t0 + k < end - begin && n > 0)
+                load8<ROWS_BF16>(g.rows, token * g.rows_stride + c, n, g.vector, row[k]);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int t = t0 + k;
+            if (t >= end - begin)
+                break;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += row[k][i];
+            const int32_t id = __shfl(id_of, t);
+            const bool last = t + 1 == end - begin;
+            if (!last && __shfl(id_of, t + 1) == id)
+                continue;
+            // the id ends here, or goes on in the next chunk
+            const bool open = last && id == id_after;
+            if (n > 0) {
+                if (open || id == id_before) {
+                    // an id that reaches back goes to the chunk's first slot, one that
+                    // only reaches on to its second
+                    float *to = g.partial + (2 * chunk + (id != id_before)) * g.columns + c;
+                    *(float4 *)to = make_float4(sum[0], sum[1], sum[2], sum[3]);
+                    *(float4 *)(to + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
+                } else {
+                    finish<TABLE_BF16>(a, g, id, c, sum);
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+        }
+    }
+}
+
+// A wave per chunk and kSumColumns columns: if an id begins in the chunk and goes on,
+// its partial sums from there on, in order.
+template <bool TABLE_BF16>
+__global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, EmbedGrad g) {
+    const int lane = threadIdx.x & 63;
+    const int across = g.columns / kSumColumns;
+    const int64_t work = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
+    const int64_t chunk = work / across;
+    const int c = int(work % across) * kSumColumns + lane * 8;
+    const int32_t total = g.first[a.vocab];
+    const int64_t end = (chunk + 1) * kSumTokens;
+    if (end >= total || c >= a.dim)
+        return;
+    const int32_t id = g.sorted[end - 1];
+    if (g.sorted[end] != id || g.first[id] < chunk * kSumTokens)
+        return;
+    const int64_t last = (g.first[id + 1] - 1) / kSumTokens;
+    float sum[8];
+    load8<false>(g.partial, (2 * chunk + 1) * g.columns + c, 8, true, sum);
+    for (int64_t k = chunk + 1; k <= last; ++k) {
+        float part[8];
+        load8<false>(g.partial, 2 * k * g.columns + c, 8, true, part);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += part[i];
+    }
+    finish<TABLE_BF16>(a, g, id, c, sum);
+}
+
+}  // namespace
+
+hipError_t launch_embed(const EmbedArgs &args, const EmbedRows &rows, hipStream_t stream) {
+    const int64_t units = args.tokens * ((args.dim + 7) / 8);
+    const uint32_t blocks = uint32_t((units + 255) / 256);
+    auto kernel = rows.table_bf16
+                      ? (rows.out_bf16 ? embed_kernel<true, true> : embed_kernel<true, false>)
+                      : (rows.out_bf16 ? embed_kernel<false, true> : embed_kernel<false, false>);
+    kernel<<<blocks, 256, 0, stream>>>(args, rows);
+    return hipGetLastError();
+}
+
+hipError_t launch_embed_sort(const EmbedArgs &args, int64_t skip, int32_t *order, int32_t *sorted,
+                             int32_t *first, hipStream_t stream) {
+    const int32_t ids = sort_ids(args.tokens);
+    const uint32_t blocks = uint32_t((args.vocab + ids - 1) / ids);
+    embed_sort_kernel<<<blocks, kSortWaves * 64, (ids + 1) * kSortWaves * 4, stream>>>(
+        args, ids, skip, order, sorted, first);
+    return hipGetLastError();
+}
+
+hipError_t launch_embed_sum(const EmbedArgs &args, const EmbedGrad &grad, hipStream_t stream) {
+    const int64_t chunks = (args.tokens + kSumTokens - 1) / kSumTokens;
+    const int64_t waves = chunks * (grad.columns / kSumColumns) + (grad.add ? 0 : args.vocab);
+    auto kernel =
+        grad.rows_bf16
+            ? (grad.table_bf16 ? embed_sum_kernel<true, true> : embed_sum_kernel<true, false>)
+            : (grad.table_bf16 ? embed_sum_kernel<false, true> : embed_sum_kernel<false, false>);
+    kernel<<<uint32_t((waves + 3) / 4), 256, 0, stream>>>(args, grad);
+    return hipGetLastError();
+}
+
+hipError_t launch_embed_join(const EmbedArgs &args, const EmbedGrad &grad, hipStream_t stream) {
+    const int64_t chunks = (args.tokens + kSumTokens - 1) / kSumTokens;
+    const int64_t waves = chunks * (grad.columns / kSumColumns);
+    auto kernel = grad.table_bf16 ? embed_join_kernel<true> : embed_join_kernel<false>;
+    kernel<<<uint32_t((waves + 3) / 4), 256, 0, stream>>>(args, grad);
+    return hipGetLastError();
+}
+
+}  // namespace lamb_mi355x

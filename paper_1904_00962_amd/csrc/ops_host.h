@@ -82,4 +82,31 @@ inline lamb_status check_spans(Span *spans, size_t n) {
     return LAMB_OK;
 }
 
+// The limits that the operators' entry points share.
+constexpr int64_t kMaxTokens = int64_t(1) << 24, kMaxVocab = int64_t(1) << 24,
+                  kMaxDim = int64_t(1) << 16, kMaxStride = int64_t(1) << 40;
+
+inline bool is_float(int32_t dtype) {
+    return dtype == LAMB_DTYPE_F32 || dtype == LAMB_DTYPE_BF16;
+}
+inline bool is_id(int32_t dtype) { return dtype == LAMB_DTYPE_I32 || dtype == LAMB_DTYPE_I64; }
+inline int64_t size_of(int32_t dtype) {
+    return dtype == LAMB_DTYPE_BF16 ? 2 : dtype == LAMB_DTYPE_I64 ? 8 : 4;
+}
+
+// Bytes from the first to the last element of `rows` rows.
+inline uint64_t rows_bytes(int64_t rows, int64_t stride, int64_t cols, int64_t size) {
+    return rows ? uint64_t((rows - 1) * stride + cols) * uint64_t(size) : 0;
+}
+
+inline lamb_status check_workspace(const void *workspace, size_t bytes, size_t need) {
+    if (!workspace)
+        return fail(LAMB_ENULL, "workspace must not be NULL");
+    if (!aligned_to(workspace, 256))
+        return fail(LAMB_EALIGN, "the workspace must be 256-byte aligned");
+    if (bytes < need)
+        return fail(LAMB_EINVAL, "the workspace has %zu bytes, the call needs %zu", bytes, need);
+    return LAMB_OK;
+}
+
 }  // namespace lamb_mi355x

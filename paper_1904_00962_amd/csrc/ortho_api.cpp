@@ -26,7 +26,6 @@ struct lamb_ns_plan {
 namespace {
 
 constexpr int64_t kMaxSide = int64_t(1) << 20;
-constexpr int64_t kMaxStride = int64_t(1) << 40;
 
 // The bounds of lamb_ns_params: where singular values that start in [0, 1] go.
 lamb_status check_params(const lamb_ns_params &p) {
@@ -309,15 +308,13 @@ lamb_status lamb_ortho_plan_create(const lamb_matrix *matrices, int32_t n, int32
         return fail(LAMB_ENULL, "matrices must not be NULL");
     if (n < 1)
         return fail(LAMB_EINVAL, "n = %d, need >= 1", n);
-    if ((in_dtype != LAMB_DTYPE_F32 && in_dtype != LAMB_DTYPE_BF16) ||
-        (out_dtype != LAMB_DTYPE_F32 && out_dtype != LAMB_DTYPE_BF16))
+    if (!is_float(in_dtype) || !is_float(out_dtype))
         return fail(LAMB_EINVAL, "matrices are float32 or bfloat16");
     lamb_status st = check_precision(precision);
     if (st != LAMB_OK)
         return st;
     return guarded([&]() -> lamb_status {
-        const int64_t in_size = in_dtype == LAMB_DTYPE_BF16 ? 2 : 4;
-        const int64_t out_size = out_dtype == LAMB_DTYPE_BF16 ? 2 : 4;
+        const int64_t in_size = size_of(in_dtype), out_size = size_of(out_dtype);
         std::vector<NsMatrix> list;
         std::vector<Span> spans;
         for (int32_t i = 0; i < n; ++i) {
@@ -333,13 +330,13 @@ lamb_status lamb_ortho_plan_create(const lamb_matrix *matrices, int32_t n, int32
                             static_cast<long long>(t.cols));
             if (!aligned_to(t.in, uintptr_t(in_size)) || !aligned_to(t.out, uintptr_t(out_size)))
                 return fail(LAMB_EALIGN, "matrix %d: a pointer is not aligned to its elements", i);
-            const int64_t in_len = ((t.rows - 1) * t.in_stride + t.cols) * in_size;
-            const int64_t out_len = ((t.rows - 1) * t.out_stride + t.cols) * out_size;
             const bool in_place =
                 t.in == t.out && in_dtype == out_dtype && t.in_stride == t.out_stride;
             if (!in_place)
-                spans.push_back(span_of(t.in, in_len, false, i, "in"));
-            spans.push_back(span_of(t.out, out_len, true, i, "out"));
+                spans.push_back(span_of(
+                    t.in, rows_bytes(t.rows, t.in_stride, t.cols, in_size), false, i, "in"));
+            spans.push_back(span_of(
+                t.out, rows_bytes(t.rows, t.out_stride, t.cols, out_size), true, i, "out"));
             NsMatrix m{};
             m.in = t.in;
             m.out = t.out;
@@ -371,7 +368,7 @@ lamb_status lamb_muon_plan_create(const lamb_muon_tensor *tensors, int32_t n, in
         return fail(LAMB_ENULL, "tensors must not be NULL");
     if (n < 1)
         return fail(LAMB_EINVAL, "n = %d, need >= 1", n);
-    if (g_dtype != LAMB_DTYPE_F32 && g_dtype != LAMB_DTYPE_BF16)
+    if (!is_float(g_dtype))
         return fail(LAMB_EINVAL, "gradients are float32 or bfloat16");
     lamb_status st = check_precision(precision);
     if (st != LAMB_OK)
@@ -394,7 +391,8 @@ lamb_status lamb_muon_plan_create(const lamb_muon_tensor *tensors, int32_t n, in
                 return fail(LAMB_EALIGN, "matrix %d: every buffer must be 16-byte aligned", i);
             const uint64_t numel = uint64_t(t.rows) * uint64_t(t.cols);
             spans.push_back(span_of(t.x, numel * 4, true, i, "x"));
-            spans.push_back(span_of(t.g, numel * (g_dtype == LAMB_DTYPE_BF16 ? 2 : 4), false, i, "g"));
+            spans.push_back(span_of(t.g, numel * uint64_t(size_of(g_dtype)), false, i,
+                                    "g"));
             spans.push_back(span_of(t.m, numel * 4, true, i, "m"));
             NsMatrix m{};
             m.in = t.g;

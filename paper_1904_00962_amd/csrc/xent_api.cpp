@@ -9,9 +9,7 @@ using namespace lamb_mi355x;
 
 namespace {
 
-constexpr int64_t kMaxTokens = int64_t(1) << 24, kMaxVocab = int64_t(1) << 24,
-                  kMaxDim = int64_t(1) << 16, kMaxStride = int64_t(1) << 40,
-                  kMaxReadStride = int64_t(1) << 21;  // a tile's rows within 32-bit offsets
+constexpr int64_t kMaxReadStride = int64_t(1) << 21;  // a tile's rows within 32-bit offsets
 // A piece of the vocabulary's softmax: written once and read twice, so kept within
 // the 256 MiB last-level cache.
 constexpr int64_t kPieceBytes = int64_t(128) << 20;
@@ -28,7 +26,7 @@ lamb_status check(const lamb_xent *x) {
         return fail(LAMB_EINVAL,
                     "tokens %lld, vocab %lld, dim %lld: need 0 to 2^24, 1 to 2^24, 1 to 2^16",
                     (long long)x->tokens, (long long)x->vocab, (long long)x->dim);
-    if (x->target_dtype != LAMB_DTYPE_I32 && x->target_dtype != LAMB_DTYPE_I64)
+    if (!is_id(x->target_dtype))
         return fail(LAMB_EINVAL, "targets are int32 or int64");
     if (!x->table || (x->tokens && (!x->hidden || !x->targets)))
         return fail(LAMB_ENULL, "hidden, table and targets must not be NULL");
@@ -36,7 +34,7 @@ lamb_status check(const lamb_xent *x) {
         x->table_stride > kMaxStride)
         return fail(LAMB_EINVAL, "a row stride is below dim, or above 2^40");
     if (!aligned_to(x->hidden, 2) || !aligned_to(x->table, 2) ||
-        !aligned_to(x->targets, x->target_dtype == LAMB_DTYPE_I64 ? 8 : 4))
+        !aligned_to(x->targets, uintptr_t(size_of(x->target_dtype))))
         return fail(LAMB_EALIGN, "a pointer is not aligned to its elements");
     return LAMB_OK;
 }
@@ -157,20 +155,6 @@ lamb_status begin(const lamb_xent &x, const Layout &l, char *work, float *loss, 
     return err == hipSuccess ? LAMB_OK : fail_hip(err, "kernel launch");
 }
 
-lamb_status check_workspace(const void *workspace, size_t bytes, size_t need) {
-    if (!workspace)
-        return fail(LAMB_ENULL, "workspace must not be NULL");
-    if (!aligned_to(workspace, 256))
-        return fail(LAMB_EALIGN, "the workspace must be 256-byte aligned");
-    if (bytes < need)
-        return fail(LAMB_EINVAL, "the workspace has %zu bytes, the call needs %zu", bytes, need);
-    return LAMB_OK;
-}
-
-uint64_t rows_bytes(int64_t rows, int64_t stride, int64_t cols, int64_t size) {
-    return rows ? uint64_t((rows - 1) * stride + cols) * uint64_t(size) : 0;
-}
-
 }  // namespace
 
 extern "C" {
@@ -202,7 +186,7 @@ lamb_status lamb_xent_forward(const lamb_xent *xent, float *loss, float *lse, fl
     st = check_workspace(workspace, workspace_bytes, l.forward);
     if (st != LAMB_OK)
         return st;
-    const int64_t id = x.target_dtype == LAMB_DTYPE_I64 ? 8 : 4;
+    const int64_t id = size_of(x.target_dtype);
     Span spans[] = {
         span_of(x.hidden, rows_bytes(x.tokens, x.hidden_stride, x.dim, 2), false, 0, "hidden"),
         span_of(x.table, rows_bytes(x.vocab, x.table_stride, x.dim, 2), false, 0, "table"),
@@ -248,7 +232,7 @@ lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
     if (!std::isfinite(g.grad_scale))
         return fail(LAMB_EINVAL, "grads.grad_scale = %g must be finite", double(g.grad_scale));
     const bool bf16 = g.grad_table_dtype == LAMB_DTYPE_BF16;
-    if (g.grad_table && !bf16 && g.grad_table_dtype != LAMB_DTYPE_F32)
+    if (g.grad_table && !is_float(g.grad_table_dtype))
         return fail(LAMB_EINVAL, "grad_table is float32 or bfloat16");
     if ((g.grad_hidden && (g.grad_hidden_stride < x.dim || g.grad_hidden_stride > kMaxStride)) ||
         (g.grad_table && (g.grad_table_stride < x.dim || g.grad_table_stride > kMaxStride)))
@@ -260,7 +244,7 @@ lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
     st = check_workspace(workspace, workspace_bytes, l.backward);
     if (st != LAMB_OK)
         return st;
-    const int64_t id = x.target_dtype == LAMB_DTYPE_I64 ? 8 : 4;
+    const int64_t id = size_of(x.target_dtype);
     Span spans[] = {
         span_of(x.hidden, rows_bytes(x.tokens, x.hidden_stride, x.dim, 2), false, 0, "hidden"),
         span_of(x.table, rows_bytes(x.vocab, x.table_stride, x.dim, 2), false, 0, "table"),

@@ -14,7 +14,7 @@
 // where a tile past them ends at once. What such a token's row holds, NaN included,
 // reaches no result.
 //
-// Q's rounding to bf16 (2^-9 at most, relative, each entry by itself) is the one to
+// Q's rounding to bf16 (2^-8 at most, relative, each entry by itself) is the one to
 // fewer bits; sums are fp32.
 #include <hip/hip_runtime.h>
 #include <math.h>

@@ -3,6 +3,8 @@
   Orthogonalizer            lists of matrices made orthogonal by Newton-Schulz products
   linear_cross_entropy      softmax cross entropy against a vocabulary table, and
   linear_cross_entropy_grad its gradients, without keeping the logits
+  embedding                 rows of a token table, scaled
+  embedding_grad            the table's gradient, summed in the tokens' order
 
 PyTorch supplies device memory and the current stream only; the work is the HIP
 library's (``_ops``). Argument errors raise ``ValueError`` or ``TypeError`` here,
@@ -207,3 +209,56 @@ def linear_cross_entropy_grad(hidden, table, targets, lse, grad_hidden=None, gra
     work = _workspace(need, device)
     with torch.cuda.device(device):
         _ops.lamb_xent_backward(x, lse.data_ptr(), g, work.data_ptr(), need, _stream(device))
+
+
+def _embed(ids, table, scale):
+    code = _ids("ids", ids, table.device)
+    return _ops.lamb_embed(ids.data_ptr() or None, ids.numel(), table.shape[0], table.shape[1],
+                           code, float(scale))
+
+
+def embedding(ids, table, *, scale: float = 1.0, out_dtype=None, out=None):
+    """``scale`` x the rows of ``table`` [vocab, dim] (float32 or bfloat16) that ``ids``
+    (int32 or int64, any shape) name: a tensor [*ids.shape, dim] of ``out_dtype`` (the
+    table's by default), or ``out`` [ids.numel(), dim]. An id outside the table gives a
+    row of NaN."""
+    torch = _torch()
+    stride = _rows("table", table, table.dtype)
+    e = _embed(ids, table, scale)
+    if out is None:
+        result = torch.empty(*ids.shape, table.shape[1], dtype=out_dtype or table.dtype,
+                             device=table.device)
+        out_stride = table.shape[1]
+    else:
+        result = out
+        out_stride = _rows("out", out, out_dtype or out.dtype, table.device)
+        if out.shape != (ids.numel(), table.shape[1]):
+            raise ValueError("out must be [%d, %d]" % (ids.numel(), table.shape[1]))
+    with torch.cuda.device(table.device):
+        _ops.lamb_embed_forward(e, table.data_ptr(), stride, _float_code(table.dtype),
+                                result.data_ptr(), out_stride, _float_code(result.dtype),
+                                _stream(table.device))
+    return result
+
+
+def embedding_grad(ids, grad_out, grad_table, *, scale: float = 1.0,
+                   padding_id: Optional[int] = None, accumulate: bool = False) -> None:
+    """The gradient of :func:`embedding` for its table into ``grad_table`` [vocab, dim]:
+    row v becomes, or with ``accumulate`` grows by, ``scale`` x the sum of the rows of
+    ``grad_out`` [ids.numel(), dim] whose id is v, in their order and in fp32. Either is
+    float32 or bfloat16. Tokens with id ``padding_id``, or outside the table, add
+    nothing."""
+    torch = _torch()
+    stride = _rows("grad_table", grad_table, grad_table.dtype)
+    out_stride = _rows("grad_out", grad_out, grad_out.dtype, grad_table.device)
+    if grad_out.shape != (ids.numel(), grad_table.shape[1]):
+        raise ValueError("grad_out must be [%d, %d]" % (ids.numel(), grad_table.shape[1]))
+    e = _embed(ids, grad_table, scale)
+    need = _ops.lamb_embed_workspace(e)
+    work = _workspace(need, grad_table.device)
+    with torch.cuda.device(grad_table.device):
+        _ops.lamb_embed_backward(
+            e, grad_out.data_ptr(), out_stride, _float_code(grad_out.dtype),
+            grad_table.data_ptr(), stride, _float_code(grad_table.dtype),
+            -1 if padding_id is None else int(padding_id), int(bool(accumulate)),
+            work.data_ptr(), need, _stream(grad_table.device))

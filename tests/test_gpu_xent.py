@@ -3,9 +3,10 @@
 
 Tolerances. Logits are sums of exact products in fp32: off by at most dim 2^-24 of the
 sum of magnitudes, in practice by far less; losses are held to 2e-6 (1 + largest
-logit). Q is rounded to bf16, each entry by at most 2^-9: the gradients are held, as a
-2-norm, to 2^-8 (that and the result's own rounding) of the sums of magnitudes of their
-terms, which the fp32 errors of lse stay below."""
+logit). Q is rounded to bf16, and so is a bf16 result, each entry by at most 2^-8 and
+by 2^-9.2 in the root mean square: the gradients are held, as a 2-norm, to 2^-8 (the
+two together are 2^-8.7) of the sums of magnitudes of their terms, which the fp32
+errors of lse stay below."""
 
 import math
 
