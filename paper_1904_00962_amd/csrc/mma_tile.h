@@ -35,6 +35,36 @@ constexpr int kBufferBytes = 0x7ffffff0;  // a voffset with the sign bit set is 
 constexpr int kOutside = int(0x80000000u);
 
 #define LAMB_LDS __attribute__((address_space(3)))
+#define LAMB_GLOBAL __attribute__((address_space(1)))
+
+template <int BYTES>
+struct Words {
+    using Type = uint32_t __attribute__((ext_vector_type(BYTES / 4)));
+};
+template <>
+struct Words<4> {
+    using Type = uint32_t;
+};
+template <>
+struct Words<2> {
+    using Type = uint16_t;
+};
+
+// Global memory through pointers that themselves come out of memory, which the
+// compiler would else access as possibly LDS.
+template <class T>
+__device__ inline T load_global(const void *p) {
+    const auto w = *(LAMB_GLOBAL const typename Words<sizeof(T)>::Type *)p;
+    T v;
+    __builtin_memcpy(&v, &w, sizeof v);
+    return v;
+}
+template <class T>
+__device__ inline void store_global(void *p, T v) {
+    typename Words<sizeof(T)>::Type w;
+    __builtin_memcpy(&w, &v, sizeof v);
+    *(LAMB_GLOBAL typename Words<sizeof(T)>::Type *)p = w;
+}
 
 struct HalfMath {
     using Elem = _Float16;
@@ -74,9 +104,10 @@ struct TileShape {
     static constexpr int kStage = (kA + kB) * PARTS;
     static constexpr int kLds = kStage * STAGES;
     static constexpr int kLoads = kStage / 8 / kThreads;  // a lane's loads per stage
-    // workgroups per CU that LDS allows
-    static constexpr int kPerCu = 160 * 1024 / (kLds * 2);
-    static_assert(DEPTH % 32 == 0 && STAGES >= 2 && kPerCu >= 1 && kLoads * (STAGES - 2) < 64, "");
+    static constexpr bool kAlternating = kWaves == 8;
+    // workgroups per CU: what LDS allows, and at most two
+    static constexpr int kPerCu = 160 * 1024 / (kLds * 2) >= 2 ? 2 : 1;
+    static_assert(DEPTH % 32 == 0 && STAGES >= 2 && kLds * 2 <= 160 * 1024 && kLoads * (STAGES - 2) < 64, "");
 };
 
 // Bank swizzle of a `rows` stage: 8 rows at the same k get different banks.
@@ -211,6 +242,62 @@ __device__ inline void run_stages(int32_t count, const short *lds, Issue issue, 
     meet<0>();
 }
 
+// A meeting in the middle of a turn: what has been read from LDS is in registers, and
+// OPEN of the wave's loads may still run. Nothing moves over it.
+template <int OPEN>
+__device__ inline void phase() {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(OPEN) : "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// The alternating form, for workgroups of 8 waves that have a CU to themselves. The
+// waves 0..3 and 4..7 are a phase apart, so that of the two waves on a SIMD one reads
+// fragments while the other's matrix instructions run: read(stage, part) and
+// compute(part), for the PARTS parts of a stage. A stage's place is loaded again once
+// the later half has read it, one phase after the earlier half.
+template <class Shape, int PARTS, class Issue, class Read, class Compute>
+__device__ inline void run_alternating(int32_t count, const short *lds, int wave, Issue issue,
+                                       Read read, Compute compute) {
+    static_assert(Shape::kWaves == 8, "two waves on each SIMD");
+    constexpr int kOpen = (Shape::STAGES - 2) * Shape::kLoads;
+#pragma unroll
+    for (int s = 0; s < Shape::STAGES - 1; ++s) issue(lds + s * Shape::kStage);
+    const short *reads = lds, *writes = lds + (Shape::STAGES - 1) * Shape::kStage;
+    const short *end = lds + Shape::kLds;
+    auto next = [&](const short *p) {
+        p += Shape::kStage;
+        return p == end ? lds : p;
+    };
+    phase<kOpen>();
+    if (wave >= 4)
+        phase<kOpen>();
+    for (int32_t it = 0; it < count; ++it) {
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+            read(reads, part);
+            if (part == 0)
+                issue(writes);
+            // the next stage has landed when this one's last part has been read
+            if (part + 1 == PARTS)
+                phase<kOpen>();
+            else
+                phase<kOpen + Shape::kLoads>();
+            __builtin_amdgcn_s_setprio(1);
+            compute(part);
+            __builtin_amdgcn_s_setprio(0);
+            phase<kOpen + Shape::kLoads>();
+        }
+        reads = next(reads);
+        writes = next(writes);
+    }
+    if (wave < 4)
+        phase<kOpen + Shape::kLoads>();
+    meet<0>();
+}
+
 // acc[i][j][r] += D at row 16 i + lane % 16 and column 16 j + 4 (lane / 16) + r of
 // the wave's part, over `depth` values of k.
 //
@@ -256,6 +343,54 @@ __device__ inline void tile_product(float4v (&acc)[Shape::MI][Shape::NI], const 
         return read_fragment<Shape::BN, D, COLS_B>(s + Shape::PARTS * kA,
                                                    (wn * Shape::NI + j) * 16, step, lane);
     };
+    const int32_t count = int32_t((depth + D - 1) / D);
+    if constexpr (Shape::kAlternating) {
+        static_assert(D == 32, "a stage is one step");
+        // two parts keep a split product's fragments within the registers
+        constexpr int kParts = Shape::PARTS, kRows = Shape::MI / kParts;
+        short8v fa[Shape::PARTS][kRows], fb[Shape::PARTS][Shape::NI];
+        run_alternating<Shape, kParts>(
+            count, lds, wave, issue,
+            [&](const short *s, int part) {
+#pragma unroll
+                for (int p = 0; p < Shape::PARTS; ++p) {
+                    if (part == 0) {
+#pragma unroll
+                        for (int j = 0; j < Shape::NI; ++j) fb[p][j] = read_b(s + p * kB, j, 0);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i)
+                        fa[p][i] = read_a(s + p * kA, part * kRows + i, 0);
+                }
+            },
+            [&](int part) {
+#pragma unroll
+                for (int i = 0; i < kRows; ++i) {
+                    float4v(&to)[Shape::NI] = acc[part * kRows + i];
+                    if constexpr (!kSplit) {
+#pragma unroll
+                        for (int j = 0; j < Shape::NI; ++j)
+                            to[j] = Math::mma(fb[0][j], fa[0][i], to[j]);
+                    } else {
+                        float4v sum[Shape::NI];
+#pragma unroll
+                        for (int j = 0; j < Shape::NI; ++j)
+                            sum[j] = Math::mma(fb[0][j], fa[1][i], float4v{});
+#pragma unroll
+                        for (int j = 0; j < Shape::NI; ++j)
+                            sum[j] = Math::mma(fb[1][j], fa[0][i], sum[j]);
+#pragma unroll
+                        for (int j = 0; j < Shape::NI; ++j)
+                            sum[j] = Math::mma(fb[0][j], fa[0][i], sum[j]);
+#pragma unroll
+                        for (int j = 0; j < Shape::NI; ++j)
+#pragma unroll
+                            for (int r = 0; r < 4; ++r) to[j][r] += sum[j][r];
+                    }
+                }
+            });
+        return;
+    }
     auto compute = [&](const short *s) {
 #pragma unroll
         for (int step = 0; step < D / 32; ++step) {
@@ -289,7 +424,7 @@ __device__ inline void tile_product(float4v (&acc)[Shape::MI][Shape::NI], const 
             }
         }
     };
-    run_stages<Shape>(int32_t((depth + D - 1) / D), lds, issue, compute);
+    run_stages<Shape>(count, lds, issue, compute);
 }
 
 // The lane's first value of acc in the tile.
@@ -300,6 +435,43 @@ struct Place {
         const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
         row = wave / Shape::WN * (Shape::BM / Shape::WM) + (lane & 15);
         col = wave % Shape::WN * (Shape::BN / Shape::WN) + 4 * (lane >> 4);
+    }
+};
+
+// A tile of 16-bit values leaves through LDS, so that rows are written 16 bytes a lane:
+// put() writes the lane's four of row m, columns n .. n + 3 (MIRROR: of column m, rows
+// n .. n + 3 of the transposed tile), flush() stores the tile's rows. 16-byte pieces
+// are swapped within a row, by slot(), to spread the banks. All of the workgroup takes
+// part; LDS must hold ROWS x COLS elements.
+template <int ROWS, int COLS, int THREADS>
+struct TileStore {
+    static constexpr int kPieces = COLS / 8;
+    static constexpr int kMask = kPieces < 8 ? kPieces - 1 : 7;
+    short *lds;
+    __device__ explicit TileStore(short *p) : lds(p) {}
+    static __device__ int at(int row, int col, int slot) {
+        return row * COLS + (((col >> 3) ^ (slot & kMask)) << 3) + (col & 7);
+    }
+    __device__ void put(int m, int n, ushort4 v) const { *(ushort4 *)(lds + at(m, n, m)) = v; }
+    __device__ void put_mirror(int m, int n, ushort4 v) const {
+        lds[at(n, m, n >> 2)] = short(v.x);
+        lds[at(n + 1, m, n >> 2)] = short(v.y);
+        lds[at(n + 2, m, n >> 2)] = short(v.z);
+        lds[at(n + 3, m, n >> 2)] = short(v.w);
+    }
+    // Rows and columns below the limits, from `to` with `ld` elements a row; the column
+    // limit is a multiple of 8.
+    template <bool MIRROR>
+    __device__ void flush(uint16_t *to, int64_t ld, int rows, int cols) const {
+        __syncthreads();
+#pragma unroll 4
+        for (int p = threadIdx.x; p < ROWS * kPieces; p += THREADS) {
+            const int row = p / kPieces, col = p % kPieces * 8;
+            if (row < rows && col < cols)
+                store_global(to + row * ld + col,
+                             *(const uint4 *)(lds + at(row, col, MIRROR ? row >> 2 : row)));
+        }
+        __syncthreads();
     }
 };
 

@@ -17,15 +17,17 @@ namespace lamb_mi355x {
 
 constexpr int kXcds = 8;  // accelerator dies, each with its own L2; blocks go to them in turn
 
-// Workgroup b of `n` runs on die b % kXcds. Gives each die a run of consecutive
-// items, so that tiles that read the same operand rows share an L2.
+// Workgroup b runs on die b % kXcds. Deals the items to the dies in runs, so that tiles
+// that read the same operand rows share an L2, and each die still gets its part of the
+// long items, which come first.
 template <class T>
 std::vector<T> spread_over_dies(const std::vector<T> &items) {
-    const size_t n = items.size(), each = n / kXcds, more = n % kXcds;
+    constexpr size_t kRun = 8;
+    const size_t n = items.size(), whole = n / (kXcds * kRun) * (kXcds * kRun);
     std::vector<T> out(n);
     for (size_t b = 0; b < n; ++b) {
         const size_t die = b % kXcds, at = b / kXcds;
-        out[b] = items[die * each + (die < more ? die : more) + at];
+        out[b] = b < whole ? items[(at / kRun * kXcds + die) * kRun + at % kRun] : items[b];
     }
     return out;
 }

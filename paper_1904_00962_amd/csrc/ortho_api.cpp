@@ -13,7 +13,7 @@ struct lamb_ns_plan {
     int device = 0;
     bool muon = false, bf16_in = false, split = false;
     NsKind kind = kNsBf16Out;
-    int shape = 0;
+    int sym_shape = 0, update_shape = 0;
     int32_t n = 0, blocks = 0, n_sym = 0, n_update = 0;
     void *block = nullptr;  // every device buffer of the plan
     NsMatrix *matrices = nullptr;
@@ -74,34 +74,58 @@ lamb_status check_params(const lamb_ns_params &p) {
     return LAMB_OK;
 }
 
-// A product takes the largest tiles that still fill the device: kFill workgroups.
-// Split products have no large shape.
-constexpr int64_t kFill = 512;
+// The tile shape of a product is the one whose estimated time is least: the longest
+// tile alone, or all tiles' time over the CUs, whichever is more. Microseconds, from
+// lists of 1 to 1024 tiles with k = 1024 and 4096 on one GPU: a tile's fixed part, and
+// its time per 1024 of k on a CU by itself and where all CUs work.
+struct TileCost {
+    double fixed, alone, full;
+};
+constexpr TileCost kCost[2][3] = {{{2.0, 3.7, 3.0}, {4.0, 8.6, 7.5}, {8.0, 17.5, 24.5}},
+                                  {{2.5, 8.5, 7.9}, {6.0, 19.8, 20.0}, {18.0, 58.0, 77.0}}};
+constexpr double kCus = 256.0;
 
-int pick_shape(const std::vector<NsMatrix> &matrices, bool split) {
-    for (int shape = split ? kNsSmall : kNsLarge; shape > kNsTiny; --shape) {
-        int64_t tiles = 0;
-        for (const NsMatrix &m : matrices)
-            tiles += (round_up(m.rows, ns_tile_rows(shape)) / ns_tile_rows(shape)) *
-                     (round_up(m.cols, ns_tile_cols(shape)) / ns_tile_cols(shape));
-        if (tiles >= kFill)
-            return shape;
+struct Estimate {
+    TileCost cost;
+    double longest = 0.0, total = 0.0;
+    void add(double tiles, double depth) {
+        longest = std::max(longest, cost.fixed + depth / 1024.0 * cost.alone);
+        total += tiles * (cost.fixed + depth / 1024.0 * cost.full);
     }
-    return kNsTiny;
+    double time() const { return std::max(longest, total / kCus); }
+};
+
+void pick_shapes(const std::vector<NsMatrix> &matrices, bool split, int *sym, int *update) {
+    double best_sym = 1e300, best_update = 1e300;
+    for (int shape = kNsTiny; shape <= kNsLarge; ++shape) {
+        const double t = ns_tile(shape);
+        Estimate gram{kCost[split][shape]}, poly{kCost[split][shape]}, up{kCost[split][shape]};
+        for (const NsMatrix &m : matrices) {
+            const double side = std::min(m.rows, m.cols), length = std::max(m.rows, m.cols);
+            const double across = std::ceil(side / t);
+            gram.add(across * (across + 1) / 2, length);
+            poly.add(across * (across + 1) / 2, side);
+            up.add(across * std::ceil(length / t), side);
+        }
+        const double time_sym = gram.time() + poly.time();
+        if (time_sym < best_sym)
+            best_sym = time_sym, *sym = shape;
+        if (up.time() < best_update)
+            best_update = up.time(), *update = shape;
+    }
 }
 
 template <class F>
 void for_tiles(int32_t rows, int32_t cols, int shape, F f) {
-    const int64_t h = ns_tile_rows(shape), w = ns_tile_cols(shape);
-    for (int32_t r = 0; r * h < rows; ++r)
-        for (int32_t c = 0; c * w < cols; ++c) f(r, c);
+    const int64_t t = ns_tile(shape);
+    for (int32_t r = 0; r * t < rows; ++r)
+        for (int32_t c = 0; c * t < cols; ++c) f(r, c);
 }
 
 // Fills in sizes, tiles and workspace; `matrices` has its user's fields set.
 lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
     plan->n = int32_t(matrices.size());
-    plan->shape = pick_shape(matrices, plan->split);
-    const int64_t tile_rows = ns_tile_rows(plan->shape), tile_cols = ns_tile_cols(plan->shape);
+    pick_shapes(matrices, plan->split, &plan->sym_shape, &plan->update_shape);
 
     // Longest products first, so that the last workgroups are short ones.
     std::vector<int32_t> order(matrices.size());
@@ -139,14 +163,14 @@ lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
     std::stable_sort(order.begin(), order.end(),
                      [&](int32_t p, int32_t q) { return longest(p) > longest(q); });
     for (int32_t i : order)
-        for_tiles(side(i), side(i), plan->shape, [&](int32_t r, int32_t c) {
-            if (c * tile_cols < (r + 1) * tile_rows)  // not wholly above the diagonal
+        for_tiles(side(i), side(i), plan->sym_shape, [&](int32_t r, int32_t c) {
+            if (c <= r)
                 sym.push_back(NsTile{i, r, c});
         });
     std::stable_sort(order.begin(), order.end(),
                      [&](int32_t p, int32_t q) { return side(p) > side(q); });
     for (int32_t i : order)
-        for_tiles(matrices[i].rows, matrices[i].cols, plan->shape,
+        for_tiles(matrices[i].rows, matrices[i].cols, plan->update_shape,
                   [&](int32_t r, int32_t c) { update.push_back(NsTile{i, r, c}); });
     if (sym.size() > INT32_MAX || update.size() > INT32_MAX)
         return fail(LAMB_EINVAL, "the matrices take too many tiles for one plan");
@@ -235,14 +259,14 @@ lamb_status run(lamb_ns_plan *plan, const lamb_ns_params &ns, NsStep step, uint3
                                 plan->bf16_in, plan->split, step, plan->partials, flag, stream);
     for (int32_t k = 0; k < ns.steps && err == hipSuccess; ++k) {
         const int parity = k & 1;
-        err = launch_ns_gram(plan->matrices, plan->sym_tiles, plan->n_sym, plan->shape,
+        err = launch_ns_gram(plan->matrices, plan->sym_tiles, plan->n_sym, plan->sym_shape,
                              plan->split, parity, stream);
         if (err == hipSuccess)
-            err = launch_ns_poly(plan->matrices, plan->sym_tiles, plan->n_sym, plan->shape,
+            err = launch_ns_poly(plan->matrices, plan->sym_tiles, plan->n_sym, plan->sym_shape,
                                  plan->split, step, stream);
         if (err == hipSuccess)
-            err = launch_ns_update(plan->matrices, plan->update_tiles, plan->n_update, plan->shape,
-                                   plan->split, parity, k + 1 == ns.steps, plan->kind, step, flag,
+            err = launch_ns_update(plan->matrices, plan->update_tiles, plan->n_update,
+                                   plan->update_shape, plan->split, parity, k + 1 == ns.steps, plan->kind, step, flag,
                                    stream);
     }
     if (err != hipSuccess)

@@ -44,10 +44,9 @@ struct NsTile {
     int32_t row, col;  // in tiles
 };
 
-// Tile shapes of the products, rows by columns.
+// Tile shapes of the products, all square.
 enum NsShape : int32_t { kNsTiny = 0, kNsSmall = 1, kNsLarge = 2 };
-constexpr int32_t ns_tile_rows(int32_t shape) { return 64 << shape; }
-constexpr int32_t ns_tile_cols(int32_t shape) { return shape == kNsTiny ? 64 : 128; }
+constexpr int32_t ns_tile(int32_t shape) { return 64 << shape; }
 
 enum NsKind : int32_t { kNsBf16Out = 0, kNsF32Out = 1, kNsMuon = 2 };
 

@@ -39,29 +39,16 @@ __device__ inline float from_half(uint16_t v) { return float(__builtin_bit_cast(
 // twice: near a tie the low part then belongs to another high part.
 __device__ inline void pin(float &v) { asm volatile("" : "+v"(v)); }
 
-// Four values as 16-bit floats, their low parts beside.
-template <bool SPLIT>
-__device__ inline void store_halves(uint16_t *at, int64_t low, float (&v)[4]) {
+__device__ inline ushort4 high_halves(float (&v)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) pin(v[i]);
-    ushort4 hi;
-    hi.x = to_half(v[0]), hi.y = to_half(v[1]), hi.z = to_half(v[2]), hi.w = to_half(v[3]);
-    *(ushort4 *)at = hi;
-    if (SPLIT) {
-        ushort4 lo;
-        lo.x = to_half(v[0] - from_half(hi.x)), lo.y = to_half(v[1] - from_half(hi.y));
-        lo.z = to_half(v[2] - from_half(hi.z)), lo.w = to_half(v[3] - from_half(hi.w));
-        *(ushort4 *)(at + low) = lo;
-    }
+    return make_ushort4(to_half(v[0]), to_half(v[1]), to_half(v[2]), to_half(v[3]));
 }
 
-template <bool SPLIT>
-__device__ inline void store_half(uint16_t *at, int64_t low, float v) {
-    pin(v);
-    const uint16_t hi = to_half(v);
-    *at = hi;
-    if (SPLIT)
-        at[low] = to_half(v - from_half(hi));
+// What the high parts leave.
+__device__ inline ushort4 low_halves(const float (&v)[4], ushort4 hi) {
+    return make_ushort4(to_half(v[0] - from_half(hi.x)), to_half(v[1] - from_half(hi.y)),
+                        to_half(v[2] - from_half(hi.z)), to_half(v[3] - from_half(hi.w)));
 }
 
 // Eight values of a row from column `col`, of which `n` exist; the rest are 0.
@@ -70,7 +57,7 @@ __device__ inline void load_row(const void *base, int64_t at, int n, bool vector
     if (BF16) {
         const uint16_t *p = (const uint16_t *)base + at;
         if (vector && n == 8) {
-            const uint4 w = *(const uint4 *)p;
+            const uint4 w = load_global<uint4>(p);
             const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -80,30 +67,30 @@ __device__ inline void load_row(const void *base, int64_t at, int n, bool vector
             return;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? widen(p[i]) : 0.0f;
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? widen(load_global<uint16_t>(p + i)) : 0.0f;
     } else {
         const float *p = (const float *)base + at;
         if (vector && n == 8) {
-            const float4 lo = *(const float4 *)p, hi = *(const float4 *)(p + 4);
+            const float4 lo = load_global<float4>(p), hi = load_global<float4>(p + 4);
             v[0] = lo.x, v[1] = lo.y, v[2] = lo.z, v[3] = lo.w;
             v[4] = hi.x, v[5] = hi.y, v[6] = hi.z, v[7] = hi.w;
             return;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.0f;
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? load_global<float>(p + i) : 0.0f;
     }
 }
 
 __device__ inline void store_row(float *p, int n, bool vector, const float (&v)[8]) {
     if (vector && n == 8) {
-        *(float4 *)p = make_float4(v[0], v[1], v[2], v[3]);
-        *(float4 *)(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+        store_global(p, make_float4(v[0], v[1], v[2], v[3]));
+        store_global(p + 4, make_float4(v[4], v[5], v[6], v[7]));
         return;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i)
         if (i < n)
-            p[i] = v[i];
+            store_global(p + i, v[i]);
 }
 
 // The workgroup's sum, on every thread of wave 0, in a fixed order.
@@ -230,13 +217,22 @@ __global__ __launch_bounds__(kNsBlock) void ns_convert_kernel(const NsMatrix *ma
                            : m[i];
         }
         uint16_t *x = mat.x[0] + row * mat.ld + col;
+        ushort4 hi[2], lo[2];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             float v[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) v[i] = g[4 * h + i] * to_x;
-            store_halves<SPLIT>(x + 4 * h, mat.x_low, v);
+            hi[h] = high_halves(v);
+            lo[h] = low_halves(v, hi[h]);
         }
+        auto pack = [](const ushort4 (&h)[2]) {
+            return make_uint4(h[0].x | uint32_t(h[0].y) << 16, h[0].z | uint32_t(h[0].w) << 16,
+                              h[1].x | uint32_t(h[1].y) << 16, h[1].z | uint32_t(h[1].w) << 16);
+        };
+        store_global(x, pack(hi));
+        if (SPLIT)
+            store_global(x + mat.x_low, pack(lo));
     });
 }
 
@@ -248,31 +244,37 @@ __device__ inline Operand columns_of(const uint16_t *p, int64_t ld, int64_t firs
     return Operand{(const char *)(p + first), ld * 2, int32_t(ld - first)};
 }
 
-// A symmetric result's tile, and its mirror image where that is another tile.
-template <class Shape, class F>
+// A symmetric result's tile, and its mirror image where that is another tile, in
+// `parts` 16-bit parts. acc holds the values already; rows and columns from the
+// matrix's side on are 0.
+template <class Shape>
 __device__ inline void store_symmetric(const NsMatrix &mat, uint16_t *to, const NsTile &tile,
-                                       F value) {
+                                       float4v (&acc)[Shape::MI][Shape::NI], short *lds) {
+    static_assert(Shape::BM == Shape::BN, "square tiles");
     const Place<Shape> at;
+    const TileStore<Shape::BM, Shape::BN, Shape::kThreads> store(lds);
     const int64_t ld = mat.side_ld;
+    const int m0 = tile.row * Shape::BM, n0 = tile.col * Shape::BN;
 #pragma unroll
-    for (int i = 0; i < Shape::MI; ++i) {
+    for (int part = 0; part < Shape::PARTS; ++part) {
+        uint16_t *plane = to + part * mat.gram_low;
+        auto each = [&](auto put) {
 #pragma unroll
-        for (int j = 0; j < Shape::NI; ++j) {
-            const int m = tile.row * Shape::BM + at.row + 16 * i;
-            const int n = tile.col * Shape::BN + at.col + 16 * j;
-            if (m >= ld || n >= ld)
-                continue;
-            float v[4] = {};  // columns up to ld, of the mirror image too, are 0
-            if (m < mat.side) {
-                value(i, j, m, n, v);
-                store_halves<Shape::PARTS == 2>(to + m * ld + n, mat.gram_low, v);
-            }
-            if ((tile.col + 1) * Shape::BN <= tile.row * Shape::BM) {
+            for (int i = 0; i < Shape::MI; ++i)
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
-                    if (n + r < mat.side)
-                        store_half<Shape::PARTS == 2>(to + (n + r) * ld + m, mat.gram_low, v[r]);
-            }
+                for (int j = 0; j < Shape::NI; ++j) {
+                    float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                    ushort4 h = high_halves(v);
+                    if (part)
+                        h = low_halves(v, h);
+                    put(at.row + 16 * i, at.col + 16 * j, h);
+                }
+        };
+        each([&](int m, int n, ushort4 h) { store.put(m, n, h); });
+        store.template flush<false>(plane + m0 * ld + n0, ld, mat.side - m0, mat.side_ld - n0);
+        if (tile.row != tile.col) {
+            each([&](int m, int n, ushort4 h) { store.put_mirror(m, n, h); });
+            store.template flush<true>(plane + n0 * ld + m0, ld, mat.side - n0, mat.side_ld - m0);
         }
     }
 }
@@ -298,10 +300,11 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_gram_kernel
         tile_product<HalfMath, Shape, false, false>(acc, lds, a, b, mat.cols, 2 * mat.x_low,
                                                    2 * mat.x_low);
     }
-    store_symmetric<Shape>(mat, mat.gram, tile, [&](int i, int j, int, int, float (&v)[4]) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r] * (1.0f / kNsScale);
-    });
+    for (int i = 0; i < Shape::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < Shape::NI; ++j) acc[i][j] *= 1.0f / kNsScale;
+    store_symmetric<Shape>(mat, mat.gram, tile, acc, lds);
 }
 
 template <class Shape>
@@ -316,23 +319,42 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_poly_kernel
     const Operand b = rows_of(mat.gram, mat.side_ld, int64_t(tile.col) * Shape::BN, mat.side);
     tile_product<HalfMath, Shape, false, false>(acc, lds, a, b, mat.side, 2 * mat.gram_low,
                                                    2 * mat.gram_low);
-    store_symmetric<Shape>(
-        mat, mat.poly, tile, [&](int i, int j, int m, int n, float (&v)[4]) {
-            const uint16_t *at = mat.gram + int64_t(m) * mat.side_ld + n;
-            const ushort4 hi = *(const ushort4 *)at;
-            float g[4] = {from_half(hi.x), from_half(hi.y), from_half(hi.z), from_half(hi.w)};
+    const Place<Shape> at;
+#pragma unroll
+    for (int i = 0; i < Shape::MI; ++i) {
+        const int m = tile.row * Shape::BM + at.row + 16 * i;
+        // a row's loads go out together: from inside the matrix, wherever they are used
+        ushort4 part[Shape::PARTS][Shape::NI];
+#pragma unroll
+        for (int j = 0; j < Shape::NI; ++j) {
+            const int n = tile.col * Shape::BN + at.col + 16 * j;
+            const uint16_t *from = mat.gram + int64_t(m < mat.side ? m : mat.side - 1) * mat.side_ld +
+                                   (n < mat.side_ld ? n : mat.side_ld - 4);
+#pragma unroll
+            for (int p = 0; p < Shape::PARTS; ++p)
+                part[p][j] = load_global<ushort4>(from + p * mat.gram_low);
+        }
+#pragma unroll
+        for (int j = 0; j < Shape::NI; ++j) {
+            const int n = tile.col * Shape::BN + at.col + 16 * j;
+            float g[4] = {from_half(part[0][j].x), from_half(part[0][j].y),
+                          from_half(part[0][j].z), from_half(part[0][j].w)};
             if (Shape::PARTS == 2) {
-                const ushort4 lo = *(const ushort4 *)(at + mat.gram_low);
+                const ushort4 lo = part[Shape::PARTS - 1][j];
                 g[0] += from_half(lo.x), g[1] += from_half(lo.y);
                 g[2] += from_half(lo.z), g[3] += from_half(lo.w);
             }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                v[r] = __builtin_fmaf(step.b, g[r], step.c * (acc[i][j][r] * (1.0f / kNsScale)));
+                float v = __builtin_fmaf(step.b, g[r], step.c * (acc[i][j][r] * (1.0f / kNsScale)));
                 if (m == n + r)
-                    v[r] = __builtin_fmaf(step.a, kNsScale, v[r]);
+                    v = __builtin_fmaf(step.a, kNsScale, v);
+                // rows and columns from `side` on are 0
+                acc[i][j][r] = m < mat.side && n + r < mat.side ? v : 0.0f;
             }
-        });
+        }
+    }
+    store_symmetric<Shape>(mat, mat.poly, tile, acc, lds);
 }
 
 __device__ inline float update_scale(const NsMatrix &mat, int32_t kind) {
@@ -368,6 +390,39 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_update_kern
                                                    2 * mat.x_low);
     }
     const Place<Shape> at;
+    constexpr float kBack = KIND < 0 ? 1.0f / kNsScale : 1.0f / (kNsScale * kNsScale);
+#pragma unroll
+    for (int i = 0; i < Shape::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < Shape::NI; ++j) acc[i][j] *= kBack;
+    if (KIND < 0 || (KIND == kNsBf16Out && mat.vector && mat.cols % 8 == 0)) {
+        const TileStore<Shape::BM, Shape::BN, Shape::kThreads> store(lds);
+        uint16_t *to = KIND < 0 ? (parity ? mat.x[0] : mat.x[1]) : (uint16_t *)mat.out;
+        const int64_t ld = KIND < 0 ? int64_t(mat.ld) : mat.out_stride;
+        uint16_t *out = to + m0 * ld + n0;
+#pragma unroll
+        for (int part = 0; part < (KIND < 0 ? Shape::PARTS : 1); ++part) {
+#pragma unroll
+            for (int i = 0; i < Shape::MI; ++i)
+#pragma unroll
+                for (int j = 0; j < Shape::NI; ++j) {
+                    float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+                    ushort4 h;
+                    if (KIND < 0) {
+                        h = high_halves(v);
+                        if (part)
+                            h = low_halves(v, h);
+                    } else {
+                        h = make_ushort4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]),
+                                         to_bf16(v[3]));
+                    }
+                    store.put(at.row + 16 * i, at.col + 16 * j, h);
+                }
+            store.template flush<false>(out + part * mat.x_low, ld, int(mat.rows - m0),
+                                        int((KIND < 0 ? mat.ld : mat.cols) - n0));
+        }
+        return;
+    }
     const float move = KIND == kNsMuon ? -step.lr * update_scale(mat, step.scale) : 0.0f;
     const float keep = KIND == kNsMuon && mat.wd ? step.decay : 1.0f;
 #pragma unroll
@@ -376,48 +431,38 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_update_kern
         for (int j = 0; j < Shape::NI; ++j) {
             const int64_t m = m0 + at.row + 16 * i;
             const int n = int(n0) + at.col + 16 * j;
-            if (m >= mat.rows || n >= (KIND < 0 ? mat.ld : mat.cols))
+            if (m >= mat.rows || n >= mat.cols)
                 continue;
-            float v[4];
-            constexpr float kBack = KIND < 0 ? 1.0f / kNsScale : 1.0f / (kNsScale * kNsScale);
-#pragma unroll
-            for (int r = 0; r < 4; ++r) v[r] = acc[i][j][r] * kBack;
-            if (KIND < 0) {
-                store_halves<Shape::PARTS == 2>((parity ? mat.x[0] : mat.x[1]) + m * mat.ld + n, mat.x_low, v);
-            } else if (KIND == kNsBf16Out) {
+            float v[4] = {acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]};
+            const bool whole = mat.vector && n + 4 <= mat.cols;
+            if (KIND == kNsBf16Out) {
                 uint16_t *out = (uint16_t *)mat.out + m * mat.out_stride + n;
-                if (mat.vector && n + 4 <= mat.cols) {
-                    *(ushort4 *)out = make_ushort4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]),
-                                                   to_bf16(v[3]));
-                } else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (n + r < mat.cols)
-                            out[r] = to_bf16(v[r]);
-                }
-            } else {
-                float *out = (float *)mat.out + m * mat.out_stride + n;
-                const bool whole = mat.vector && n + 4 <= mat.cols;
-                if (KIND == kNsMuon) {
-                    float xs[4] = {};
-                    if (whole) {
-                        const float4 t = *(const float4 *)out;
-                        xs[0] = t.x, xs[1] = t.y, xs[2] = t.z, xs[3] = t.w;
-                    } else {
-#pragma unroll
-                        for (int r = 0; r < 4; ++r) xs[r] = n + r < mat.cols ? out[r] : 0.0f;
-                    }
-#pragma unroll
-                    for (int r = 0; r < 4; ++r) v[r] = __builtin_fmaf(move, v[r], keep * xs[r]);
-                }
+                for (int r = 0; r < 4; ++r)
+                    if (n + r < mat.cols)
+                        store_global(out + r, to_bf16(v[r]));
+                continue;
+            }
+            float *out = (float *)mat.out + m * mat.out_stride + n;
+            if (KIND == kNsMuon) {
+                float xs[4] = {};
                 if (whole) {
-                    *(float4 *)out = make_float4(v[0], v[1], v[2], v[3]);
+                    const float4 t = load_global<float4>(out);
+                    xs[0] = t.x, xs[1] = t.y, xs[2] = t.z, xs[3] = t.w;
                 } else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r)
-                        if (n + r < mat.cols)
-                            out[r] = v[r];
+                    for (int r = 0; r < 4; ++r) xs[r] = n + r < mat.cols ? load_global<float>(out + r) : 0.0f;
                 }
+#pragma unroll
+                for (int r = 0; r < 4; ++r) v[r] = __builtin_fmaf(move, v[r], keep * xs[r]);
+            }
+            if (whole) {
+                store_global(out, make_float4(v[0], v[1], v[2], v[3]));
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (n + r < mat.cols)
+                        store_global(out + r, v[r]);
             }
         }
     }
@@ -425,10 +470,11 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_update_kern
 
 // The shapes of launch_ns_*: see the table in ortho_internal.h.
 using Tiny = TileShape<64, 64, 2, 2, 64, 4, 1>;
-using Small = TileShape<128, 128, 2, 2, 32, 4, 1>;
-using Large = TileShape<256, 128, 2, 2, 32, 3, 1>;
+using Small = TileShape<128, 128, 2, 4, 32, 4, 1>;
+using Large = TileShape<256, 256, 2, 4, 32, 4, 1>;
 using TinySplit = TileShape<64, 64, 2, 2, 32, 4, 2>;
-using SmallSplit = TileShape<128, 128, 2, 2, 32, 2, 2>;
+using SmallSplit = TileShape<128, 128, 2, 4, 32, 4, 2>;
+using LargeSplit = TileShape<256, 256, 2, 4, 32, 2, 2>;
 
 }  // namespace
 
@@ -474,6 +520,7 @@ hipError_t with_shape(int shape, bool split, F f) {
     case kNsLarge: f(Large{}); break;
     case 8 + kNsTiny: f(TinySplit{}); break;
     case 8 + kNsSmall: f(SmallSplit{}); break;
+    case 8 + kNsLarge: f(LargeSplit{}); break;
     default: return hipErrorInvalidValue;
     }
     return hipGetLastError();

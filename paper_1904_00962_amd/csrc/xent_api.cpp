@@ -14,7 +14,6 @@ constexpr int64_t kMaxReadStride = int64_t(1) << 21;  // a tile's rows within 32
 // the 256 MiB last-level cache.
 constexpr int64_t kPieceBytes = int64_t(128) << 20;
 constexpr int64_t kPieceAlign = 256;
-constexpr int64_t kFill = 512;  // workgroups that fill the device (two on each CU)
 
 lamb_status check(const lamb_xent *x) {
     if (!x)
@@ -44,18 +43,37 @@ bool in_place(const void *p, int64_t stride, int64_t dim) {
 }
 
 int64_t count_tiles(int64_t rows, int64_t cols, int shape) {
-    return round_up(rows, xent_rows(shape)) / xent_rows(shape) *
-           (round_up(cols, xent_cols(shape)) / xent_cols(shape));
+    const int64_t t = xent_tile(shape);
+    return (rows + t - 1) / t * ((cols + t - 1) / t);
 }
 
-// The largest tiles that fill the device and whose last row of tiles wastes at most
-// half of the work.
-int pick_shape(int64_t rows, int64_t cols) {
-    for (int shape = kXentLarge; shape > kXentTiny; --shape)
-        if (count_tiles(rows, cols, shape) >= kFill &&
-            2 * round_up(rows, xent_rows(shape)) <= 3 * round_up(rows, 64))
-            return shape;
-    return kXentTiny;
+// The tile shape of a product of `rows` x `cols` over `depth`, and the parts that
+// `depth` is cut in (at most `most`), by the least estimated time: rounds of workgroups
+// over the CUs times a tile's time. Microseconds, measured on one GPU: a tile's fixed
+// part, and per 1024 of depth with its CU to itself (which two of the smaller tiles
+// share at no cost).
+int pick_shape(int64_t rows, int64_t cols, int64_t depth, int64_t most, int32_t *splits) {
+    constexpr double kFixed[3] = {2.0, 4.0, 8.0}, kDeep[3] = {4.5, 12.0, 22.0};
+    constexpr int64_t kSlots[3] = {512, 512, 256};
+    int best = 0;
+    double least = 1e300;
+    for (int shape = kXentTiny; shape <= kXentLarge; ++shape) {
+        const int64_t tiles = std::max<int64_t>(1, count_tiles(rows, cols, shape));
+        for (int64_t parts = 1; parts <= most; parts *= 2) {
+            const int64_t rounds = (tiles * parts + kSlots[shape] - 1) / kSlots[shape];
+            // a part more writes and reads rows x cols of fp32 once more
+            const double time = double(rounds) * (kFixed[shape] + double(depth) / double(parts) /
+                                                                      1024.0 * kDeep[shape]) +
+                                double(parts - 1) * double(rows) * double(cols) * 8.0 / 5e6;
+            if (time < least) {
+                least = time;
+                best = shape;
+                if (splits)
+                    *splits = int32_t(parts);
+            }
+        }
+    }
+    return best;
 }
 
 struct Layout {
@@ -85,9 +103,9 @@ Layout layout_of(const lamb_xent &x) {
     l.packed = take(2 * x.tokens * l.ld);
     l.table = take(l.copy_table ? 2 * x.vocab * l.ld : 0);
     const size_t common = at;
-    l.logits_shape = pick_shape(x.tokens, x.vocab);
-    l.parts = int32_t(round_up(x.vocab, xent_cols(l.logits_shape)) / xent_cols(l.logits_shape)) *
-              kXentColumnWaves;
+    l.logits_shape = pick_shape(x.tokens, x.vocab, x.dim, 1, nullptr);
+    const int32_t tile = xent_tile(l.logits_shape);
+    l.parts = int32_t((x.vocab + tile - 1) / tile) * xent_column_waves(tile);
     l.parts_at = take(int64_t(l.parts) * x.tokens * 8);
     l.at_target = take(4 * x.tokens);
     l.forward = at;
@@ -97,13 +115,11 @@ Layout layout_of(const lamb_xent &x) {
     const int64_t most = std::max<int64_t>(kPieceAlign, kPieceBytes / 2 / rows);
     const int64_t pieces = (x.vocab + most - 1) / most;
     l.piece = std::min(round_up((x.vocab + pieces - 1) / pieces, kPieceAlign), round_up(x.vocab, 8));
-    l.probs_shape = pick_shape(x.tokens, l.piece);
-    l.table_shape = pick_shape(l.piece, x.dim);
-    l.hidden_shape = pick_shape(x.tokens, x.dim);
-    // few rows: the piece's columns are split over workgroups, 512 each at least
-    const int64_t tiles = std::max<int64_t>(1, count_tiles(x.tokens, x.dim, l.hidden_shape));
-    l.splits = int32_t(std::max<int64_t>(
-        1, std::min((kFill + tiles - 1) / tiles, l.piece / 512)));
+    l.probs_shape = pick_shape(x.tokens, l.piece, x.dim, 1, nullptr);
+    l.table_shape = pick_shape(l.piece, x.dim, x.tokens, 1, nullptr);
+    // few rows: the piece's columns are split over workgroups, 256 each at least
+    l.hidden_shape = pick_shape(x.tokens, x.dim, l.piece, std::max<int64_t>(1, l.piece / 256),
+                                &l.splits);
     l.probs = take(2 * x.tokens * l.piece);
     l.partial = take(int64_t(l.splits) * x.tokens * l.ld * 4);
     l.backward = at;

@@ -8,13 +8,12 @@
 
 namespace lamb_mi355x {
 
-// Tile shapes, rows by columns.
+// Tile shapes, all square, and the waves across a tile's columns.
 enum XentShape : int32_t { kXentTiny = 0, kXentSmall = 1, kXentLarge = 2 };
-constexpr int32_t xent_rows(int32_t shape) { return 64 << shape; }
-constexpr int32_t xent_cols(int32_t shape) { return shape == kXentTiny ? 64 : 128; }
-constexpr int32_t kXentColumnWaves = 2;  // waves across a tile's columns, in every shape
+constexpr int32_t xent_tile(int32_t shape) { return 64 << shape; }
+constexpr int32_t xent_column_waves(int32_t tile) { return tile == 64 ? 2 : 4; }
 
-constexpr int kPackTokens = 64;   // tokens per workgroup of the packing pass
+constexpr int kPackTokens = 16;    // tokens per workgroup of the packing pass
 constexpr int kReduceTokens = 16;  // tokens per workgroup of the logsumexp pass
 
 // What every pass of a call reads. `hidden` is the packed copy of the tokens that

@@ -32,8 +32,8 @@ constexpr int kXcdCount = 8;
 constexpr int kGroupRows = 8;  // tile rows that are worked on together
 
 using Tiny = TileShape<64, 64, 2, 2, 64, 4, 1>;
-using Small = TileShape<128, 128, 2, 2, 32, 4, 1>;
-using Large = TileShape<256, 128, 2, 2, 32, 3, 1>;
+using Small = TileShape<128, 128, 2, 4, 32, 4, 1>;
+using Large = TileShape<256, 256, 2, 4, 32, 4, 1>;
 
 __device__ inline uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, __bf16(v)); }
 __device__ inline float widen(uint16_t v) { return __uint_as_float(uint32_t(v) << 16); }
@@ -98,14 +98,15 @@ __global__ __launch_bounds__(256) void xent_pack_kernel(XentPack a) {
         int32_t base = before[0] + before[1] + before[2] + before[3];
         const int64_t i = first + lane;
         const int64_t t = i < a.tokens ? target_of(a, i) : a.ignore;
-        const bool counts = t != a.ignore;
+        const bool counts = lane < kPackTokens && t != a.ignore;
         const uint64_t mask = __ballot(counts);
         const int32_t row = base + __popcll(mask & ((uint64_t(1) << lane) - 1));
-        row_of[lane] = counts ? row : -1;
+        if (lane < kPackTokens)
+            row_of[lane] = counts ? row : -1;
         if (counts) {
             a.source[row] = int32_t(i);
             a.target[row] = t >= 0 && t < a.vocab ? int32_t(t) : -1;
-        } else if (i < a.tokens && a.loss) {
+        } else if (lane < kPackTokens && i < a.tokens && a.loss) {
             a.loss[i] = 0.0f;
             a.lse[i] = 0.0f;
         }
@@ -433,8 +434,8 @@ hipError_t with_shape(int shape, F f) {
 }
 
 int64_t tiles(int64_t rows, int64_t cols, int shape) {
-    const int64_t h = xent_rows(shape), w = xent_cols(shape);
-    return (rows + h - 1) / h * ((cols + w - 1) / w);
+    const int64_t t = xent_tile(shape);
+    return (rows + t - 1) / t * ((cols + t - 1) / t);
 }
 
 }  // namespace
@@ -456,7 +457,7 @@ hipError_t launch_xent_logits(const XentArgs &args, int shape, float2 *parts, fl
                               hipStream_t stream) {
     return with_shape(shape, [&](auto s) {
         using Shape = decltype(s);
-        static_assert(Shape::WN == kXentColumnWaves, "parts per tile");
+        static_assert(Shape::WN == xent_column_waves(Shape::BN), "parts per tile");
         xent_logits_kernel<Shape>
             <<<uint32_t(tiles(args.tokens, args.vocab, shape)), Shape::kThreads, 0, stream>>>(
                 args, parts, at_target);
