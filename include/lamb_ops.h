@@ -170,7 +170,7 @@ typedef struct lamb_xent {
 
 /* Bytes of device workspace (256-byte aligned) that a forward and a backward call need;
  * host only. The backward holds a piece of the vocabulary's softmax, at most about
- * 128 MiB, beside the hidden states and their gradient in fp32. */
+ * 160 MiB, beside the hidden states and their gradient in fp32. */
 LAMB_API lamb_status lamb_xent_workspace(const lamb_xent *xent, size_t *forward_bytes,
                                          size_t *backward_bytes);
 

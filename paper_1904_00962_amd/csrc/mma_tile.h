@@ -104,7 +104,8 @@ struct TileShape {
     static constexpr int kStage = (kA + kB) * PARTS;
     static constexpr int kLds = kStage * STAGES;
     static constexpr int kLoads = kStage / 8 / kThreads;  // a lane's loads per stage
-    static constexpr bool kAlternating = kWaves == 8;
+    // small tiles have too few matrix instructions a phase to pay for its meetings
+    static constexpr bool kAlternating = BM == 256;
     // workgroups per CU: what LDS allows, and at most two
     static constexpr int kPerCu = 160 * 1024 / (kLds * 2) >= 2 ? 2 : 1;
     static_assert(DEPTH % 32 == 0 && STAGES >= 2 && kLds * 2 <= 160 * 1024 && kLoads * (STAGES - 2) < 64, "");
@@ -257,11 +258,13 @@ __device__ inline void phase() {
 // waves 0..3 and 4..7 are a phase apart, so that of the two waves on a SIMD one reads
 // fragments while the other's matrix instructions run: read(stage, part) and
 // compute(part), for the PARTS parts of a stage. A stage's place is loaded again once
-// the later half has read it, one phase after the earlier half.
+// the later half has read it, one phase after the earlier half. (Sent out
+// beside the matrix instructions instead of the reads, the loads cost 7%.)
 template <class Shape, int PARTS, class Issue, class Read, class Compute>
 __device__ inline void run_alternating(int32_t count, const short *lds, int wave, Issue issue,
                                        Read read, Compute compute) {
     static_assert(Shape::kWaves == 8, "two waves on each SIMD");
+    constexpr int kAny = Shape::STAGES * Shape::kLoads;
     constexpr int kOpen = (Shape::STAGES - 2) * Shape::kLoads;
 #pragma unroll
     for (int s = 0; s < Shape::STAGES - 1; ++s) issue(lds + s * Shape::kStage);
@@ -284,17 +287,17 @@ __device__ inline void run_alternating(int32_t count, const short *lds, int wave
             if (part + 1 == PARTS)
                 phase<kOpen>();
             else
-                phase<kOpen + Shape::kLoads>();
+                phase<kAny>();
             __builtin_amdgcn_s_setprio(1);
             compute(part);
             __builtin_amdgcn_s_setprio(0);
-            phase<kOpen + Shape::kLoads>();
+            phase<kAny>();
         }
         reads = next(reads);
         writes = next(writes);
     }
     if (wave < 4)
-        phase<kOpen + Shape::kLoads>();
+        phase<kAny>();
     meet<0>();
 }
 

@@ -81,8 +81,8 @@ lamb_status check_params(const lamb_ns_params &p) {
 struct TileCost {
     double fixed, alone, full;
 };
-constexpr TileCost kCost[2][3] = {{{2.0, 3.7, 3.0}, {4.0, 8.6, 7.5}, {8.0, 17.5, 24.5}},
-                                  {{2.5, 8.5, 7.9}, {6.0, 19.8, 20.0}, {18.0, 58.0, 77.0}}};
+constexpr TileCost kCost[2][3] = {{{2.0, 3.7, 4.2}, {4.0, 8.6, 9.0}, {15.0, 17.5, 23.0}},
+                                  {{2.5, 8.5, 8.5}, {3.5, 19.8, 24.5}, {18.0, 58.0, 77.0}}};
 constexpr double kCus = 256.0;
 
 struct Estimate {

@@ -470,10 +470,10 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_update_kern
 
 // The shapes of launch_ns_*: see the table in ortho_internal.h.
 using Tiny = TileShape<64, 64, 2, 2, 64, 4, 1>;
-using Small = TileShape<128, 128, 2, 4, 32, 4, 1>;
+using Small = TileShape<128, 128, 2, 2, 32, 4, 1>;
 using Large = TileShape<256, 256, 2, 4, 32, 4, 1>;
 using TinySplit = TileShape<64, 64, 2, 2, 32, 4, 2>;
-using SmallSplit = TileShape<128, 128, 2, 4, 32, 4, 2>;
+using SmallSplit = TileShape<128, 128, 2, 2, 32, 2, 2>;
 using LargeSplit = TileShape<256, 256, 2, 4, 32, 2, 2>;
 
 }  // namespace

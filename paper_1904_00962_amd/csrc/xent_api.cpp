@@ -12,7 +12,7 @@ namespace {
 constexpr int64_t kMaxReadStride = int64_t(1) << 21;  // a tile's rows within 32-bit offsets
 // A piece of the vocabulary's softmax: written once and read twice, so kept within
 // the 256 MiB last-level cache.
-constexpr int64_t kPieceBytes = int64_t(128) << 20;
+constexpr int64_t kPieceBytes = int64_t(160) << 20;
 constexpr int64_t kPieceAlign = 256;
 
 lamb_status check(const lamb_xent *x) {
@@ -47,30 +47,31 @@ int64_t count_tiles(int64_t rows, int64_t cols, int shape) {
     return (rows + t - 1) / t * ((cols + t - 1) / t);
 }
 
-// The tile shape of a product of `rows` x `cols` over `depth`, and the parts that
-// `depth` is cut in (at most `most`), by the least estimated time: rounds of workgroups
+// The tile shape of a product of `rows` x `cols` over `depth`, the parts that `depth`
+// is cut in (at most `most`), and the time, by the least estimate: rounds of workgroups
 // over the CUs times a tile's time. Microseconds, measured on one GPU: a tile's fixed
-// part, and per 1024 of depth with its CU to itself (which two of the smaller tiles
-// share at no cost).
-int pick_shape(int64_t rows, int64_t cols, int64_t depth, int64_t most, int32_t *splits) {
-    constexpr double kFixed[3] = {2.0, 4.0, 8.0}, kDeep[3] = {4.5, 12.0, 22.0};
+// part, and per 1024 of depth where all CUs work (two of the smaller tiles share one).
+struct Product {
+    int shape = 0;
+    int32_t parts = 1;
+    double time = 1e300;
+};
+
+Product pick(int64_t rows, int64_t cols, int64_t depth, int64_t most) {
+    constexpr double kFixed[3] = {2.0, 4.0, 15.0}, kDeep[3] = {8.4, 18.0, 23.0};
     constexpr int64_t kSlots[3] = {512, 512, 256};
-    int best = 0;
-    double least = 1e300;
+    constexpr double kBytesPerUs = 5e6;
+    Product best;
     for (int shape = kXentTiny; shape <= kXentLarge; ++shape) {
         const int64_t tiles = std::max<int64_t>(1, count_tiles(rows, cols, shape));
-        for (int64_t parts = 1; parts <= most; parts *= 2) {
+        for (int64_t parts = 1; parts <= std::min<int64_t>(most, 32); ++parts) {
             const int64_t rounds = (tiles * parts + kSlots[shape] - 1) / kSlots[shape];
             // a part more writes and reads rows x cols of fp32 once more
             const double time = double(rounds) * (kFixed[shape] + double(depth) / double(parts) /
                                                                       1024.0 * kDeep[shape]) +
-                                double(parts - 1) * double(rows) * double(cols) * 8.0 / 5e6;
-            if (time < least) {
-                least = time;
-                best = shape;
-                if (splits)
-                    *splits = int32_t(parts);
-            }
+                                double(parts - 1) * double(rows) * double(cols) * 8.0 / kBytesPerUs;
+            if (time < best.time)
+                best = Product{shape, int32_t(parts), time};
         }
     }
     return best;
@@ -103,23 +104,37 @@ Layout layout_of(const lamb_xent &x) {
     l.packed = take(2 * x.tokens * l.ld);
     l.table = take(l.copy_table ? 2 * x.vocab * l.ld : 0);
     const size_t common = at;
-    l.logits_shape = pick_shape(x.tokens, x.vocab, x.dim, 1, nullptr);
+    l.logits_shape = pick(x.tokens, x.vocab, x.dim, 1).shape;
     const int32_t tile = xent_tile(l.logits_shape);
-    l.parts = int32_t((x.vocab + tile - 1) / tile) * xent_column_waves(tile);
+    l.parts = int32_t((x.vocab + tile - 1) / tile);
     l.parts_at = take(int64_t(l.parts) * x.tokens * 8);
     l.at_target = take(4 * x.tokens);
     l.forward = at;
     at = common;
-    // equal pieces, whole multiples of a tile
+    // equal pieces of at most kPieceBytes: of the next few counts, the one whose products
+    // fill their last rounds of workgroups best
     const int64_t rows = x.tokens ? x.tokens : 1;
     const int64_t most = std::max<int64_t>(kPieceAlign, kPieceBytes / 2 / rows);
-    const int64_t pieces = (x.vocab + most - 1) / most;
-    l.piece = std::min(round_up((x.vocab + pieces - 1) / pieces, kPieceAlign), round_up(x.vocab, 8));
-    l.probs_shape = pick_shape(x.tokens, l.piece, x.dim, 1, nullptr);
-    l.table_shape = pick_shape(l.piece, x.dim, x.tokens, 1, nullptr);
-    // few rows: the piece's columns are split over workgroups, 256 each at least
-    l.hidden_shape = pick_shape(x.tokens, x.dim, l.piece, std::max<int64_t>(1, l.piece / 256),
-                                &l.splits);
+    const int64_t least = (x.vocab + most - 1) / most;
+    double best = 1e300;
+    for (int64_t pieces = least; pieces < least + 4; ++pieces) {
+        const int64_t size = std::min(round_up((x.vocab + pieces - 1) / pieces, kPieceAlign),
+                                      round_up(x.vocab, 8));
+        const Product probs = pick(x.tokens, size, x.dim, 1);
+        const Product table = pick(size, x.dim, x.tokens, 1);
+        // few rows: the piece's columns are split over workgroups, 256 each at least
+        const Product hidden = pick(x.tokens, x.dim, size, std::max<int64_t>(1, size / 256));
+        const double time = double((x.vocab + size - 1) / size) *
+                            (probs.time + table.time + hidden.time);
+        if (time < best) {
+            best = time;
+            l.piece = size;
+            l.probs_shape = probs.shape;
+            l.table_shape = table.shape;
+            l.hidden_shape = hidden.shape;
+            l.splits = hidden.parts;
+        }
+    }
     l.probs = take(2 * x.tokens * l.piece);
     l.partial = take(int64_t(l.splits) * x.tokens * l.ld * 4);
     l.backward = at;

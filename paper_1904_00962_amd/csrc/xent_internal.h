@@ -8,10 +8,9 @@
 
 namespace lamb_mi355x {
 
-// Tile shapes, all square, and the waves across a tile's columns.
+// Tile shapes, all square.
 enum XentShape : int32_t { kXentTiny = 0, kXentSmall = 1, kXentLarge = 2 };
 constexpr int32_t xent_tile(int32_t shape) { return 64 << shape; }
-constexpr int32_t xent_column_waves(int32_t tile) { return tile == 64 ? 2 : 4; }
 
 constexpr int kPackTokens = 16;    // tokens per workgroup of the packing pass
 constexpr int kReduceTokens = 16;  // tokens per workgroup of the logsumexp pass
@@ -49,8 +48,8 @@ hipError_t launch_xent_pack(const XentPack &args, hipStream_t stream);
 // dst[r][0 .. ld) = src[r][0 .. dim) and zeros, `rows` rows.
 hipError_t launch_xent_copy(const uint16_t *src, int64_t stride, uint16_t *dst, int32_t dim,
                             int32_t ld, int64_t rows, hipStream_t stream);
-// Logits of all of the vocabulary, tile by tile: each tile column's wave halves'
-// maximum and sum of exponentials, parts[part][token], and the targets' logits.
+// Logits of all of the vocabulary, tile by tile: each tile column's maxima and sums of
+// exponentials, parts[column][token], and the targets' logits.
 hipError_t launch_xent_logits(const XentArgs &args, int shape, float2 *parts, float *at_target,
                               hipStream_t stream);
 hipError_t launch_xent_reduce(const XentArgs &args, int32_t n_parts, const float2 *parts,

@@ -32,7 +32,7 @@ constexpr int kXcdCount = 8;
 constexpr int kGroupRows = 8;  // tile rows that are worked on together
 
 using Tiny = TileShape<64, 64, 2, 2, 64, 4, 1>;
-using Small = TileShape<128, 128, 2, 4, 32, 4, 1>;
+using Small = TileShape<128, 128, 2, 2, 32, 4, 1>;
 using Large = TileShape<256, 256, 2, 4, 32, 4, 1>;
 
 __device__ inline uint16_t to_bf16(float v) { return __builtin_bit_cast(uint16_t, __bf16(v)); }
@@ -88,6 +88,7 @@ __global__ __launch_bounds__(256) void xent_pack_kernel(XentPack a) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t first = int64_t(blockIdx.x) * kPackTokens;
     int32_t count = 0;
+#pragma unroll 8
     for (int64_t i = threadIdx.x; i < first; i += 256) count += target_of(a, i) != a.ignore;
 #pragma unroll
     for (int d = 32; d; d >>= 1) count += __shfl_xor(count, d);
@@ -140,6 +141,14 @@ __device__ inline void logits_tile(float4v (&acc)[Shape::MI][Shape::NI], const s
                                                 rows_at(a.table, a.table_ld, n0, a.vocab), a.dim);
 }
 
+// Joins two (maximum, sum of exponentials from it).
+__device__ inline float2 join(float2 p, float2 q) {
+    const float top = fmaxf(p.x, q.x);
+    const float from = top == -INFINITY ? 0.0f : top;
+    return make_float2(top, p.y * __builtin_amdgcn_exp2f((p.x - from) * kLog2e) +
+                                q.y * __builtin_amdgcn_exp2f((q.x - from) * kLog2e));
+}
+
 template <class Shape>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_logits_kernel(
     XentArgs a, float2 *parts, float *at_target) {
@@ -152,8 +161,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_logits_ke
     float4v acc[Shape::MI][Shape::NI] = {};
     logits_tile<Shape>(acc, lds, a, m0, n0, kept);
     const Place<Shape> at;
-    const int lane = threadIdx.x & 63;
-    const int part = tile.col * Shape::WN + (threadIdx.x >> 6) % Shape::WN;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float2 *row_parts = (float2 *)lds;  // [BM][WN]
 #pragma unroll
     for (int i = 0; i < Shape::MI; ++i) {
         const int m = m0 + at.row + 16 * i;
@@ -172,7 +181,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_logits_ke
             }
         top = fmaxf(top, __shfl_xor(top, 16));
         top = fmaxf(top, __shfl_xor(top, 32));
-        // no column of this half exists, or all are -inf: any finite offset will do
+        // no column of this wave exists, or all are -inf: any finite offset will do
         const float from = top == -INFINITY ? 0.0f : top;
         float sum = 0.0f;
 #pragma unroll
@@ -185,17 +194,15 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_logits_ke
             }
         sum += __shfl_xor(sum, 16);
         sum += __shfl_xor(sum, 32);
-        if (lane < 16 && m < kept)
-            parts[int64_t(part) * a.tokens + m] = make_float2(top, sum);
+        if (lane < 16)
+            row_parts[(at.row + 16 * i) * Shape::WN + wave % Shape::WN] = make_float2(top, sum);
     }
-}
-
-// Joins two (maximum, sum of exponentials from it).
-__device__ inline float2 join(float2 p, float2 q) {
-    const float top = fmaxf(p.x, q.x);
-    const float from = top == -INFINITY ? 0.0f : top;
-    return make_float2(top, p.y * __builtin_amdgcn_exp2f((p.x - from) * kLog2e) +
-                                q.y * __builtin_amdgcn_exp2f((q.x - from) * kLog2e));
+    __syncthreads();
+    for (int t = threadIdx.x; t < Shape::BM && m0 + t < kept; t += Shape::kThreads) {
+        float2 sum = row_parts[t * Shape::WN];
+        for (int w = 1; w < Shape::WN; ++w) sum = join(sum, row_parts[t * Shape::WN + w]);
+        parts[int64_t(tile.col) * a.tokens + m0 + t] = sum;
+    }
 }
 
 // kReduceTokens tokens by 16 threads each, joined in a fixed order.
@@ -457,7 +464,6 @@ hipError_t launch_xent_logits(const XentArgs &args, int shape, float2 *parts, fl
                               hipStream_t stream) {
     return with_shape(shape, [&](auto s) {
         using Shape = decltype(s);
-        static_assert(Shape::WN == xent_column_waves(Shape::BN), "parts per tile");
         xent_logits_kernel<Shape>
             <<<uint32_t(tiles(args.tokens, args.vocab, shape)), Shape::kThreads, 0, stream>>>(
                 args, parts, at_target);
