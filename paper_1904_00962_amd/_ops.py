@@ -187,33 +187,30 @@ def lamb_muon_step(plan: NsPlan, hp: lamb_muon_hparams, stream: int = 0,
                                  _vp(nonfinite_out)), "lamb_muon_step")
 
 
-def lamb_xent_workspace(xent: lamb_xent) -> Tuple[int, int]:
-    """Bytes that a forward and a backward call need."""
-    a, b = ctypes.c_size_t(), ctypes.c_size_t()
-    _check(load().lamb_xent_workspace(ctypes.byref(xent), ctypes.byref(a), ctypes.byref(b)),
-           "lamb_xent_workspace")
-    return a.value, b.value
+def lamb_xent_workspace(xent: lamb_xent, backward: bool) -> int:
+    """Bytes that a forward or a backward call needs."""
+    n = ctypes.c_size_t()
+    to = (None, ctypes.byref(n)) if backward else (ctypes.byref(n), None)
+    _check(load().lamb_xent_workspace(ctypes.byref(xent), *to), "lamb_xent_workspace")
+    return n.value
 
 
 def lamb_xent_forward(xent: lamb_xent, loss: int, lse: int, mean: int, workspace: int,
                       workspace_bytes: int, stream: int = 0) -> None:
-    _check(load().lamb_xent_forward(ctypes.byref(xent), _vp(loss), _vp(lse), _vp(mean),
-                                    _vp(workspace), workspace_bytes, _vp(stream)),
-           "lamb_xent_forward")
+    _check(load().lamb_xent_forward(ctypes.byref(xent), loss, lse, mean, workspace,
+                                    workspace_bytes, stream), "lamb_xent_forward")
 
 
 def lamb_xent_backward(xent: lamb_xent, lse: int, grads: lamb_xent_grads, workspace: int,
                        workspace_bytes: int, stream: int = 0) -> None:
-    _check(load().lamb_xent_backward(ctypes.byref(xent), _vp(lse), ctypes.byref(grads),
-                                     _vp(workspace), workspace_bytes, _vp(stream)),
-           "lamb_xent_backward")
+    _check(load().lamb_xent_backward(ctypes.byref(xent), lse, ctypes.byref(grads), workspace,
+                                     workspace_bytes, stream), "lamb_xent_backward")
 
 
 def lamb_embed_forward(embed: lamb_embed, table: int, table_stride: int, table_dtype: int, out: int,
                        out_stride: int, out_dtype: int, stream: int = 0) -> None:
-    _check(load().lamb_embed_forward(ctypes.byref(embed), _vp(table), table_stride, table_dtype,
-                                     _vp(out), out_stride, out_dtype, _vp(stream)),
-           "lamb_embed_forward")
+    _check(load().lamb_embed_forward(ctypes.byref(embed), table, table_stride, table_dtype, out,
+                                     out_stride, out_dtype, stream), "lamb_embed_forward")
 
 
 def lamb_embed_workspace(embed: lamb_embed) -> int:
@@ -227,7 +224,7 @@ def lamb_embed_backward(embed: lamb_embed, grad_out: int, grad_out_stride: int,
                         grad_out_dtype: int, grad_table: int, grad_table_stride: int,
                         grad_table_dtype: int, padding_id: int, add: int, workspace: int,
                         workspace_bytes: int, stream: int = 0) -> None:
-    _check(load().lamb_embed_backward(ctypes.byref(embed), _vp(grad_out), grad_out_stride,
-                                      grad_out_dtype, _vp(grad_table), grad_table_stride,
-                                      grad_table_dtype, padding_id, add, _vp(workspace),
-                                      workspace_bytes, _vp(stream)), "lamb_embed_backward")
+    _check(load().lamb_embed_backward(ctypes.byref(embed), grad_out, grad_out_stride,
+                                      grad_out_dtype, grad_table, grad_table_stride,
+                                      grad_table_dtype, padding_id, add, workspace,
+                                      workspace_bytes, stream), "lamb_embed_backward")

@@ -28,15 +28,17 @@ hipError_t launch_embed(const EmbedArgs &args, const EmbedRows &rows, hipStream_
 // Sorting: a workgroup of kSortWaves waves takes the ids of one range of the
 // vocabulary out of all tokens.
 constexpr int kSortWaves = 16;
-constexpr int32_t kSortIds = 64;     // ids of a range where tokens are few
+constexpr int32_t kSortIds = 128;    // ids of a range where tokens are few
 constexpr int32_t kSortIdsMost = 512;
 constexpr int32_t sort_ids(int64_t tokens) {
     // Every workgroup reads every id, so many tokens are given fewer, wider ranges.
-    return tokens <= 32768 ? kSortIds : tokens <= 262144 ? 4 * kSortIds : kSortIdsMost;
+    return tokens <= 32768 ? kSortIds : tokens <= 262144 ? 2 * kSortIds : kSortIdsMost;
 }
 
-// Summing: a wave takes kSumTokens tokens of the sorted order and kSumColumns columns.
-constexpr int32_t kSumTokens = 32;
+// Summing: a wave takes kSumTokens tokens of the sorted order and kSumColumns columns,
+// or kZeroRows rows of the table that no token names.
+constexpr int32_t kSumTokens = 16;
+constexpr int32_t kZeroRows = 8;
 constexpr int32_t kSumColumns = 512;
 
 // order[0 .. first[vocab]): the tokens in the order of their ids, those of one id in

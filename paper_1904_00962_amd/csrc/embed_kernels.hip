@@ -16,6 +16,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "embed_internal.h"
 
 namespace lamb_mi355x {
@@ -126,14 +128,23 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(EmbedArgs a
     const int64_t share = (groups + kSortWaves - 1) / kSortWaves * 64;
     const int64_t begin = wave * share;
     const int64_t end = begin + share < a.tokens ? begin + share : a.tokens;
+    constexpr int kAhead = 8;  // groups of 64 ids in flight
     int32_t before = 0;
-    for (int64_t i = begin + lane; i < end; i += 64) {
-        const int64_t id = id_at(a, i);
-        if (id == skip || id < 0 || id >= a.vocab)
-            continue;
-        before += id < low;
-        if (id >= low && id < low + ids)
-            atomicAdd(&counts[wave * ids + int(id - low)], 1);
+    for (int64_t g = begin; g < end; g += 64 * kAhead) {
+        int64_t id[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t i = g + 64 * k + lane;
+            id[k] = i < end ? id_at(a, i) : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (id[k] == skip || id[k] < 0 || id[k] >= a.vocab)
+                continue;
+            before += id[k] < low;
+            if (id[k] >= low && id[k] < low + ids)
+                atomicAdd(&counts[wave * ids + int(id[k] - low)], 1);
+        }
     }
 #pragma unroll
     for (int d = 32; d; d >>= 1) before += __shfl_xor(before, d);
@@ -174,44 +185,44 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(EmbedArgs a
     // Put the tokens in their places. Lanes with the same id take theirs in lane order,
     // found id by id among the few lanes of a group that are in the range.
     int32_t *mine = counts + wave * ids;
-    for (int64_t g = begin; g < end; g += 64) {
-        const int64_t i = g + lane;
-        const int64_t id = i < end ? id_at(a, i) : -1;
-        const bool inside = id >= low && id < low + ids && id < a.vocab && id != skip;
-        uint64_t todo = __ballot(inside);
-        const int local = int(id - low);
-        while (todo) {
-            const int leader = __ffsll((unsigned long long)todo) - 1;
-            const int which = __shfl(local, leader);
-            const uint64_t same = __ballot(inside && local == which);
-            const int32_t place = mine[which];
-            if (inside && local == which) {
-                const int32_t at = place + __popcll(same & ((uint64_t(1) << lane) - 1));
-                order[at] = int32_t(i);
-                sorted[at] = int32_t(id);
+    for (int64_t g0 = begin; g0 < end; g0 += 64 * kAhead) {
+        int64_t ahead[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t i = g0 + 64 * k + lane;
+            ahead[k] = i < end ? id_at(a, i) : -1;
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t i = g0 + 64 * k + lane, id = ahead[k];
+            const bool inside = id >= low && id < low + ids && id < a.vocab && id != skip;
+            uint64_t todo = __ballot(inside);
+            const int local = int(id - low);
+            while (todo) {
+                const int leader = __ffsll((unsigned long long)todo) - 1;
+                const int which = __shfl(local, leader);
+                const uint64_t same = __ballot(inside && local == which);
+                const int32_t place = mine[which];
+                if (inside && local == which) {
+                    const int32_t at = place + __popcll(same & ((uint64_t(1) << lane) - 1));
+                    order[at] = int32_t(i);
+                    sorted[at] = int32_t(id);
+                }
+                if (lane == leader)
+                    mine[which] = place + __popcll(same);
+                todo &= ~same;
             }
-            if (lane == leader)
-                mine[which] = place + __popcll(same);
-            todo &= ~same;
         }
     }
 }
 
-// Writes, or adds to, a finished row's eight columns.
+// Writes, or adds to `old`, a finished row's eight columns.
 template <bool BF16>
 __device__ inline void finish(const EmbedArgs &a, const EmbedGrad &g, int64_t id, int c,
-                              float (&v)[8]) {
-    const int n = a.dim - c;
-    const int64_t at = id * g.table_stride + c;
+                              float (&v)[8], const float (&old)[8]) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= a.scale;
-    if (g.add) {
-        float old[8];
-        load8<BF16>(g.table, at, n, g.vector, old);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] += old[i];
-    }
-    store8<BF16>(g.table, at, n, g.vector, v);
+    for (int i = 0; i < 8; ++i) v[i] = g.add ? v[i] * a.scale + old[i] : v[i] * a.scale;
+    store8<BF16>(g.table, id * g.table_stride + c, a.dim - c, g.vector, v);
 }
 
 // Waves of the first `chunks` x (columns / kSumColumns) sum a chunk's columns; where the
@@ -223,12 +234,25 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedGrad g
     const int64_t chunks = (a.tokens + kSumTokens - 1) / kSumTokens;
     int64_t work = int64_t(blockIdx.x) * 4 + (threadIdx.x >> 6);
     if (work >= chunks * across) {
-        work -= chunks * across;
-        if (g.add || work >= a.vocab || g.first[work] != g.first[work + 1])
+        // kZeroRows rows: which of them are empty, then those one after another
+        const int64_t row0 = (work - chunks * across) * kZeroRows;
+        if (g.add || row0 >= a.vocab)
             return;
-        const float zero[8] = {};
-        for (int c = lane * 8; c < a.dim; c += 512)
-            store8<TABLE_BF16>(g.table, work * g.table_stride + c, a.dim - c, g.vector, zero);
+        const int64_t row = row0 + (lane < kZeroRows ? lane : kZeroRows);
+        const int32_t from = g.first[row < a.vocab ? row : a.vocab];
+        const int32_t to = __shfl_down(from, 1);
+        uint64_t empty = __ballot(lane < kZeroRows && row < a.vocab && from == to);
+        using T = typename std::conditional<TABLE_BF16, uint16_t, float>::type;
+        constexpr int kEach = 16 / sizeof(T);
+        const int whole = g.vector ? a.dim / kEach * kEach : 0;  // in 16 bytes a lane
+        while (empty) {
+            const int r = __ffsll((unsigned long long)empty) - 1;
+            empty &= empty - 1;
+            T *to = (T *)g.table + (row0 + r) * g.table_stride;
+            for (int c = lane * kEach; c < whole; c += 64 * kEach)
+                *(uint4 *)(to + c) = make_uint4(0, 0, 0, 0);
+            for (int c = whole + lane; c < a.dim; c += 64) to[c] = T(0);
+        }
         return;
     }
     const int64_t chunk = work / across;
@@ -245,37 +269,44 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedGrad g
     const int32_t id_before = begin > 0 ? g.sorted[begin - 1] : -1;
     const int32_t id_after = end < total ? g.sorted[end] : -1;
     float sum[8] = {};
-    constexpr int kAhead = 4;  // rows in flight
+    // rows in flight, and with them what the table holds for the ids that end there
+    constexpr int kAhead = 8;
     for (int t0 = 0; t0 < end - begin; t0 += kAhead) {
-        float row[kAhead][8];
-#pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const int32_t token = __shfl(token_of, t0 + k);
-            if (t0 + k < end - begin && n > 0)
-                load8<ROWS_BF16>(g.rows, token * g.rows_stride + c, n, g.vector, row[k]);
-        }
+        float row[kAhead][8], old[kAhead][8];
+        int32_t id[kAhead];
+        bool ends[kAhead], whole[kAhead];  // the id's last token here; all of them are here
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             const int t = t0 + k;
-            if (t >= end - begin)
+            const int32_t token = __shfl(token_of, t);
+            id[k] = __shfl(id_of, t);
+            const bool last = t + 1 == end - begin;
+            const int32_t after = last ? id_after : __shfl(id_of, t + 1);
+            ends[k] = last || after != id[k];
+            whole[k] = ends[k] && after != id[k] && id[k] != id_before;
+            if (t < end - begin && n > 0) {
+                load8<ROWS_BF16>(g.rows, token * g.rows_stride + c, n, g.vector, row[k]);
+                if (g.add && whole[k])
+                    load8<TABLE_BF16>(g.table, id[k] * g.table_stride + c, n, g.vector, old[k]);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (t0 + k >= end - begin)
                 break;
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += row[k][i];
-            const int32_t id = __shfl(id_of, t);
-            const bool last = t + 1 == end - begin;
-            if (!last && __shfl(id_of, t + 1) == id)
+            if (!ends[k])
                 continue;
-            // the id ends here, or goes on in the next chunk
-            const bool open = last && id == id_after;
             if (n > 0) {
-                if (open || id == id_before) {
+                if (whole[k]) {
+                    finish<TABLE_BF16>(a, g, id[k], c, sum, old[k]);
+                } else {
                     // an id that reaches back goes to the chunk's first slot, one that
                     // only reaches on to its second
-                    float *to = g.partial + (2 * chunk + (id != id_before)) * g.columns + c;
+                    float *to = g.partial + (2 * chunk + (id[k] != id_before)) * g.columns + c;
                     *(float4 *)to = make_float4(sum[0], sum[1], sum[2], sum[3]);
                     *(float4 *)(to + 4) = make_float4(sum[4], sum[5], sum[6], sum[7]);
-                } else {
-                    finish<TABLE_BF16>(a, g, id, c, sum);
                 }
             }
 #pragma unroll
@@ -301,15 +332,18 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, EmbedGrad 
     if (g.sorted[end] != id || g.first[id] < chunk * kSumTokens)
         return;
     const int64_t last = (g.first[id + 1] - 1) / kSumTokens;
-    float sum[8];
+    float sum[8], old[8] = {};
+    if (g.add)
+        load8<TABLE_BF16>(g.table, id * g.table_stride + c, a.dim - c, g.vector, old);
     load8<false>(g.partial, (2 * chunk + 1) * g.columns + c, 8, true, sum);
+#pragma unroll 8
     for (int64_t k = chunk + 1; k <= last; ++k) {
         float part[8];
         load8<false>(g.partial, 2 * k * g.columns + c, 8, true, part);
 #pragma unroll
         for (int i = 0; i < 8; ++i) sum[i] += part[i];
     }
-    finish<TABLE_BF16>(a, g, id, c, sum);
+    finish<TABLE_BF16>(a, g, id, c, sum, old);
 }
 
 }  // namespace
@@ -335,7 +369,7 @@ hipError_t launch_embed_sort(const EmbedArgs &args, int64_t skip, int32_t *order
 
 hipError_t launch_embed_sum(const EmbedArgs &args, const EmbedGrad &grad, hipStream_t stream) {
     const int64_t chunks = (args.tokens + kSumTokens - 1) / kSumTokens;
-    const int64_t waves = chunks * (grad.columns / kSumColumns) + (grad.add ? 0 : args.vocab);
+    const int64_t waves = chunks * (grad.columns / kSumColumns) + (grad.add ? 0 : (args.vocab + kZeroRows - 1) / kZeroRows);
     auto kernel =
         grad.rows_bf16
             ? (grad.table_bf16 ? embed_sum_kernel<true, true> : embed_sum_kernel<true, false>)

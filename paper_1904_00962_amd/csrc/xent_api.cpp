@@ -64,7 +64,9 @@ Product pick(int64_t rows, int64_t cols, int64_t depth, int64_t most) {
     Product best;
     for (int shape = kXentTiny; shape <= kXentLarge; ++shape) {
         const int64_t tiles = std::max<int64_t>(1, count_tiles(rows, cols, shape));
-        for (int64_t parts = 1; parts <= std::min<int64_t>(most, 32); ++parts) {
+        // more than two rounds of parts never pay
+        const int64_t limit = std::min<int64_t>({most, 32, 2 * kSlots[shape] / tiles + 1});
+        for (int64_t parts = 1; parts <= limit; ++parts) {
             const int64_t rounds = (tiles * parts + kSlots[shape] - 1) / kSlots[shape];
             // a part more writes and reads rows x cols of fp32 once more
             const double time = double(rounds) * (kFixed[shape] + double(depth) / double(parts) /
@@ -85,10 +87,10 @@ struct Layout {
     int64_t piece = 0;
     // offsets, and the end
     size_t kept = 0, source = 0, target = 0, packed = 0, table = 0, parts_at = 0, at_target = 0,
-           probs = 0, partial = 0, forward = 0, backward = 0;
+           probs = 0, partial = 0, bytes = 0;
 };
 
-Layout layout_of(const lamb_xent &x) {
+Layout layout_of(const lamb_xent &x, bool backward) {
     Layout l;
     l.ld = round_up(x.dim, 8);
     l.copy_table = !in_place(x.table, x.table_stride, x.dim);
@@ -103,14 +105,15 @@ Layout layout_of(const lamb_xent &x) {
     l.target = take(4 * x.tokens);
     l.packed = take(2 * x.tokens * l.ld);
     l.table = take(l.copy_table ? 2 * x.vocab * l.ld : 0);
-    const size_t common = at;
-    l.logits_shape = pick(x.tokens, x.vocab, x.dim, 1).shape;
-    const int32_t tile = xent_tile(l.logits_shape);
-    l.parts = int32_t((x.vocab + tile - 1) / tile);
-    l.parts_at = take(int64_t(l.parts) * x.tokens * 8);
-    l.at_target = take(4 * x.tokens);
-    l.forward = at;
-    at = common;
+    if (!backward) {
+        l.logits_shape = pick(x.tokens, x.vocab, x.dim, 1).shape;
+        const int32_t tile = xent_tile(l.logits_shape);
+        l.parts = int32_t((x.vocab + tile - 1) / tile);
+        l.parts_at = take(int64_t(l.parts) * x.tokens * 8);
+        l.at_target = take(4 * x.tokens);
+        l.bytes = at;
+        return l;
+    }
     // equal pieces of at most kPieceBytes: of the next few counts, the one whose products
     // fill their last rounds of workgroups best
     const int64_t rows = x.tokens ? x.tokens : 1;
@@ -137,7 +140,7 @@ Layout layout_of(const lamb_xent &x) {
     }
     l.probs = take(2 * x.tokens * l.piece);
     l.partial = take(int64_t(l.splits) * x.tokens * l.ld * 4);
-    l.backward = at;
+    l.bytes = at;
     return l;
 }
 
@@ -195,11 +198,10 @@ lamb_status lamb_xent_workspace(const lamb_xent *xent, size_t *forward_bytes,
     const lamb_status st = check(xent);
     if (st != LAMB_OK)
         return st;
-    const Layout l = layout_of(*xent);
     if (forward_bytes)
-        *forward_bytes = l.forward;
+        *forward_bytes = layout_of(*xent, false).bytes;
     if (backward_bytes)
-        *backward_bytes = l.backward;
+        *backward_bytes = layout_of(*xent, true).bytes;
     return LAMB_OK;
 }
 
@@ -213,8 +215,8 @@ lamb_status lamb_xent_forward(const lamb_xent *xent, float *loss, float *lse, fl
         return fail(LAMB_ENULL, "loss and lse must not be NULL");
     if (!aligned_to(loss, 4) || !aligned_to(lse, 4) || !aligned_to(mean, 4))
         return fail(LAMB_EALIGN, "a pointer is not aligned to its elements");
-    const Layout l = layout_of(x);
-    st = check_workspace(workspace, workspace_bytes, l.forward);
+    const Layout l = layout_of(x, false);
+    st = check_workspace(workspace, workspace_bytes, l.bytes);
     if (st != LAMB_OK)
         return st;
     const int64_t id = size_of(x.target_dtype);
@@ -225,7 +227,7 @@ lamb_status lamb_xent_forward(const lamb_xent *xent, float *loss, float *lse, fl
         span_of(loss, uint64_t(x.tokens) * 4, true, 0, "loss"),
         span_of(lse, uint64_t(x.tokens) * 4, true, 0, "lse"),
         span_of(mean, mean ? 4 : 0, true, 0, "mean"),
-        span_of(workspace, l.forward, true, 0, "workspace")};
+        span_of(workspace, l.bytes, true, 0, "workspace")};
     st = check_spans(spans, sizeof spans / sizeof spans[0]);
     if (st != LAMB_OK)
         return st;
@@ -236,14 +238,16 @@ lamb_status lamb_xent_forward(const lamb_xent *xent, float *loss, float *lse, fl
     if (st != LAMB_OK)
         return st;
     hipError_t err = hipSuccess;
+    const bool few = x.tokens > 0 && x.tokens <= kReduceTokens;  // one workgroup reduces
     if (x.tokens) {
         float2 *parts = reinterpret_cast<float2 *>(work + l.parts_at);
         float *at_target = reinterpret_cast<float *>(work + l.at_target);
         err = launch_xent_logits(args, l.logits_shape, parts, at_target, stream);
         if (err == hipSuccess)
-            err = launch_xent_reduce(args, l.parts, parts, at_target, loss, lse, stream);
+            err = launch_xent_reduce(args, l.parts, parts, at_target, loss, lse,
+                                     few ? mean : nullptr, stream);
     }
-    if (err == hipSuccess && mean)
+    if (err == hipSuccess && mean && !few)
         err = launch_xent_mean(loss, args.tokens, args.kept, mean, stream);
     return err == hipSuccess ? LAMB_OK : fail_hip(err, "kernel launch");
 }
@@ -271,8 +275,8 @@ lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
     if (!aligned_to(g.grad_loss, 4) || !aligned_to(lse, 4) || !aligned_to(g.grad_hidden, 2) ||
         !aligned_to(g.grad_table, bf16 ? 2 : 4))
         return fail(LAMB_EALIGN, "a pointer is not aligned to its elements");
-    const Layout l = layout_of(x);
-    st = check_workspace(workspace, workspace_bytes, l.backward);
+    const Layout l = layout_of(x, true);
+    st = check_workspace(workspace, workspace_bytes, l.bytes);
     if (st != LAMB_OK)
         return st;
     const int64_t id = size_of(x.target_dtype);
@@ -288,7 +292,7 @@ lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
         span_of(g.grad_table,
                 g.grad_table ? rows_bytes(x.vocab, g.grad_table_stride, x.dim, bf16 ? 2 : 4) : 0,
                 true, 0, "grad_table"),
-        span_of(workspace, l.backward, true, 0, "workspace")};
+        span_of(workspace, l.bytes, true, 0, "workspace")};
     st = check_spans(spans, sizeof spans / sizeof spans[0]);
     if (st != LAMB_OK)
         return st;

@@ -52,8 +52,9 @@ hipError_t launch_xent_copy(const uint16_t *src, int64_t stride, uint16_t *dst, 
 // exponentials, parts[column][token], and the targets' logits.
 hipError_t launch_xent_logits(const XentArgs &args, int shape, float2 *parts, float *at_target,
                               hipStream_t stream);
+// `mean` non-null: the mean too, where kReduceTokens hold all tokens.
 hipError_t launch_xent_reduce(const XentArgs &args, int32_t n_parts, const float2 *parts,
-                              const float *at_target, float *loss, float *lse,
+                              const float *at_target, float *loss, float *lse, float *mean,
                               hipStream_t stream);
 // mean = sum of the losses over the count of tokens (0 without any).
 hipError_t launch_xent_mean(const float *loss, int32_t tokens, const int32_t *kept, float *mean,

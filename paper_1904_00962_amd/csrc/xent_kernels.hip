@@ -205,29 +205,42 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_logits_ke
     }
 }
 
-// kReduceTokens tokens by 16 threads each, joined in a fixed order.
+// kReduceTokens tokens by 16 threads each, joined in a fixed order. `mean` non-null: of
+// all tokens, which are one workgroup's.
 __global__ __launch_bounds__(256) void xent_reduce_kernel(XentArgs a, int32_t n_parts,
                                                           const float2 *parts,
                                                           const float *at_target, float *loss,
-                                                          float *lse) {
+                                                          float *lse, float *mean) {
     __shared__ float2 shared[16][kReduceTokens];
     const int32_t kept = *a.kept;
     const int t = threadIdx.x % kReduceTokens, group = threadIdx.x / kReduceTokens;
     const int m = blockIdx.x * kReduceTokens + t;
-    if (int(blockIdx.x) * kReduceTokens >= kept)
+    if (int(blockIdx.x) * kReduceTokens >= kept) {
+        if (mean && threadIdx.x == 0)
+            *mean = 0.0f;
         return;
+    }
     float2 sum = make_float2(-INFINITY, 0.0f);
     if (m < kept)
         for (int p = group; p < n_parts; p += 16) sum = join(sum, parts[int64_t(p) * a.tokens + m]);
     shared[group][t] = sum;
     __syncthreads();
+    double value = 0.0;
     if (group == 0 && m < kept) {
         for (int g = 1; g < 16; ++g) sum = join(sum, shared[g][t]);
         const int token = a.source[m];
         const bool inside = a.target[m] >= 0;
         const float total = sum.x + logf(sum.y);
+        const float mine = inside ? total - at_target[m] : NAN;
         lse[token] = inside ? total : NAN;
-        loss[token] = inside ? total - at_target[m] : NAN;
+        loss[token] = mine;
+        value = mine;
+    }
+    if (mean && group < 4) {  // wave 0, whose other groups hold zeros
+#pragma unroll
+        for (int d = 8; d; d >>= 1) value += __shfl_xor(value, d);
+        if (threadIdx.x == 0)
+            *mean = float(value / double(kept));
     }
 }
 
@@ -471,10 +484,10 @@ hipError_t launch_xent_logits(const XentArgs &args, int shape, float2 *parts, fl
 }
 
 hipError_t launch_xent_reduce(const XentArgs &args, int32_t n_parts, const float2 *parts,
-                              const float *at_target, float *loss, float *lse,
+                              const float *at_target, float *loss, float *lse, float *mean,
                               hipStream_t stream) {
     xent_reduce_kernel<<<tiles_of(args.tokens, kReduceTokens), 256, 0, stream>>>(
-        args, n_parts, parts, at_target, loss, lse);
+        args, n_parts, parts, at_target, loss, lse, mean);
     return hipGetLastError();
 }
 

@@ -20,26 +20,57 @@ from . import _lib, _ops
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
+_torch_module = None
+_FLOAT_CODES = {}
+_ID_CODES = {}
+
+
 def _torch():
-    import torch
-    return torch
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _FLOAT_CODES.update({torch.float32: _ops.LAMB_DTYPE_F32,
+                             torch.bfloat16: _ops.LAMB_DTYPE_BF16})
+        _ID_CODES.update({torch.int32: _ops.LAMB_DTYPE_I32, torch.int64: _ops.LAMB_DTYPE_I64})
+        _torch_module = torch
+    return _torch_module
 
 
 def _stream(device) -> int:
-    return _torch().cuda.current_stream(device).cuda_stream
+    torch = _torch()
+    # the raw handle by itself, where torch has it: a Stream object costs 4 us a call
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if raw is not None:
+        return raw(device.index)
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+class _NoSwitch:
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        return False
+
+
+_NO_SWITCH = _NoSwitch()
+
+
+def _on(device):
+    """A context on ``device``; nothing where it is current already."""
+    cuda = _torch().cuda
+    return _NO_SWITCH if cuda.current_device() == device.index else cuda.device(device)
 
 
 def _float_code(dtype) -> int:
-    torch = _torch()
-    if dtype == torch.float32:
-        return _ops.LAMB_DTYPE_F32
-    if dtype == torch.bfloat16:
-        return _ops.LAMB_DTYPE_BF16
-    raise TypeError("need float32 or bfloat16, got %s" % dtype)
+    code = _FLOAT_CODES.get(dtype)
+    if code is None:
+        raise TypeError("need float32 or bfloat16, got %s" % dtype)
+    return code
 
 
 def _on_gpu(name, t, device=None):
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError("%s must live on a GPU" % name)
     if device is not None and t.device != device:
         raise ValueError("%s is on another device" % name)
@@ -93,7 +124,7 @@ class Orthogonalizer:
         self.precision = precision
         self.params = _ops.lamb_ns_params_init(steps=int(steps), a=coefficients[0],
                                                b=coefficients[1], c=coefficients[2], eps=eps)
-        with torch.cuda.device(self.device):
+        with _on(self.device):
             self.plan = _ops.lamb_ortho_plan_create(
                 rows, _float_code(self.inputs[0].dtype), _float_code(self.outputs[0].dtype),
                 _ops.PRECISIONS[precision])
@@ -110,26 +141,25 @@ class Orthogonalizer:
 def _rows(name, t, dtype, device=None):
     """A 2-D tensor whose rows are contiguous: its row stride."""
     _on_gpu(name, t, device)
-    if t.dtype != dtype:
+    if t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
     if t.dim() != 2:
         raise ValueError("%s must have two dimensions" % name)
-    if t.shape[1] > 1 and t.stride(1) != 1:
+    rows, cols = t.shape
+    stride, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError("%s: the elements of a row must be adjacent" % name)
-    # the stride of a single row means nothing; an expanded row's is 0
-    if t.shape[0] <= 1:
-        return t.shape[1]
-    return t.stride(0)
+    return stride if rows > 1 else cols  # the stride of a single row means nothing
 
 
 def _ids(name, t, device):
-    torch = _torch()
     _on_gpu(name, t, device)
-    if t.dtype not in (torch.int32, torch.int64):
+    code = _ID_CODES.get(t.dtype)
+    if code is None:
         raise TypeError("%s must be int32 or int64, got %s" % (name, t.dtype))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    return _ops.LAMB_DTYPE_I64 if t.dtype == torch.int64 else _ops.LAMB_DTYPE_I32
+    return code
 
 
 def _xent(hidden, table, targets, ignore_index):
@@ -160,11 +190,11 @@ def linear_cross_entropy(hidden, table, targets, *, ignore_index: int = -100):
     """
     torch = _torch()
     x = _xent(hidden, table, targets, ignore_index)
-    need, _ = _ops.lamb_xent_workspace(x)
+    need = _ops.lamb_xent_workspace(x, False)
     out = torch.empty(2, hidden.shape[0], dtype=torch.float32, device=hidden.device)
     mean = torch.empty((), dtype=torch.float32, device=hidden.device)
     work = _workspace(need, hidden.device)
-    with torch.cuda.device(hidden.device):
+    with _on(hidden.device):
         _ops.lamb_xent_forward(x, out[0].data_ptr(), out[1].data_ptr(), mean.data_ptr(),
                                work.data_ptr(), need, _stream(hidden.device))
     return mean, out[0], out[1]
@@ -205,16 +235,16 @@ def linear_cross_entropy_grad(hidden, table, targets, lse, grad_hidden=None, gra
         if grad_table.shape != table.shape:
             raise ValueError("grad_table must have the table's shape")
         g.grad_table = grad_table.data_ptr()
-    _, need = _ops.lamb_xent_workspace(x)
+    need = _ops.lamb_xent_workspace(x, True)
     work = _workspace(need, device)
-    with torch.cuda.device(device):
+    with _on(device):
         _ops.lamb_xent_backward(x, lse.data_ptr(), g, work.data_ptr(), need, _stream(device))
 
 
-def _embed(ids, table, scale):
-    code = _ids("ids", ids, table.device)
-    return _ops.lamb_embed(ids.data_ptr() or None, ids.numel(), table.shape[0], table.shape[1],
-                           code, float(scale))
+def _embed(ids, table, scale, device):
+    code = _ids("ids", ids, device)
+    vocab, dim = table.shape
+    return _ops.lamb_embed(ids.data_ptr() or None, ids.numel(), vocab, dim, code, scale)
 
 
 def embedding(ids, table, *, scale: float = 1.0, out_dtype=None, out=None):
@@ -223,21 +253,23 @@ def embedding(ids, table, *, scale: float = 1.0, out_dtype=None, out=None):
     table's by default), or ``out`` [ids.numel(), dim]. An id outside the table gives a
     row of NaN."""
     torch = _torch()
-    stride = _rows("table", table, table.dtype)
-    e = _embed(ids, table, scale)
+    device, dtype = table.device, table.dtype
+    stride = _rows("table", table, dtype)
+    e = _embed(ids, table, scale, device)
     if out is None:
-        result = torch.empty(*ids.shape, table.shape[1], dtype=out_dtype or table.dtype,
-                             device=table.device)
-        out_stride = table.shape[1]
+        out_dtype = out_dtype or dtype
+        out_code = _float_code(out_dtype)
+        out_stride = e.dim
+        result = torch.empty((*ids.shape, out_stride), dtype=out_dtype, device=device)
     else:
         result = out
-        out_stride = _rows("out", out, out_dtype or out.dtype, table.device)
-        if out.shape != (ids.numel(), table.shape[1]):
-            raise ValueError("out must be [%d, %d]" % (ids.numel(), table.shape[1]))
-    with torch.cuda.device(table.device):
-        _ops.lamb_embed_forward(e, table.data_ptr(), stride, _float_code(table.dtype),
-                                result.data_ptr(), out_stride, _float_code(result.dtype),
-                                _stream(table.device))
+        out_code = _float_code(out.dtype)
+        out_stride = _rows("out", out, out_dtype or out.dtype, device)
+        if out.shape != (e.tokens, e.dim):
+            raise ValueError("out must be [%d, %d]" % (e.tokens, e.dim))
+    with _on(device):
+        _ops.lamb_embed_forward(e, table.data_ptr(), stride, _float_code(dtype),
+                                result.data_ptr(), out_stride, out_code, _stream(device))
     return result
 
 
@@ -248,17 +280,18 @@ def embedding_grad(ids, grad_out, grad_table, *, scale: float = 1.0,
     ``grad_out`` [ids.numel(), dim] whose id is v, in their order and in fp32. Either is
     float32 or bfloat16. Tokens with id ``padding_id``, or outside the table, add
     nothing."""
-    torch = _torch()
+    _torch()
+    device = grad_table.device
     stride = _rows("grad_table", grad_table, grad_table.dtype)
-    out_stride = _rows("grad_out", grad_out, grad_out.dtype, grad_table.device)
-    if grad_out.shape != (ids.numel(), grad_table.shape[1]):
-        raise ValueError("grad_out must be [%d, %d]" % (ids.numel(), grad_table.shape[1]))
-    e = _embed(ids, grad_table, scale)
+    out_stride = _rows("grad_out", grad_out, grad_out.dtype, device)
+    e = _embed(ids, grad_table, scale, device)
+    if grad_out.shape != (e.tokens, e.dim):
+        raise ValueError("grad_out must be [%d, %d]" % (e.tokens, e.dim))
+    out_code, code = _float_code(grad_out.dtype), _float_code(grad_table.dtype)
     need = _ops.lamb_embed_workspace(e)
-    work = _workspace(need, grad_table.device)
-    with torch.cuda.device(grad_table.device):
-        _ops.lamb_embed_backward(
-            e, grad_out.data_ptr(), out_stride, _float_code(grad_out.dtype),
-            grad_table.data_ptr(), stride, _float_code(grad_table.dtype),
-            -1 if padding_id is None else int(padding_id), int(bool(accumulate)),
-            work.data_ptr(), need, _stream(grad_table.device))
+    work = _workspace(need, device)
+    with _on(device):
+        _ops.lamb_embed_backward(e, grad_out.data_ptr(), out_stride, out_code,
+                                 grad_table.data_ptr(), stride, code,
+                                 -1 if padding_id is None else padding_id, bool(accumulate),
+                                 work.data_ptr(), need, _stream(device))
