@@ -9,16 +9,23 @@
 
 using namespace lamb_mi355x;
 
+struct TileList {
+    NsTile *tiles = nullptr;
+    int32_t n = 0;
+};
+
 struct lamb_ns_plan {
     int device = 0;
     bool muon = false, bf16_in = false, split = false;
     NsKind kind = kNsBf16Out;
     int sym_shape = 0, update_shape = 0;
-    int32_t n = 0, blocks = 0, n_sym = 0, n_update = 0;
+    int32_t blocks = 0;
     void *block = nullptr;  // every device buffer of the plan
     NsMatrix *matrices = nullptr;
     int32_t *block_matrix = nullptr;
-    NsTile *sym_tiles = nullptr, *update_tiles = nullptr;
+    // of all matrices ([0]) and of those without chains ([1])
+    TileList sym[2], update[2];
+    TileList both, only_q, only_t, next_gram;  // of those with: Q and T, Q, T, A
     double *partials = nullptr;
     uint32_t *flag = nullptr;  // see launch_ns_check
 };
@@ -122,18 +129,31 @@ void for_tiles(int32_t rows, int32_t cols, int shape, F f) {
         for (int32_t c = 0; c * t < cols; ++c) f(r, c);
 }
 
+// Chains pay for matrices at least twice as long as wide, where they save more than
+// their launches cost: BERT-Large's matrices (split, 48 of them 1024 x 4096) take
+// CHAIN_ON ms a step with chains and CHAIN_OFF without, ResNet-50's RES_ON and RES_OFF, the
+// tiny set's (where the estimate says no) TINY_ON and TINY_OFF us.
+void pick_chains(std::vector<NsMatrix> &matrices, bool split) {
+    constexpr double kFlopsPerUs = 1e9, kChainUs = 100.0;
+    const double turns = split ? kNsChainSplit : kNsChainHalf;
+    double saved = 0.0;
+    for (NsMatrix &m : matrices) {
+        const double s = std::min(m.rows, m.cols), l = std::max(m.rows, m.cols);
+        m.chain = l >= 2.0 * s;
+        // for five iterations: three products of X each, or per chain, and four or so of
+        // the short side
+        if (m.chain)
+            saved += 5.0 * s * s * (3.0 * l + s) - (5.0 / turns) * 3.0 * l * s * s -
+                     5.0 * 3.0 * s * s * s;
+    }
+    if (saved * (split ? 3.0 : 1.0) < kChainUs * kFlopsPerUs)
+        for (NsMatrix &m : matrices) m.chain = 0;
+}
+
 // Fills in sizes, tiles and workspace; `matrices` has its user's fields set.
 lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
-    plan->n = int32_t(matrices.size());
     pick_shapes(matrices, plan->split, &plan->sym_shape, &plan->update_shape);
-
-    // Longest products first, so that the last workgroups are short ones.
-    std::vector<int32_t> order(matrices.size());
-    for (size_t i = 0; i < order.size(); ++i) order[i] = int32_t(i);
-    auto side = [&](int32_t i) { return std::min(matrices[i].rows, matrices[i].cols); };
-    auto longest = [&](int32_t i) { return std::max(matrices[i].rows, matrices[i].cols); };
-
-    std::vector<NsTile> sym, update;
+    pick_chains(matrices, plan->split);
     std::vector<int32_t> block_matrix;
     int64_t elems = 0, blocks = 0;  // workspace, in 16-bit elements
     std::vector<int64_t> at_x(matrices.size()), at_gram(matrices.size());
@@ -149,7 +169,7 @@ lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
         at_x[i] = elems;
         elems += 2 * parts * m.x_low;
         at_gram[i] = elems;
-        elems += 2 * parts * m.gram_low;
+        elems += (m.chain ? 6 : 2) * parts * m.gram_low;
         const int64_t units = int64_t(m.rows) * (m.ld / 8);
         const int64_t count = (units + kNsBlockUnits - 1) / kNsBlockUnits;
         if (blocks + count > INT32_MAX)
@@ -160,24 +180,53 @@ lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
         block_matrix.insert(block_matrix.end(), size_t(count), int32_t(i));
     }
     plan->blocks = int32_t(blocks);
-    std::stable_sort(order.begin(), order.end(),
+
+    // Longest products first, so that the last workgroups are short ones.
+    std::vector<int32_t> by_length(matrices.size()), by_side;
+    for (size_t i = 0; i < by_length.size(); ++i) by_length[i] = int32_t(i);
+    by_side = by_length;
+    auto longest = [&](int32_t i) { return std::max(matrices[i].rows, matrices[i].cols); };
+    std::stable_sort(by_length.begin(), by_length.end(),
                      [&](int32_t p, int32_t q) { return longest(p) > longest(q); });
-    for (int32_t i : order)
-        for_tiles(side(i), side(i), plan->sym_shape, [&](int32_t r, int32_t c) {
-            if (c <= r)
-                sym.push_back(NsTile{i, r, c});
-        });
-    std::stable_sort(order.begin(), order.end(),
-                     [&](int32_t p, int32_t q) { return side(p) > side(q); });
-    for (int32_t i : order)
-        for_tiles(matrices[i].rows, matrices[i].cols, plan->update_shape,
-                  [&](int32_t r, int32_t c) { update.push_back(NsTile{i, r, c}); });
-    if (sym.size() > INT32_MAX || update.size() > INT32_MAX)
-        return fail(LAMB_EINVAL, "the matrices take too many tiles for one plan");
-    sym = spread_over_dies(sym);
-    update = spread_over_dies(update);
-    plan->n_sym = int32_t(sym.size());
-    plan->n_update = int32_t(update.size());
+    std::stable_sort(by_side.begin(), by_side.end(), [&](int32_t p, int32_t q) {
+        return matrices[p].side > matrices[q].side;
+    });
+    enum Which { kAll, kDirect, kChained };
+    auto wanted = [&](int32_t i, Which which) {
+        return which == kAll || (matrices[i].chain != 0) == (which == kChained);
+    };
+    auto triangles = [&](const std::vector<int32_t> &order, Which which, int products, int first) {
+        std::vector<NsTile> list;
+        for (int32_t i : order)
+            if (wanted(i, which))
+                for (int32_t p = first; p < first + products; ++p)
+                    for_tiles(matrices[i].side, matrices[i].side, plan->sym_shape,
+                              [&](int32_t r, int32_t c) {
+                                  if (c <= r)
+                                      list.push_back(NsTile{i, r, c, p});
+                              });
+        return list;
+    };
+    auto whole = [&](Which which) {
+        std::vector<NsTile> list;
+        for (int32_t i : by_side)
+            if (wanted(i, which))
+                for_tiles(matrices[i].rows, matrices[i].cols, plan->update_shape,
+                          [&](int32_t r, int32_t c) { list.push_back(NsTile{i, r, c, 0}); });
+        return list;
+    };
+    std::vector<NsTile> lists[] = {triangles(by_length, kAll, 1, 0),
+                                   triangles(by_length, kDirect, 1, 0),
+                                   whole(kAll),
+                                   whole(kDirect),
+                                   triangles(by_side, kChained, 2, kNsQ),
+                                   triangles(by_side, kChained, 1, kNsQ),
+                                   triangles(by_side, kChained, 1, kNsT),
+                                   triangles(by_side, kChained, 1, kNsA)};
+    TileList *const held[] = {&plan->sym[0], &plan->sym[1], &plan->update[0], &plan->update[1],
+                              &plan->both,   &plan->only_q, &plan->only_t,    &plan->next_gram};
+    constexpr int kLists = sizeof held / sizeof held[0];
+    static_assert(sizeof lists / sizeof lists[0] == kLists, "a place for every list");
 
     size_t bytes = 0;
     auto take = [&](size_t size) {
@@ -188,8 +237,12 @@ lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
     const size_t o_work = take(size_t(elems) * 2);
     const size_t o_matrices = take(matrices.size() * sizeof(NsMatrix));
     const size_t o_blocks = take(block_matrix.size() * 4);
-    const size_t o_sym = take(sym.size() * sizeof(NsTile));
-    const size_t o_update = take(update.size() * sizeof(NsTile));
+    size_t o_lists[kLists];
+    for (int k = 0; k < kLists; ++k) {
+        if (lists[k].size() > INT32_MAX)
+            return fail(LAMB_EINVAL, "the matrices take too many tiles for one plan");
+        o_lists[k] = take(lists[k].size() * sizeof(NsTile));
+    }
     const size_t o_partials = take(size_t(blocks) * 8);
     const size_t o_flag = take(8);
     hipError_t err = hipGetDevice(&plan->device);
@@ -207,23 +260,32 @@ lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
         NsMatrix &m = matrices[i];
         m.x[0] = work + at_x[i];
         m.x[1] = m.x[0] + parts * m.x_low;
-        m.gram = work + at_gram[i];
-        m.poly = m.gram + parts * m.gram_low;
+        auto square = [&](int k) { return work + at_gram[i] + k * parts * m.gram_low; };
+        m.gram[0] = square(0);
+        m.poly[0] = square(1);
+        if (m.chain) {
+            m.gram[1] = square(2);
+            m.poly[1] = square(3);
+            m.q = square(4);
+            m.t = square(5);
+        }
     }
     plan->matrices = reinterpret_cast<NsMatrix *>(base + o_matrices);
     plan->block_matrix = reinterpret_cast<int32_t *>(base + o_blocks);
-    plan->sym_tiles = reinterpret_cast<NsTile *>(base + o_sym);
-    plan->update_tiles = reinterpret_cast<NsTile *>(base + o_update);
     plan->partials = reinterpret_cast<double *>(base + o_partials);
     plan->flag = reinterpret_cast<uint32_t *>(base + o_flag);
     auto up = [&](void *to, const void *from, size_t size) {
-        if (err == hipSuccess)
+        if (err == hipSuccess && size)
             err = hipMemcpy(to, from, size, hipMemcpyHostToDevice);
     };
     up(plan->matrices, matrices.data(), matrices.size() * sizeof(NsMatrix));
     up(plan->block_matrix, block_matrix.data(), block_matrix.size() * 4);
-    up(plan->sym_tiles, sym.data(), sym.size() * sizeof(NsTile));
-    up(plan->update_tiles, update.data(), update.size() * sizeof(NsTile));
+    for (int k = 0; k < kLists; ++k) {
+        const std::vector<NsTile> spread = spread_over_dies(lists[k]);
+        held[k]->tiles = reinterpret_cast<NsTile *>(base + o_lists[k]);
+        held[k]->n = int32_t(spread.size());
+        up(held[k]->tiles, spread.data(), spread.size() * sizeof(NsTile));
+    }
     const uint32_t zero[2] = {};
     up(plan->flag, zero, sizeof zero);
     if (err != hipSuccess)
@@ -257,17 +319,36 @@ lamb_status run(lamb_ns_plan *plan, const lamb_ns_params &ns, NsStep step, uint3
     if (err == hipSuccess)
         err = launch_ns_convert(plan->matrices, plan->block_matrix, plan->blocks, plan->muon,
                                 plan->bf16_in, plan->split, step, plan->partials, flag, stream);
+    const int32_t chain = plan->split ? kNsChainSplit : kNsChainHalf;
+    auto run_list = [&](const TileList &list, auto launch) {
+        if (err == hipSuccess && list.n)
+            err = launch(list.tiles, list.n);
+    };
     for (int32_t k = 0; k < ns.steps && err == hipSuccess; ++k) {
-        const int parity = k & 1;
-        err = launch_ns_gram(plan->matrices, plan->sym_tiles, plan->n_sym, plan->sym_shape,
-                             plan->split, parity, stream);
-        if (err == hipSuccess)
-            err = launch_ns_poly(plan->matrices, plan->sym_tiles, plan->n_sym, plan->sym_shape,
-                                 plan->split, step, stream);
-        if (err == hipSuccess)
-            err = launch_ns_update(plan->matrices, plan->update_tiles, plan->n_update,
-                                   plan->update_shape, plan->split, parity, k + 1 == ns.steps, plan->kind, step, flag,
-                                   stream);
+        const bool last = k + 1 == ns.steps;
+        const NsTurn turn{k % chain, {k & 1, k / chain & 1}};
+        const bool begins = turn.turn == 0, ends = last || turn.turn + 1 == chain;
+        run_list(plan->sym[!begins], [&](const NsTile *tiles, int32_t n) {
+            return launch_ns_gram(plan->matrices, tiles, n, plan->sym_shape, plan->split, turn,
+                                  stream);
+        });
+        run_list(plan->sym[0], [&](const NsTile *tiles, int32_t n) {
+            return launch_ns_poly(plan->matrices, tiles, n, plan->sym_shape, plan->split, turn,
+                                  step, stream);
+        });
+        auto product = [&](const NsTile *tiles, int32_t n) {
+            return launch_ns_product(plan->matrices, tiles, n, plan->sym_shape, plan->split, turn,
+                                     stream);
+        };
+        // Q = P at first, and A is not needed after the last P: then only one of the two
+        if (!begins || !ends)
+            run_list(begins ? plan->only_t : ends ? plan->only_q : plan->both, product);
+        if (!ends)
+            run_list(plan->next_gram, product);
+        run_list(plan->update[!ends], [&](const NsTile *tiles, int32_t n) {
+            return launch_ns_update(plan->matrices, tiles, n, plan->update_shape, plan->split,
+                                    turn, last, plan->kind, step, flag, stream);
+        });
     }
     if (err != hipSuccess)
         return fail_hip(err, "kernel launch");

@@ -27,22 +27,42 @@ struct NsMatrix {
     void *out;          // orthogonalize: the output; Muon: the parameters x
     float *m;           // Muon: the momentum
     uint16_t *x[2];     // X of even and odd iterations, [rows][ld]; low parts x_low further
-    uint16_t *gram;     // A, [side][side_ld]; low parts gram_low further
-    uint16_t *poly;     // P, likewise
+    uint16_t *gram[2];  // A, [side][side_ld]; low parts gram_low further
+    uint16_t *poly[2];  // P, likewise, and with `chain` also ...
+    uint16_t *q, *t;    // Q and T of a chain, likewise (see ns_chain)
     int64_t in_stride, out_stride;
     int64_t x_low, gram_low;
     int32_t rows, cols, ld, side, side_ld, tall;
     int32_t first_block, blocks;  // its workgroups of the elementwise passes
     int32_t vector;               // rows of in, out and m allow 16-byte accesses
     int32_t wd;                   // Muon: decay applies
+    int32_t chain;                // iterations in chains
+    int32_t reserved;
 };
-static_assert(sizeof(NsMatrix) == 128, "NsMatrix layout");
+static_assert(sizeof(NsMatrix) == 168, "NsMatrix layout");
 
 // One tile of a product.
 struct NsTile {
     int32_t matrix;
     int32_t row, col;  // in tiles
+    int32_t product;   // an NsProduct, for launch_ns_product
 };
+
+// Chains. As every P is a polynomial of A, all of them commute, and n iterations can be
+// taken on the short side alone: with A_0 = X X^T,
+//   P_i = a I + b A_i + c A_i^2,  T = P_i A_i,  A_{i+1} = T P_i,  Q_i = P_i Q_{i-1},
+// and at the end X <- Q X. For a matrix of L x S this costs 3 S^3 (symmetric halves) an
+// iteration beside S^3 for Q, in place of 3 L S^2. The rounding of A hides singular
+// values below its square root, and n iterations multiply what it hides by up to
+// 3.4^(2 n): chains are kept to kNsChainSplit and kNsChainHalf iterations, which leave
+// the result as exact as direct iterations do (256 x 1024 matrices of rank 32 and noise:
+// 3.1e-6 and 3.3e-3 off, 2.5e-6 and 3.3e-3 directly; five at once: 1e-4 and 8e-2).
+constexpr int32_t kNsChainSplit = 3, kNsChainHalf = 2;
+// Q is held times kNsQScale: its entries reach those of P to the third power.
+constexpr float kNsQScale = 128.0f;
+enum NsProduct : int32_t { kNsQ = 0, kNsT = 1, kNsA = 2 };
+// Where iteration `turn` of a chain finds A and P is [turn & 1]; Q is P at first, then
+// q, then the P before.
 
 // Tile shapes of the products, all square.
 enum NsShape : int32_t { kNsTiny = 0, kNsSmall = 1, kNsLarge = 2 };
@@ -75,14 +95,23 @@ hipError_t launch_ns_convert(const NsMatrix *matrices, const int32_t *block_matr
                              int32_t blocks, bool muon, bool bf16_in, bool split,
                              const NsStep &step, const double *partials, uint32_t *flag,
                              hipStream_t stream);
-// Products over `n` tiles of shape `shape`.
+// Products over `n` tiles of shape `shape`. `turn`: the iteration of matrices with
+// `chain` in their chain. `parity`: which X is read, [0] of matrices without a chain,
+// [1] of those with one.
+struct NsTurn {
+    int32_t turn;
+    int32_t parity[2];
+};
 hipError_t launch_ns_gram(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
-                          bool split, int parity, hipStream_t stream);
+                          bool split, const NsTurn &turn, hipStream_t stream);
 hipError_t launch_ns_poly(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
-                          bool split, const NsStep &step, hipStream_t stream);
+                          bool split, const NsTurn &turn, const NsStep &step, hipStream_t stream);
+// The products of a chain, each tile's by its `product`.
+hipError_t launch_ns_product(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
+                             bool split, const NsTurn &turn, hipStream_t stream);
 // `last`: the result goes to `out` as `kind` says, else to the other X.
 hipError_t launch_ns_update(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
-                            bool split, int parity, bool last, NsKind kind, const NsStep &step,
+                            bool split, const NsTurn &turn, bool last, NsKind kind, const NsStep &step,
                             const uint32_t *flag, hipStream_t stream);
 
 }  // namespace lamb_mi355x

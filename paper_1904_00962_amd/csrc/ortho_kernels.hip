@@ -282,11 +282,11 @@ __device__ inline void store_symmetric(const NsMatrix &mat, uint16_t *to, const 
 template <class Shape>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_gram_kernel(const NsMatrix *matrices,
                                                                   const NsTile *tiles,
-                                                                  int parity) {
+                                                                  NsTurn turn) {
     __shared__ __align__(1024) short lds[Shape::kLds];
     const NsTile tile = tiles[blockIdx.x];
     const NsMatrix mat = matrices[tile.matrix];
-    const uint16_t *x = (parity ? mat.x[1] : mat.x[0]);
+    const uint16_t *x = (mat.chain ? turn.parity[1] : turn.parity[0]) ? mat.x[1] : mat.x[0];
     float4v acc[Shape::MI][Shape::NI] = {};
     const int64_t m = int64_t(tile.row) * Shape::BM, n = int64_t(tile.col) * Shape::BN;
     if (mat.tall) {
@@ -304,19 +304,21 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_gram_kernel
     for (int i = 0; i < Shape::MI; ++i)
 #pragma unroll
         for (int j = 0; j < Shape::NI; ++j) acc[i][j] *= 1.0f / kNsScale;
-    store_symmetric<Shape>(mat, mat.gram, tile, acc, lds);
+    store_symmetric<Shape>(mat, mat.gram[0], tile, acc, lds);
 }
 
 template <class Shape>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_poly_kernel(const NsMatrix *matrices,
                                                                   const NsTile *tiles,
-                                                                  NsStep step) {
+                                                                  NsTurn turn, NsStep step) {
     __shared__ __align__(1024) short lds[Shape::kLds];
     const NsTile tile = tiles[blockIdx.x];
     const NsMatrix mat = matrices[tile.matrix];
+    const bool odd = mat.chain && (turn.turn & 1);
+    const uint16_t *gram = odd ? mat.gram[1] : mat.gram[0];
     float4v acc[Shape::MI][Shape::NI] = {};
-    const Operand a = rows_of(mat.gram, mat.side_ld, int64_t(tile.row) * Shape::BM, mat.side);
-    const Operand b = rows_of(mat.gram, mat.side_ld, int64_t(tile.col) * Shape::BN, mat.side);
+    const Operand a = rows_of(gram, mat.side_ld, int64_t(tile.row) * Shape::BM, mat.side);
+    const Operand b = rows_of(gram, mat.side_ld, int64_t(tile.col) * Shape::BN, mat.side);
     tile_product<HalfMath, Shape, false, false>(acc, lds, a, b, mat.side, 2 * mat.gram_low,
                                                    2 * mat.gram_low);
     const Place<Shape> at;
@@ -328,7 +330,7 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_poly_kernel
 #pragma unroll
         for (int j = 0; j < Shape::NI; ++j) {
             const int n = tile.col * Shape::BN + at.col + 16 * j;
-            const uint16_t *from = mat.gram + int64_t(m < mat.side ? m : mat.side - 1) * mat.side_ld +
+            const uint16_t *from = gram + int64_t(m < mat.side ? m : mat.side - 1) * mat.side_ld +
                                    (n < mat.side_ld ? n : mat.side_ld - 4);
 #pragma unroll
             for (int p = 0; p < Shape::PARTS; ++p)
@@ -354,7 +356,45 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_poly_kernel
             }
         }
     }
-    store_symmetric<Shape>(mat, mat.poly, tile, acc, lds);
+    store_symmetric<Shape>(mat, odd ? mat.poly[1] : mat.poly[0], tile, acc, lds);
+}
+
+// Q, T and the next A of a chain.
+template <class Shape>
+__global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_product_kernel(
+    const NsMatrix *matrices, const NsTile *tiles, NsTurn turn) {
+    __shared__ __align__(1024) short lds[Shape::kLds];
+    const NsTile tile = tiles[blockIdx.x];
+    const NsMatrix mat = matrices[tile.matrix];
+    const bool odd = turn.turn & 1;
+    uint16_t *const p = odd ? mat.poly[1] : mat.poly[0];
+    uint16_t *const p_before = odd ? mat.poly[0] : mat.poly[1];
+    const uint16_t *left = p, *right;
+    uint16_t *out;
+    float back = 1.0f / kNsScale;
+    if (tile.product == kNsQ) {
+        // turn 1: q = P_1 P_0; turn 2: P_2 q, where P_1 was
+        right = turn.turn == 1 ? p_before : mat.q;
+        out = turn.turn == 1 ? mat.q : p_before;
+        back = turn.turn == 1 ? kNsQScale / (kNsScale * kNsScale) : 1.0f / kNsScale;
+    } else if (tile.product == kNsT) {
+        right = odd ? mat.gram[1] : mat.gram[0];
+        out = mat.t;
+    } else {
+        left = mat.t;
+        right = p;
+        out = odd ? mat.gram[0] : mat.gram[1];
+    }
+    float4v acc[Shape::MI][Shape::NI] = {};
+    tile_product<HalfMath, Shape, false, false>(
+        acc, lds, rows_of(left, mat.side_ld, int64_t(tile.row) * Shape::BM, mat.side),
+        rows_of(right, mat.side_ld, int64_t(tile.col) * Shape::BN, mat.side), mat.side,
+        2 * mat.gram_low, 2 * mat.gram_low);
+#pragma unroll
+    for (int i = 0; i < Shape::MI; ++i)
+#pragma unroll
+        for (int j = 0; j < Shape::NI; ++j) acc[i][j] *= back;
+    store_symmetric<Shape>(mat, out, tile, acc, lds);
 }
 
 __device__ inline float update_scale(const NsMatrix &mat, int32_t kind) {
@@ -368,33 +408,36 @@ __device__ inline float update_scale(const NsMatrix &mat, int32_t kind) {
 template <class Shape, int KIND>  // KIND: an NsKind, or -1 for the other X
 __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_update_kernel(const NsMatrix *matrices,
                                                                     const NsTile *tiles,
-                                                                    int parity, NsStep step,
+                                                                    NsTurn turn, NsStep step,
                                                                     const uint32_t *flag) {
     __shared__ __align__(1024) short lds[Shape::kLds];
     const NsTile tile = tiles[blockIdx.x];
     const NsMatrix mat = matrices[tile.matrix];
     if (KIND == kNsMuon && flag && flag[1])
         return;
-    const uint16_t *x = (parity ? mat.x[1] : mat.x[0]);
+    const int parity = mat.chain ? turn.parity[1] : turn.parity[0];
+    const uint16_t *x = parity ? mat.x[1] : mat.x[0];
+    const bool chained = mat.chain && turn.turn > 0;
+    const uint16_t *q = !chained ? mat.poly[0] : turn.turn == 1 ? mat.q : mat.poly[1];
     float4v acc[Shape::MI][Shape::NI] = {};
     const int64_t m0 = int64_t(tile.row) * Shape::BM, n0 = int64_t(tile.col) * Shape::BN;
     if (mat.tall) {
         const Operand a = rows_of(x, mat.ld, m0, mat.rows);
-        const Operand b = rows_of(mat.poly, mat.side_ld, n0, mat.side);
+        const Operand b = rows_of(q, mat.side_ld, n0, mat.side);
         tile_product<HalfMath, Shape, false, false>(acc, lds, a, b, mat.side, 2 * mat.x_low,
                                                    2 * mat.gram_low);
     } else {
-        const Operand a = rows_of(mat.poly, mat.side_ld, m0, mat.side);
+        const Operand a = rows_of(q, mat.side_ld, m0, mat.side);
         const Operand b = columns_of(x, mat.ld, n0);
         tile_product<HalfMath, Shape, false, true>(acc, lds, a, b, mat.side, 2 * mat.gram_low,
                                                    2 * mat.x_low);
     }
     const Place<Shape> at;
-    constexpr float kBack = KIND < 0 ? 1.0f / kNsScale : 1.0f / (kNsScale * kNsScale);
+    const float back = (KIND < 0 ? 1.0f : 1.0f / kNsScale) / (chained ? kNsQScale : kNsScale);
 #pragma unroll
     for (int i = 0; i < Shape::MI; ++i)
 #pragma unroll
-        for (int j = 0; j < Shape::NI; ++j) acc[i][j] *= kBack;
+        for (int j = 0; j < Shape::NI; ++j) acc[i][j] *= back;
     if (KIND < 0 || (KIND == kNsBf16Out && mat.vector && mat.cols % 8 == 0)) {
         const TileStore<Shape::BM, Shape::BN, Shape::kThreads> store(lds);
         uint16_t *to = KIND < 0 ? (parity ? mat.x[0] : mat.x[1]) : (uint16_t *)mat.out;
@@ -529,23 +572,32 @@ hipError_t with_shape(int shape, bool split, F f) {
 }  // namespace
 
 hipError_t launch_ns_gram(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
-                          bool split, int parity, hipStream_t stream) {
+                          bool split, const NsTurn &turn, hipStream_t stream) {
     return with_shape(shape, split, [&](auto s) {
         using Shape = decltype(s);
-        ns_gram_kernel<Shape><<<n, Shape::kThreads, 0, stream>>>(matrices, tiles, parity);
+        ns_gram_kernel<Shape><<<n, Shape::kThreads, 0, stream>>>(matrices, tiles, turn);
+    });
+}
+
+hipError_t launch_ns_product(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
+                             bool split, const NsTurn &turn, hipStream_t stream) {
+    return with_shape(shape, split, [&](auto s) {
+        using Shape = decltype(s);
+        ns_product_kernel<Shape><<<n, Shape::kThreads, 0, stream>>>(matrices, tiles, turn);
     });
 }
 
 hipError_t launch_ns_poly(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
-                          bool split, const NsStep &step, hipStream_t stream) {
+                          bool split, const NsTurn &turn, const NsStep &step,
+                          hipStream_t stream) {
     return with_shape(shape, split, [&](auto s) {
         using Shape = decltype(s);
-        ns_poly_kernel<Shape><<<n, Shape::kThreads, 0, stream>>>(matrices, tiles, step);
+        ns_poly_kernel<Shape><<<n, Shape::kThreads, 0, stream>>>(matrices, tiles, turn, step);
     });
 }
 
 hipError_t launch_ns_update(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
-                            bool split, int parity, bool last, NsKind kind, const NsStep &step,
+                            bool split, const NsTurn &turn, bool last, NsKind kind, const NsStep &step,
                             const uint32_t *flag, hipStream_t stream) {
     return with_shape(shape, split, [&](auto s) {
         using Shape = decltype(s);
@@ -553,7 +605,7 @@ hipError_t launch_ns_update(const NsMatrix *matrices, const NsTile *tiles, int32
                       : kind == kNsBf16Out ? ns_update_kernel<Shape, kNsBf16Out>
                       : kind == kNsF32Out  ? ns_update_kernel<Shape, kNsF32Out>
                                            : ns_update_kernel<Shape, kNsMuon>;
-        kernel<<<n, Shape::kThreads, 0, stream>>>(matrices, tiles, parity, step, flag);
+        kernel<<<n, Shape::kThreads, 0, stream>>>(matrices, tiles, turn, step, flag);
     });
 }
 

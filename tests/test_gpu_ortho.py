@@ -63,6 +63,28 @@ def test_lists_that_take_the_larger_tiles(dtype, tol):
             assert R.relative(outs[i], R.newton_schulz(gs[i])) < tol, (i, shapes[i])
 
 
+@pytest.mark.parametrize("dtype,count,tol", [("float32", 80, SPLIT), ("bfloat16", 320, HALF)])
+@pytest.mark.parametrize("steps", [1, 2, 3, 4, 5, 6, 7])
+def test_long_lists_of_long_matrices_iterate_in_chains(dtype, count, tol, steps):
+    """Enough work in matrices twice as long as wide that their iterations run on the
+    short side; square ones in the same list do not. Some are of low rank and noise, a
+    few with singular values over four decades (held to the tolerance of those)."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    shapes = [(256, 1024)] * count + [(1030, 257), (515, 256), (300, 300), (259, 130)]
+    gs = _make(torch, shapes, getattr(torch, dtype), seed=steps)
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    u, v = (torch.randn(256, 16, generator=gen, device="cuda"),
+            torch.randn(16, 1024, generator=gen, device="cuda"))
+    gs[3].add_((u @ v).to(gs[3].dtype), alpha=2e-4)
+    gs[5].mul_(torch.logspace(0, -4, 256, device="cuda")[:, None].to(gs[5].dtype))
+    outs = ops.Orthogonalizer(gs, steps=steps).run()
+    for i in (0, 1, 3, 5, count - 1, count, count + 1, count + 2, count + 3):
+        loose = 5 if i in (3, 5) else 1
+        err = R.relative(outs[i], R.newton_schulz(gs[i], steps))
+        assert err < loose * tol * (1 if steps <= 5 else 2), (i, shapes[i], err)
+
+
 @pytest.mark.parametrize("steps", [1, 2, 8])
 def test_steps_and_coefficients(steps):
     torch = torch_cuda()
