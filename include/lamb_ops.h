@@ -72,8 +72,9 @@ typedef struct lamb_matrix {
 } lamb_matrix;
 
 /* A list of matrices that are worked on together, with their workspace: about
- * 4 bytes per element and 4 per entry of the short sides' squares (twice that
- * with LAMB_NS_SPLIT). One call may be in flight per plan; not thread-safe. */
+ * 4 bytes per element and 4 per entry of the short sides' squares (12 for matrices
+ * at least twice as long as wide in lists with much to do), twice that with
+ * LAMB_NS_SPLIT. One call may be in flight per plan; not thread-safe. */
 typedef struct lamb_ns_plan lamb_ns_plan;
 
 /*

@@ -34,7 +34,7 @@ lamb_status check_matrix(const char *what, const void *p, int64_t rows, int64_t 
     if (rows && !p)
         return fail(LAMB_ENULL, "%s must not be NULL", what);
     if (stride < dim || stride > kMaxStride)
-        return fail(LAMB_EINVAL, "%s: the row stride is below dim, or above 2^40", what);
+        return fail(LAMB_EINVAL, "%s: the row stride is below dim, or above 2^36", what);
     if (!aligned_to(p, uintptr_t(size_of(dtype))))
         return fail(LAMB_EALIGN, "%s is not aligned to its elements", what);
     return LAMB_OK;

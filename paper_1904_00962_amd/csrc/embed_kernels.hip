@@ -19,6 +19,7 @@
 #include <type_traits>
 
 #include "embed_internal.h"
+#include "ops_host.h"
 
 namespace lamb_mi355x {
 namespace {
@@ -93,7 +94,8 @@ __device__ inline void store8(void *base, int64_t at, int n, bool vector, const 
 template <bool TABLE_BF16, bool OUT_BF16>
 __global__ __launch_bounds__(256) void embed_kernel(EmbedArgs a, EmbedRows r) {
     const uint32_t per_row = uint32_t(a.dim + 7) / 8;
-    const int64_t unit = int64_t(blockIdx.x) * 256 + threadIdx.x;
+    const int64_t unit =
+        (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * 256 + threadIdx.x;
     const int64_t units = a.tokens * per_row;
     if (unit >= units)
         return;
@@ -211,6 +213,8 @@ __global__ __launch_bounds__(kSortWaves * 64) void embed_sort_kernel(EmbedArgs a
                 if (lane == leader)
                     mine[which] = place + __popcll(same);
                 todo &= ~same;
+                // the next reader of this place may be another lane
+                __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
             }
         }
     }
@@ -350,11 +354,10 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, EmbedGrad 
 
 hipError_t launch_embed(const EmbedArgs &args, const EmbedRows &rows, hipStream_t stream) {
     const int64_t units = args.tokens * ((args.dim + 7) / 8);
-    const uint32_t blocks = uint32_t((units + 255) / 256);
     auto kernel = rows.table_bf16
                       ? (rows.out_bf16 ? embed_kernel<true, true> : embed_kernel<true, false>)
                       : (rows.out_bf16 ? embed_kernel<false, true> : embed_kernel<false, false>);
-    kernel<<<blocks, 256, 0, stream>>>(args, rows);
+    kernel<<<grid_of((units + 255) / 256), 256, 0, stream>>>(args, rows);
     return hipGetLastError();
 }
 
@@ -369,7 +372,8 @@ hipError_t launch_embed_sort(const EmbedArgs &args, int64_t skip, int32_t *order
 
 hipError_t launch_embed_sum(const EmbedArgs &args, const EmbedGrad &grad, hipStream_t stream) {
     const int64_t chunks = (args.tokens + kSumTokens - 1) / kSumTokens;
-    const int64_t waves = chunks * (grad.columns / kSumColumns) + (grad.add ? 0 : (args.vocab + kZeroRows - 1) / kZeroRows);
+    const int64_t zeros = grad.add ? 0 : (args.vocab + kZeroRows - 1) / kZeroRows;
+    const int64_t waves = chunks * (grad.columns / kSumColumns) + zeros;
     auto kernel =
         grad.rows_bf16
             ? (grad.table_bf16 ? embed_sum_kernel<true, true> : embed_sum_kernel<true, false>)

@@ -108,7 +108,9 @@ struct TileShape {
     static constexpr bool kAlternating = BM == 256;
     // workgroups per CU: what LDS allows, and at most two
     static constexpr int kPerCu = 160 * 1024 / (kLds * 2) >= 2 ? 2 : 1;
-    static_assert(DEPTH % 32 == 0 && STAGES >= 2 && kLds * 2 <= 160 * 1024 && kLoads * (STAGES - 2) < 64, "");
+    static_assert(DEPTH % 32 == 0 && STAGES >= 2 && kLds * 2 <= 160 * 1024 &&
+                      kLoads * (STAGES - 2) < 64,
+                  "");
 };
 
 // Bank swizzle of a `rows` stage: 8 rows at the same k get different banks.

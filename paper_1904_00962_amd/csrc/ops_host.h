@@ -32,6 +32,14 @@ std::vector<T> spread_over_dies(const std::vector<T> &items) {
     return out;
 }
 
+// A launch has fewer than 2^32 threads along an axis: many workgroups go along two, and
+// those past `blocks` find nothing to do.
+inline dim3 grid_of(int64_t blocks) {
+    constexpr int64_t kAxis = int64_t(1) << 21;
+    return blocks <= kAxis ? dim3(uint32_t(blocks))
+                           : dim3(uint32_t(kAxis), uint32_t((blocks + kAxis - 1) / kAxis));
+}
+
 // Runs an entry point's body; what it throws becomes a status.
 template <class F>
 lamb_status guarded(F body) noexcept {
@@ -84,9 +92,10 @@ inline lamb_status check_spans(Span *spans, size_t n) {
     return LAMB_OK;
 }
 
-// The limits that the operators' entry points share.
+// The limits that the operators' entry points share. Rows times stride times 8 bytes stay
+// below 2^63.
 constexpr int64_t kMaxTokens = int64_t(1) << 24, kMaxVocab = int64_t(1) << 24,
-                  kMaxDim = int64_t(1) << 16, kMaxStride = int64_t(1) << 40;
+                  kMaxDim = int64_t(1) << 16, kMaxStride = int64_t(1) << 36;
 
 inline bool is_float(int32_t dtype) {
     return dtype == LAMB_DTYPE_F32 || dtype == LAMB_DTYPE_BF16;

@@ -111,7 +111,7 @@ hipError_t launch_ns_product(const NsMatrix *matrices, const NsTile *tiles, int3
                              bool split, const NsTurn &turn, hipStream_t stream);
 // `last`: the result goes to `out` as `kind` says, else to the other X.
 hipError_t launch_ns_update(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
-                            bool split, const NsTurn &turn, bool last, NsKind kind, const NsStep &step,
-                            const uint32_t *flag, hipStream_t stream);
+                            bool split, const NsTurn &turn, bool last, NsKind kind,
+                            const NsStep &step, const uint32_t *flag, hipStream_t stream);
 
 }  // namespace lamb_mi355x

@@ -6,7 +6,8 @@
 // values. Of A and P, which are symmetric, only tiles on and below the diagonal are
 // computed; each is written to its mirror's place too. One launch covers the tiles
 // of every matrix of a plan, so an iteration is three launches however many
-// matrices there are.
+// matrices there are. Long matrices of lists with much to do iterate on their short side
+// in chains (ortho_internal.h).
 //
 // X, A and P are held in 16-bit floats (11 significant bits; with bfloat16's 8 the
 // result would be 1e-2 off instead of 1.3e-3), scaled by a power of two; sums are
@@ -280,9 +281,8 @@ __device__ inline void store_symmetric(const NsMatrix &mat, uint16_t *to, const 
 }
 
 template <class Shape>
-__global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_gram_kernel(const NsMatrix *matrices,
-                                                                  const NsTile *tiles,
-                                                                  NsTurn turn) {
+__global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_gram_kernel(
+    const NsMatrix *matrices, const NsTile *tiles, NsTurn turn) {
     __shared__ __align__(1024) short lds[Shape::kLds];
     const NsTile tile = tiles[blockIdx.x];
     const NsMatrix mat = matrices[tile.matrix];
@@ -308,9 +308,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_gram_kernel
 }
 
 template <class Shape>
-__global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_poly_kernel(const NsMatrix *matrices,
-                                                                  const NsTile *tiles,
-                                                                  NsTurn turn, NsStep step) {
+__global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_poly_kernel(
+    const NsMatrix *matrices, const NsTile *tiles, NsTurn turn, NsStep step) {
     __shared__ __align__(1024) short lds[Shape::kLds];
     const NsTile tile = tiles[blockIdx.x];
     const NsMatrix mat = matrices[tile.matrix];
@@ -406,10 +405,9 @@ __device__ inline float update_scale(const NsMatrix &mat, int32_t kind) {
 }
 
 template <class Shape, int KIND>  // KIND: an NsKind, or -1 for the other X
-__global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_update_kernel(const NsMatrix *matrices,
-                                                                    const NsTile *tiles,
-                                                                    NsTurn turn, NsStep step,
-                                                                    const uint32_t *flag) {
+__global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_update_kernel(
+    const NsMatrix *matrices, const NsTile *tiles, NsTurn turn, NsStep step,
+    const uint32_t *flag) {
     __shared__ __align__(1024) short lds[Shape::kLds];
     const NsTile tile = tiles[blockIdx.x];
     const NsMatrix mat = matrices[tile.matrix];
@@ -494,7 +492,8 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void ns_update_kern
                     xs[0] = t.x, xs[1] = t.y, xs[2] = t.z, xs[3] = t.w;
                 } else {
 #pragma unroll
-                    for (int r = 0; r < 4; ++r) xs[r] = n + r < mat.cols ? load_global<float>(out + r) : 0.0f;
+                    for (int r = 0; r < 4; ++r)
+                        xs[r] = n + r < mat.cols ? load_global<float>(out + r) : 0.0f;
                 }
 #pragma unroll
                 for (int r = 0; r < 4; ++r) v[r] = __builtin_fmaf(move, v[r], keep * xs[r]);
@@ -544,7 +543,8 @@ hipError_t launch_ns_convert(const NsMatrix *matrices, const int32_t *block_matr
                              hipStream_t stream) {
     auto pick = [&](auto split_c) {
         constexpr bool S = decltype(split_c)::value;
-        return muon ? (bf16_in ? ns_convert_kernel<true, true, S> : ns_convert_kernel<true, false, S>)
+        return muon ? (bf16_in ? ns_convert_kernel<true, true, S>
+                               : ns_convert_kernel<true, false, S>)
                     : (bf16_in ? ns_convert_kernel<false, true, S>
                                : ns_convert_kernel<false, false, S>);
     };
@@ -597,8 +597,8 @@ hipError_t launch_ns_poly(const NsMatrix *matrices, const NsTile *tiles, int32_t
 }
 
 hipError_t launch_ns_update(const NsMatrix *matrices, const NsTile *tiles, int32_t n, int shape,
-                            bool split, const NsTurn &turn, bool last, NsKind kind, const NsStep &step,
-                            const uint32_t *flag, hipStream_t stream) {
+                            bool split, const NsTurn &turn, bool last, NsKind kind,
+                            const NsStep &step, const uint32_t *flag, hipStream_t stream) {
     return with_shape(shape, split, [&](auto s) {
         using Shape = decltype(s);
         auto kernel = !last ? ns_update_kernel<Shape, -1>

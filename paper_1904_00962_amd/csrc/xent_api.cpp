@@ -31,7 +31,7 @@ lamb_status check(const lamb_xent *x) {
         return fail(LAMB_ENULL, "hidden, table and targets must not be NULL");
     if (x->hidden_stride < x->dim || x->table_stride < x->dim || x->hidden_stride > kMaxStride ||
         x->table_stride > kMaxStride)
-        return fail(LAMB_EINVAL, "a row stride is below dim, or above 2^40");
+        return fail(LAMB_EINVAL, "a row stride is below dim, or above 2^36");
     if (!aligned_to(x->hidden, 2) || !aligned_to(x->table, 2) ||
         !aligned_to(x->targets, uintptr_t(size_of(x->target_dtype))))
         return fail(LAMB_EALIGN, "a pointer is not aligned to its elements");
@@ -158,6 +158,7 @@ lamb_status begin(const lamb_xent &x, const Layout &l, char *work, float *loss, 
     pack.ld = int32_t(l.ld);
     pack.vocab = int32_t(x.vocab);
     pack.tokens = int32_t(x.tokens);
+    pack.rounds = pack_rounds(x.tokens);
     pack.packed = reinterpret_cast<uint16_t *>(work + l.packed);
     pack.kept = reinterpret_cast<int32_t *>(work + l.kept);
     pack.source = reinterpret_cast<int32_t *>(work + l.source);
@@ -271,7 +272,7 @@ lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
         return fail(LAMB_EINVAL, "grad_table is float32 or bfloat16");
     if ((g.grad_hidden && (g.grad_hidden_stride < x.dim || g.grad_hidden_stride > kMaxStride)) ||
         (g.grad_table && (g.grad_table_stride < x.dim || g.grad_table_stride > kMaxStride)))
-        return fail(LAMB_EINVAL, "a row stride is below dim, or above 2^40");
+        return fail(LAMB_EINVAL, "a row stride is below dim, or above 2^36");
     if (!aligned_to(g.grad_loss, 4) || !aligned_to(lse, 4) || !aligned_to(g.grad_hidden, 2) ||
         !aligned_to(g.grad_table, bf16 ? 2 : 4))
         return fail(LAMB_EALIGN, "a pointer is not aligned to its elements");

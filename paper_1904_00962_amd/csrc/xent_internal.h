@@ -12,7 +12,17 @@ namespace lamb_mi355x {
 enum XentShape : int32_t { kXentTiny = 0, kXentSmall = 1, kXentLarge = 2 };
 constexpr int32_t xent_tile(int32_t shape) { return 64 << shape; }
 
-constexpr int kPackTokens = 16;    // tokens per workgroup of the packing pass
+// Tokens that a workgroup of the packing pass takes at once, and how often it does. Each
+// counts the tokens before its own first, so there are at most 1024 workgroups, four to a
+// CU: the work of counting then grows as the tokens do. A call of 2^20 tokens and 64
+// columns against 64 words takes 1.0 ms so, 14.8 with one group to a workgroup; of 65536
+// 72 and 113 us.
+constexpr int kPackTokens = 16;
+constexpr int32_t pack_rounds(int64_t tokens) {
+    return tokens > 1024 * kPackTokens
+               ? int32_t((tokens + 1024 * kPackTokens - 1) / (1024 * kPackTokens))
+               : 1;
+}
 constexpr int kReduceTokens = 16;  // tokens per workgroup of the logsumexp pass
 
 // What every pass of a call reads. `hidden` is the packed copy of the tokens that
@@ -36,6 +46,7 @@ struct XentPack {
     int32_t vector;
     int64_t ignore;
     int32_t dim, ld, vocab, tokens;
+    int32_t rounds;
     uint16_t *packed;
     int32_t *kept, *source, *target;
     float *loss, *lse;           // forward: of the tokens that do not count, 0

@@ -22,6 +22,7 @@
 #include <type_traits>
 
 #include "mma_tile.h"
+#include "ops_host.h"
 #include "xent_internal.h"
 
 namespace lamb_mi355x {
@@ -41,9 +42,14 @@ __device__ inline float widen(uint16_t v) { return __uint_as_float(uint32_t(v) <
 // The workgroup's tile of rows x cols tiles. Workgroups go to the dies in turn; each
 // die gets a run of tiles, kGroupRows rows tall, that share operand rows in its L2.
 struct TileAt {
-    int row, col;
+    int row, col;  // row >= rows: none
     __device__ TileAt(int rows, int cols) {
-        const uint32_t n = gridDim.x, b = blockIdx.x;
+        const uint32_t n = uint32_t(rows) * uint32_t(cols);
+        const uint32_t b = blockIdx.y * gridDim.x + blockIdx.x;
+        if (b >= n) {
+            row = rows, col = 0;
+            return;
+        }
         const uint32_t die = b % kXcdCount, each = n / kXcdCount, more = n % kXcdCount;
         const uint32_t item = die * each + (die < more ? die : more) + b / kXcdCount;
         const uint32_t band = item / (kGroupRows * cols), in = item % (kGroupRows * cols);
@@ -86,43 +92,50 @@ __global__ __launch_bounds__(256) void xent_pack_kernel(XentPack a) {
     __shared__ int32_t before[4];
     __shared__ int32_t row_of[kPackTokens];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t first = int64_t(blockIdx.x) * kPackTokens;
+    const int64_t begin = int64_t(blockIdx.x) * kPackTokens * a.rounds;
     int32_t count = 0;
 #pragma unroll 8
-    for (int64_t i = threadIdx.x; i < first; i += 256) count += target_of(a, i) != a.ignore;
+    for (int64_t i = threadIdx.x; i < begin; i += 256) count += target_of(a, i) != a.ignore;
 #pragma unroll
     for (int d = 32; d; d >>= 1) count += __shfl_xor(count, d);
     if (lane == 0)
         before[wave] = count;
     __syncthreads();
-    if (wave == 0) {
-        int32_t base = before[0] + before[1] + before[2] + before[3];
-        const int64_t i = first + lane;
-        const int64_t t = i < a.tokens ? target_of(a, i) : a.ignore;
-        const bool counts = lane < kPackTokens && t != a.ignore;
-        const uint64_t mask = __ballot(counts);
-        const int32_t row = base + __popcll(mask & ((uint64_t(1) << lane) - 1));
-        if (lane < kPackTokens)
-            row_of[lane] = counts ? row : -1;
-        if (counts) {
-            a.source[row] = int32_t(i);
-            a.target[row] = t >= 0 && t < a.vocab ? int32_t(t) : -1;
-        } else if (lane < kPackTokens && i < a.tokens && a.loss) {
-            a.loss[i] = 0.0f;
-            a.lse[i] = 0.0f;
+    int32_t base = before[0] + before[1] + before[2] + before[3];
+    for (int32_t round = 0; round < a.rounds; ++round) {
+        const int64_t first = begin + int64_t(round) * kPackTokens;
+        if (first >= a.tokens && first > 0)
+            return;
+        if (wave == 0) {
+            const int64_t i = first + lane;
+            const int64_t t = i < a.tokens ? target_of(a, i) : a.ignore;
+            const bool counts = lane < kPackTokens && t != a.ignore;
+            const uint64_t mask = __ballot(counts);
+            const int32_t row = base + __popcll(mask & ((uint64_t(1) << lane) - 1));
+            if (lane < kPackTokens)
+                row_of[lane] = counts ? row : -1;
+            if (counts) {
+                a.source[row] = int32_t(i);
+                a.target[row] = t >= 0 && t < a.vocab ? int32_t(t) : -1;
+            } else if (lane < kPackTokens && i < a.tokens && a.loss) {
+                a.loss[i] = 0.0f;
+                a.lse[i] = 0.0f;
+            }
+            base += __popcll(mask);
+            if (first + kPackTokens >= a.tokens && lane == 0)
+                *a.kept = base;
         }
-        if (first + kPackTokens >= a.tokens && lane == 0)
-            *a.kept = base + __popcll(mask);
-    }
-    __syncthreads();
-    for (int t = wave; t < kPackTokens && first + t < a.tokens; t += 4) {
-        if (row_of[t] >= 0) {
-            copy_row(a.hidden + (first + t) * a.stride, a.packed + int64_t(row_of[t]) * a.ld,
-                     a.dim, a.ld, a.vector, lane);
-        } else if (a.grad_hidden) {
-            uint16_t *out = a.grad_hidden + (first + t) * a.grad_stride;
-            for (int c = lane; c < a.dim; c += 64) out[c] = 0;
+        __syncthreads();
+        for (int t = wave; t < kPackTokens && first + t < a.tokens; t += 4) {
+            if (row_of[t] >= 0) {
+                copy_row(a.hidden + (first + t) * a.stride, a.packed + int64_t(row_of[t]) * a.ld,
+                         a.dim, a.ld, a.vector, lane);
+            } else if (a.grad_hidden) {
+                uint16_t *out = a.grad_hidden + (first + t) * a.grad_stride;
+                for (int c = lane; c < a.dim; c += 64) out[c] = 0;
+            }
         }
+        __syncthreads();
     }
 }
 
@@ -358,8 +371,9 @@ __global__ __launch_bounds__(256) void xent_hidden_out_kernel(XentArgs a, int32_
                                                               int64_t stride) {
     const int32_t kept = *a.kept;
     const int across = tiles_of(a.dim, 1024);
-    const int m = int(blockIdx.x) / across;
-    const int n = (int(blockIdx.x) % across * 256 + threadIdx.x) * 4;
+    const uint32_t block = blockIdx.y * gridDim.x + blockIdx.x;
+    const int m = int(block / across);
+    const int n = (int(block % across) * 256 + threadIdx.x) * 4;
     if (m >= kept || n >= a.dim)
         return;
     const float scale = final_scale(grad_loss, grad_scale, mean, kept);
@@ -462,7 +476,7 @@ int64_t tiles(int64_t rows, int64_t cols, int shape) {
 
 hipError_t launch_xent_pack(const XentPack &args, hipStream_t stream) {
     // one workgroup at least: it writes the count
-    const int blocks = args.tokens ? tiles_of(args.tokens, kPackTokens) : 1;
+    const int blocks = args.tokens ? tiles_of(args.tokens, kPackTokens * args.rounds) : 1;
     xent_pack_kernel<<<blocks, 256, 0, stream>>>(args);
     return hipGetLastError();
 }
@@ -478,7 +492,7 @@ hipError_t launch_xent_logits(const XentArgs &args, int shape, float2 *parts, fl
     return with_shape(shape, [&](auto s) {
         using Shape = decltype(s);
         xent_logits_kernel<Shape>
-            <<<uint32_t(tiles(args.tokens, args.vocab, shape)), Shape::kThreads, 0, stream>>>(
+            <<<grid_of(tiles(args.tokens, args.vocab, shape)), Shape::kThreads, 0, stream>>>(
                 args, parts, at_target);
     });
 }
@@ -520,9 +534,9 @@ hipError_t launch_xent_hidden(const XentArgs &args, int shape, const XentPiece &
 hipError_t launch_xent_hidden_out(const XentArgs &args, int32_t splits, const float *partial,
                                   const float *grad_loss, float grad_scale, bool mean,
                                   uint16_t *grad_hidden, int64_t stride, hipStream_t stream) {
-    const uint32_t grid = uint32_t(tiles_of(args.dim, 1024)) * uint32_t(args.tokens);
-    xent_hidden_out_kernel<<<grid, 256, 0, stream>>>(args, splits, partial, grad_loss, grad_scale,
-                                                     mean, grad_hidden, stride);
+    const int64_t blocks = int64_t(tiles_of(args.dim, 1024)) * args.tokens;
+    xent_hidden_out_kernel<<<grid_of(blocks), 256, 0, stream>>>(
+        args, splits, partial, grad_loss, grad_scale, mean, grad_hidden, stride);
     return hipGetLastError();
 }
 

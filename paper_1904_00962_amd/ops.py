@@ -88,7 +88,8 @@ class Orthogonalizer:
     float32 outputs, and "half" for bfloat16 ones, whose own rounding is 1.7e-3, unless
     the list has a matrix of short side below 64: its few roundings do not average out
     (2.1e-3 off, 1.3e-3 from 128 on), and such lists are short work.
-    The plan keeps a workspace of about 4 bytes per element (8 for "split").
+    The plan keeps a workspace of about 4 bytes per element, and 4 to 12 per entry of the
+    short sides' squares; twice that for "split".
     """
 
     def __init__(self, inputs: Sequence, outputs: Optional[Sequence] = None, steps: int = 5,

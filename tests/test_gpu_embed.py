@@ -2,7 +2,7 @@
 
 Tolerances. A looked-up value is a product in fp32, rounded once more to its type: it
 is compared with exactly that. A gradient is a sum of n terms in fp32 (off by at most
-n 2^-24 of the sum of magnitudes), rounded to its type (2^-9 for bf16)."""
+n 2^-24 of the sum of magnitudes), rounded to its type (half a unit of bf16's last place)."""
 
 import math
 
@@ -228,3 +228,18 @@ def test_refusals():
     with pytest.raises(_lib.LambError) as e:
         ops.embedding(ids, table, out=table[:4])
     assert e.value.status == _lib.LAMB_EOVERLAP
+
+
+def test_lookup_past_one_axis_of_workgroups():
+    """2^32 units of eight columns and more."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    tokens, dim, vocab = (1 << 19) + 3, 1 << 16, 5
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    table = torch.randn(vocab, dim, generator=gen, device="cuda").to(torch.bfloat16)
+    ids = torch.arange(tokens, device="cuda") % vocab
+    out = ops.embedding(ids, table)
+    assert out.dtype == torch.bfloat16
+    for first in range(0, tokens, 1 << 16):
+        part = out[first:first + (1 << 16)]
+        assert torch.equal(part, table[ids[first:first + (1 << 16)]])

@@ -266,3 +266,35 @@ def test_muon_schedule():
     want, _ = R.muon_step(xs[0], gs[0], ms[0], _lib.lamb_lr_at(stages, 1), 0.95)
     opt.step()
     assert R.relative(xs[0], want) < 1e-6
+
+
+@pytest.mark.parametrize("fields,words", [
+    (dict(steps=0), "steps"), (dict(steps=65), "steps"), (dict(eps=-1.0), "eps"),
+    (dict(a=math.nan), "finite"), (dict(reserved=1), "reserved"),
+    (dict(a=1e4), "polynomial"), (dict(a=3.4445, b=0.0, c=0.0), "singular value"),
+])
+def test_iteration_bounds(fields, words):
+    """Among them coefficients that let the iteration leave the range of its operands."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import _lib, _ops, ops
+    g = torch.ones(4, 8, device="cuda")
+    o = ops.Orthogonalizer([g])
+    with pytest.raises(_lib.LambError, match=words):
+        _ops.lamb_orthogonalize(o.plan, _ops.lamb_ns_params_init(**fields), 0)
+
+
+def test_muon_scalars():
+    torch = torch_cuda()
+    from paper_1904_00962_amd import _lib, _ops
+    x, m = torch.ones(4, 8, device="cuda"), torch.zeros(4, 8, device="cuda")
+    g = torch.ones(4, 8, device="cuda")
+    row = (x.data_ptr(), g.data_ptr(), m.data_ptr(), 4, 8, 1)
+    plan = _ops.lamb_muon_plan_create([row], _ops.LAMB_DTYPE_F32, _ops.LAMB_NS_HALF)
+    for fields in (dict(lr=-1.0), dict(lr=math.nan), dict(momentum=1.0), dict(weight_decay=-0.1),
+                   dict(grad_scale=0.0), dict(nesterov=2), dict(scale=3), dict(skip_nonfinite=-1),
+                   dict(reserved=1)):
+        with pytest.raises(_lib.LambError):
+            _ops.lamb_muon_step(plan, _ops.lamb_muon_hparams_init(**fields), 0)
+    torch.cuda.synchronize()
+    plan.close()
+    assert x.eq(1).all() and m.eq(0).all()

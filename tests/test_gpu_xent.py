@@ -254,3 +254,48 @@ def test_refusals():
     assert e.value.status == _lib.LAMB_EOVERLAP
     with pytest.raises(ValueError):
         ops.linear_cross_entropy_grad(h, w, t, lse, reduction="none")
+
+
+def _sampled_lse(torch, h, w, rows):
+    return torch.logsumexp(h[rows].double().cpu() @ w.double().cpu().t(), dim=1)
+
+
+def test_many_tokens_and_words():
+    """More workgroups than a launch takes along one axis, several groups of tokens packed
+    by each, and parts past 2^32 bytes."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    tokens, dim, vocab = 1 << 22, 8, 1 << 18
+    h, w, t = _problem(torch, tokens, dim, vocab, ignored=0.25)
+    mean, loss, lse = ops.linear_cross_entropy(h, w, t)
+    keep = t != -100
+    rows = torch.nonzero(keep)[:, 0]
+    rows = torch.cat([rows[:40], rows[len(rows) // 2:][:40], rows[-40:]])
+    want = _sampled_lse(torch, h, w, rows)
+    mine = (h[rows].double() * w[t[rows]].double()).sum(1).cpu()
+    assert float((lse[rows].cpu().double() - want).abs().max()) < 4e-5
+    assert float((loss[rows].cpu().double() - (want - mine)).abs().max()) < 4e-5
+    assert bool(loss[~keep].eq(0).all()) and bool(loss[keep].gt(0).all())
+    assert abs(float(mean) - float(loss.double().sum() / keep.sum())) < 1e-5
+
+
+def test_gradient_of_the_most_tokens():
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    tokens, dim, vocab = 1 << 24, 8, 8
+    h, w, t = _problem(torch, tokens, dim, vocab, ignored=0.25)
+    logits = h.float() @ w.float().t().contiguous()
+    lse = torch.logsumexp(logits, dim=1)
+    gh = torch.full_like(h, math.nan)
+    gw = torch.full(w.shape, math.nan, device="cuda")
+    ops.linear_cross_entropy_grad(h, w, t, lse, gh, gw, reduction="sum")
+    q = torch.exp(logits - lse[:, None])
+    q.scatter_add_(1, t.clamp(min=0)[:, None], torch.full((tokens, 1), -1.0, device="cuda"))
+    q.mul_((t != -100)[:, None])
+    want = q @ w.float()
+    size = q.abs() @ w.float().abs()
+    assert bool(((gh.float() - want).abs() <= 2 * GRAD * size + 1e-6).all())
+    assert bool(gh[t == -100].eq(0).all())
+    q, size = q.t().contiguous(), q.abs().t().contiguous()
+    off = float(torch.linalg.vector_norm(gw - q @ h.float()))
+    assert off <= GRAD * float(torch.linalg.vector_norm(size @ h.float().abs()))

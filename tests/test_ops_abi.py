@@ -118,3 +118,100 @@ def test_defaults(lib):
     with pytest.raises(AttributeError):
         _ops.lamb_muon_hparams_init(beta=1)
     assert math.isclose(hp.momentum, 0.95, rel_tol=1e-6)
+
+
+def _xent(**fields):
+    x = _ops.lamb_xent(A, A + (1 << 24), A + (1 << 25), 64, 64, 10, 20, 64, -100,
+                       _ops.LAMB_DTYPE_I64, 0)
+    for k, v in fields.items():
+        setattr(x, k, v)
+    return x
+
+
+@pytest.mark.parametrize("fields,status", [
+    (dict(tokens=-1), _lib.LAMB_EINVAL), (dict(tokens=(1 << 24) + 1), _lib.LAMB_EINVAL),
+    (dict(vocab=0), _lib.LAMB_EINVAL), (dict(dim=0), _lib.LAMB_EINVAL),
+    (dict(dim=(1 << 16) + 1), _lib.LAMB_EINVAL), (dict(hidden_stride=63), _lib.LAMB_EINVAL),
+    (dict(table_stride=63), _lib.LAMB_EINVAL), (dict(target_dtype=0), _lib.LAMB_EINVAL),
+    (dict(hidden_stride=1 << 40, tokens=1 << 24), _lib.LAMB_EINVAL),
+    (dict(reserved=1), _lib.LAMB_EINVAL), (dict(table=None), _lib.LAMB_ENULL),
+    (dict(hidden=None), _lib.LAMB_ENULL), (dict(targets=None), _lib.LAMB_ENULL),
+    (dict(hidden=A + 1), _lib.LAMB_EALIGN), (dict(targets=A + 4), _lib.LAMB_EALIGN),
+])
+def test_cross_entropy_refusals(lib, fields, status):
+    x = _xent(**fields)
+    for call in (lambda: _ops.lamb_xent_workspace(x, False),
+                 lambda: _ops.lamb_xent_forward(x, A, A, A, A, 1 << 40),
+                 lambda: _ops.lamb_xent_backward(x, A, _ops.lamb_xent_grads(), A, 1 << 40)):
+        _refused(status, call)
+
+
+def test_cross_entropy_buffers(lib):
+    x, far = _xent(), A + (1 << 30)
+    need = _ops.lamb_xent_workspace(x, False)
+    back = _ops.lamb_xent_workspace(x, True)
+    assert need > 0 and back > 0 and need % 256 == 0
+    fwd = lambda loss, lse, mean, work, size: _ops.lamb_xent_forward(  # noqa: E731
+        x, loss, lse, mean, work, size)
+    _refused(_lib.LAMB_ENULL, lambda: fwd(0, far, 0, far, need))
+    _refused(_lib.LAMB_ENULL, lambda: fwd(far, far + 64, 0, 0, need))
+    _refused(_lib.LAMB_EALIGN, lambda: fwd(far, far + 64, 0, far + 128, need))
+    _refused(_lib.LAMB_EALIGN, lambda: fwd(far + 2, far + 64, 0, far + 256, need))
+    _refused(_lib.LAMB_EINVAL, lambda: fwd(far, far + 64, 0, far + 256, need - 1), "workspace")
+    _refused(_lib.LAMB_EOVERLAP, lambda: fwd(far, far + 36, 0, far + 256, need))
+    _refused(_lib.LAMB_EOVERLAP, lambda: fwd(far, far + 64, A, far + 256, need))
+    for fields, status in ((dict(add_table=2), _lib.LAMB_EINVAL), (dict(mean=-1), _lib.LAMB_EINVAL),
+                           (dict(grad_scale=math.inf), _lib.LAMB_EINVAL),
+                           (dict(grad_table=far, grad_table_stride=64, grad_table_dtype=2),
+                            _lib.LAMB_EINVAL),
+                           (dict(grad_table=far, grad_table_stride=63), _lib.LAMB_EINVAL),
+                           (dict(grad_hidden=A, grad_hidden_stride=64), _lib.LAMB_EOVERLAP),
+                           (dict(grad_hidden=far + 1, grad_hidden_stride=64), _lib.LAMB_EALIGN)):
+        _refused(status, lambda: _ops.lamb_xent_backward(
+            x, A, _ops.lamb_xent_grads(**fields), far + (1 << 20), back))
+    _refused(_lib.LAMB_ENULL, lambda: _ops.lamb_xent_backward(
+        x, 0, _ops.lamb_xent_grads(), far, back))
+
+
+def test_cross_entropy_workspace_is_a_piece(lib):
+    """Far below the logits, which 16384 tokens against 200,000 words would take 6.5 GB for."""
+    x = _xent(tokens=16384, vocab=200000, dim=1024, hidden_stride=1024, table_stride=1024)
+    assert _ops.lamb_xent_workspace(x, True) < 16384 * 1024 * (2 + 8 * 4) + (200 << 20)
+
+
+def _embed(**fields):
+    e = _ops.lamb_embed(A, 10, 20, 64, _ops.LAMB_DTYPE_I64, 1.0)
+    for k, v in fields.items():
+        setattr(e, k, v)
+    return e
+
+
+@pytest.mark.parametrize("fields,status", [
+    (dict(tokens=-1), _lib.LAMB_EINVAL), (dict(vocab=0), _lib.LAMB_EINVAL),
+    (dict(dim=1 << 20), _lib.LAMB_EINVAL), (dict(id_dtype=1), _lib.LAMB_EINVAL),
+    (dict(scale=math.nan), _lib.LAMB_EINVAL), (dict(ids=None), _lib.LAMB_ENULL),
+    (dict(ids=A + 4), _lib.LAMB_EALIGN),
+])
+def test_table_refusals(lib, fields, status):
+    e, t, o = _embed(**fields), A + (1 << 24), A + (1 << 25)
+    for call in (lambda: _ops.lamb_embed_forward(e, t, 64, 0, o, 64, 0),
+                 lambda: _ops.lamb_embed_workspace(e),
+                 lambda: _ops.lamb_embed_backward(e, o, 64, 0, t, 64, 0, -1, 0, A, 1 << 40)):
+        _refused(status, call)
+
+
+def test_table_buffers(lib):
+    e, t, o, w = _embed(), A + (1 << 24), A + (1 << 25), A + (1 << 26)
+    need = _ops.lamb_embed_workspace(e)
+    for args, status in (((0, 64, 0, o, 64, 0), _lib.LAMB_ENULL),
+                         ((t, 63, 0, o, 64, 0), _lib.LAMB_EINVAL),
+                         ((t, 64, 2, o, 64, 0), _lib.LAMB_EINVAL),
+                         ((t, 64, 0, o + 2, 64, 0), _lib.LAMB_EALIGN),
+                         ((t, 64, 0, t + 256, 64, 0), _lib.LAMB_EOVERLAP)):
+        _refused(status, lambda: _ops.lamb_embed_forward(e, *args))
+    for args, status in (((0, 64, 0, t, 64, 0, -1, 0, w, need), _lib.LAMB_ENULL),
+                         ((o, 64, 0, t, 64, 0, -1, 2, w, need), _lib.LAMB_EINVAL),
+                         ((o, 64, 0, t, 64, 0, -1, 0, 0, need), _lib.LAMB_ENULL),
+                         ((o, 64, 0, t, 64, 0, -1, 0, w, need - 1), _lib.LAMB_EINVAL),
+                         ((o, 64, 0, o, 64, 0, -1, 0, w, need), _lib.LAMB_EOVERLAP)):
+        _refused(status, lambda: _ops.lamb_embed_backward(e, *args))
