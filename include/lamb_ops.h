@@ -59,7 +59,7 @@ LAMB_API lamb_status lamb_ns_params_init(lamb_ns_params *params);
 
 /*
  * One matrix to orthogonalize, row-major with rows `*_stride` elements apart
- * (>= cols). rows and cols 1 to 2^20, aligned to their element. A row or column
+ * (>= cols, at most 2^36). rows and cols 1 to 2^20, aligned to their element. A row or column
  * vector is a matrix of short side 1. No output may overlap an input of the plan
  * or another output, but for an input that has the output's address, type and
  * stride (in place).
@@ -156,7 +156,7 @@ LAMB_API lamb_status lamb_ns_plan_destroy(lamb_ns_plan *plan);
  * count: its loss and gradient are 0 and nothing that its row holds reaches any
  * result. Any other target outside [0, vocab) makes that token's loss and lse NaN, and
  * with them the mean and the gradients.
- * tokens 0 to 2^24, vocab 1 to 2^24, dim 1 to 2^16.
+ * tokens 0 to 2^24, vocab 1 to 2^24, dim 1 to 2^16, strides at most 2^36.
  */
 typedef struct lamb_xent {
     const void *hidden;
@@ -210,7 +210,7 @@ LAMB_API lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
  * [tokens][dim] are float32 or bfloat16 each, rows `*_stride` elements apart (>= dim;
  * out's rows do not overlap), aligned to their elements. ids: LAMB_DTYPE_I32 or _I64.
  * The row of an id outside [0, vocab) becomes NaN. tokens 0 to 2^24, vocab 1 to 2^24,
- * dim 1 to 2^16.
+ * dim 1 to 2^16, strides at most 2^36.
  */
 typedef struct lamb_embed {
     const void *ids;

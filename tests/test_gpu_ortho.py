@@ -298,3 +298,23 @@ def test_muon_scalars():
     torch.cuda.synchronize()
     plan.close()
     assert x.eq(1).all() and m.eq(0).all()
+
+
+def test_small_matrices_are_no_further_off_than_fp32():
+    """Their few roundings do not average out, so the split products keep every part."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    a, b, c = ops.COEFFICIENTS
+    for shape in ((12, 10), (45, 45), (59, 161)):
+        gs = _make(torch, [shape] * 100, torch.float32, seed=5)
+        ours, plain = [], []
+        for g, got in zip(gs, ops.Orthogonalizer(gs, precision="split").run()):
+            x = g.mT if g.shape[0] > g.shape[1] else g
+            x = x / (torch.linalg.vector_norm(x) + 1e-7)
+            for _ in range(5):
+                gram = x @ x.mT
+                x = a * x + (b * gram + c * (gram @ gram)) @ x
+            want = R.newton_schulz(g)
+            ours.append(R.relative(got, want))
+            plain.append(R.relative(x.mT if g.shape[0] > g.shape[1] else x, want))
+        assert sorted(ours)[50] <= sorted(plain)[50]
