@@ -167,8 +167,8 @@ __device__ inline float2 join(float2 p, float2 q) {
 
 // A tile of logits, its rows' maxima and sums of exponentials: in registers, then over the
 // 4 lanes of a row, then over the WN waves through LDS. Bound by the matrix cores: 8192
-// tokens of 1600 against 50257 words take 1.15 ms, 1.15 PFLOP/s; 1229 of 1024 against 30522
-// (9.6 rows of 128 x 128 tiles) 0.119, 0.65.
+// tokens of 1600 against 50257 words take 1.15 ms, 1.15 PFLOP/s; 1190 of 1024 against 30522
+// (9.3 rows of 128 x 128 tiles) 0.12, 0.62.
 template <class Shape>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_logits_kernel(
     XentArgs a, float2 *parts, float *at_target) {
@@ -284,9 +284,9 @@ __global__ __launch_bounds__(1024) void xent_mean_kernel(const float *loss, int3
 }
 
 // Q of a piece: the logits again, so the same product, and 2 B written per entry, through
-// LDS in whole lines (128 x 128 tiles, 1229 tokens of 1024 against 30522 words: 128 us,
+// LDS in whole lines (128 x 128 tiles, 1190 tokens of 1024 against 30522 words: 128 us,
 // 132 from registers; 256 x 256, 8192 of 1600 against a sixth of 50257: 245 and 240).
-// Bound by the matrix cores: 0.60 and 0.90 PFLOP/s.
+// Bound by the matrix cores: 0.58 and 0.90 PFLOP/s.
 template <class Shape>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_probs_kernel(
     XentArgs a, XentPiece piece, const float *lse) {
