@@ -31,12 +31,17 @@ typedef enum lamb_dtype {
 
 /*
  * How the products of the Newton-Schulz iteration round their operands.
- *  LAMB_NS_HALF   to one 16-bit float (11 significant bits). The result is about
- *                 1.3e-3 off (2-norm, relative) for matrices of independent
- *                 entries and up to 7e-3 for ones whose singular values span
- *                 many decades: the rounding of a bf16 result is 1.7e-3.
- *  LAMB_NS_SPLIT  to the sum of two (22 bits), three products for one: errors as
- *                 of fp32 arithmetic.
+ *  LAMB_NS_SPLIT  to the sum of two 16-bit floats (22 bits), three products for one:
+ *                 errors as of fp32 arithmetic.
+ *  LAMB_NS_HALF   to one (11 bits). X, of norm 1, is so rounded to 2^-11 of itself at
+ *                 most, and the iteration multiplies what is small in it by up to
+ *                 |a|^steps (485 by default): the result is off by up to 0.25, beside
+ *                 its own norm of about sqrt(min(rows, cols)) where most singular
+ *                 values reach 1. Relative, as 2-norms: 1.3e-3 for independent entries,
+ *                 4e-3 to 1.5e-2 for singular values that fall evenly over 2 to 6
+ *                 decades, 4e-2 for rank 16 and noise of 2e-3 of it, 1.5e-1 where one
+ *                 singular value outweighs all others together by a thousand. (The
+ *                 rounding of a bf16 result is 1.7e-3.)
  */
 typedef enum lamb_ns_precision { LAMB_NS_HALF = 0, LAMB_NS_SPLIT = 1 } lamb_ns_precision;
 

@@ -82,12 +82,13 @@ class Orthogonalizer:
 
     ``inputs`` and ``outputs`` are persistent 2-D tensors (float32 or bfloat16, one
     type each, rows contiguous); ``run()`` reads the inputs as they are then. An
-    output may be its own input. ``precision``: "half" rounds the products' operands
-    to 16-bit floats with 11 significant bits (the result is 1e-3 to 7e-3 off),
-    "split" to pairs of them (as fp32, three times the work). By default "split" for
-    float32 outputs, and "half" for bfloat16 ones, whose own rounding is 1.7e-3, unless
-    the list has a matrix of short side below 64: its few roundings do not average out
-    (2.1e-3 off, 1.3e-3 from 128 on), and such lists are short work.
+    output may be its own input. ``precision``: "split" (the default) rounds the products'
+    operands to pairs of 16-bit floats (22 bits, an error as of fp32), "half" to one (11
+    bits, a third of the work). "half" has to be asked for: its error depends on the singular values.
+    The steps multiply the small ones by up to 485 (by default), and the rounding of the
+    large ones with them: 1.3e-3 off (2-norm, relative) for independent entries, 1e-2
+    where the singular values span decades, 1e-1 where a few outweigh the rest, as a
+    network's gradients and momenta often have it.
     The plan keeps a workspace of about 4 bytes per element, and 4 to 12 per entry of the
     short sides' squares; twice that for "split".
     """
@@ -120,10 +121,7 @@ class Orthogonalizer:
             r, c = a.shape
             rows.append((a.data_ptr(), b.data_ptr(), r, c, *(t.stride(0) if r > 1 else c
                                                             for t in (a, b))))
-        if precision is None:
-            half = (self.outputs[0].dtype == torch.bfloat16
-                    and min(min(t.shape) for t in self.inputs) >= 64)
-            precision = "half" if half else "split"
+        precision = "split" if precision is None else precision
         if precision not in _ops.PRECISIONS:
             raise ValueError("precision must be one of %s" % (tuple(_ops.PRECISIONS),))
         self.precision = precision
