@@ -13,7 +13,7 @@ constexpr int64_t kMaxReadStride = int64_t(1) << 21;  // a tile's rows within 32
 // A piece of the vocabulary's softmax: written once and read twice, so kept within
 // the 256 MiB last-level cache.
 constexpr int64_t kPieceBytes = int64_t(160) << 20;
-constexpr int64_t kPieceAlign = 256;
+constexpr int64_t kPieceAlign = 256;  // half of it where Q is in two parts
 
 lamb_status check(const lamb_xent *x) {
     if (!x)
@@ -79,12 +79,42 @@ Product pick(int64_t rows, int64_t cols, int64_t depth, int64_t most) {
     return best;
 }
 
+// The backward's pieces of the vocabulary, and the shapes of their products.
+struct Pieces {
+    int64_t size = 0;
+    int probs_shape = 0, hidden_shape = 0, table_shape = 0;
+    int32_t splits = 1;  // workgroups that share the sum of a tile of dH
+    double time = 1e300;
+};
+
+// Equal pieces whose Q, in `q_parts` parts, has at most kPieceBytes: of the next few counts,
+// the one whose products fill their last rounds of workgroups best.
+Pieces pick_pieces(const lamb_xent &x, int32_t q_parts) {
+    const int64_t rows = x.tokens ? x.tokens : 1, align = kPieceAlign / q_parts;
+    const int64_t most = std::max<int64_t>(align, kPieceBytes / 2 / q_parts / rows);
+    const int64_t least = (x.vocab + most - 1) / most;
+    Pieces best;
+    for (int64_t count = least; count < least + 4; ++count) {
+        const int64_t size =
+            std::min(round_up((x.vocab + count - 1) / count, align), round_up(x.vocab, 8));
+        const Product probs = pick(x.tokens, size, x.dim, 1);
+        const Product table = pick(size, x.dim, q_parts * x.tokens, 1);
+        // few rows: the piece's columns are split over workgroups, 256 each at least
+        const Product hidden = pick(x.tokens, x.dim, size, std::max<int64_t>(1, size / 256));
+        const double time = double((x.vocab + size - 1) / size) *
+                            (probs.time + table.time + hidden.time);
+        if (time < best.time)
+            best = Pieces{size, probs.shape, hidden.shape, table.shape, hidden.parts, time};
+    }
+    return best;
+}
+
 struct Layout {
     int64_t ld = 0;
     bool copy_table = false;
-    int logits_shape = 0, probs_shape = 0, hidden_shape = 0, table_shape = 0;
-    int32_t parts = 0, splits = 1;
-    int64_t piece = 0;
+    int logits_shape = 0;
+    int32_t parts = 0;
+    Pieces pieces[2];  // Q in one part, and in two
     // offsets, and the end
     size_t kept = 0, source = 0, target = 0, packed = 0, table = 0, parts_at = 0, at_target = 0,
            probs = 0, partial = 0, bytes = 0;
@@ -114,32 +144,15 @@ Layout layout_of(const lamb_xent &x, bool backward) {
         l.bytes = at;
         return l;
     }
-    // equal pieces of at most kPieceBytes: of the next few counts, the one whose products
-    // fill their last rounds of workgroups best
-    const int64_t rows = x.tokens ? x.tokens : 1;
-    const int64_t most = std::max<int64_t>(kPieceAlign, kPieceBytes / 2 / rows);
-    const int64_t least = (x.vocab + most - 1) / most;
-    double best = 1e300;
-    for (int64_t pieces = least; pieces < least + 4; ++pieces) {
-        const int64_t size = std::min(round_up((x.vocab + pieces - 1) / pieces, kPieceAlign),
-                                      round_up(x.vocab, 8));
-        const Product probs = pick(x.tokens, size, x.dim, 1);
-        const Product table = pick(size, x.dim, x.tokens, 1);
-        // few rows: the piece's columns are split over workgroups, 256 each at least
-        const Product hidden = pick(x.tokens, x.dim, size, std::max<int64_t>(1, size / 256));
-        const double time = double((x.vocab + size - 1) / size) *
-                            (probs.time + table.time + hidden.time);
-        if (time < best) {
-            best = time;
-            l.piece = size;
-            l.probs_shape = probs.shape;
-            l.table_shape = table.shape;
-            l.hidden_shape = hidden.shape;
-            l.splits = hidden.parts;
-        }
+    int64_t probs = 0;
+    int32_t splits = 1;
+    for (int32_t k = 0; k < 2; ++k) {
+        l.pieces[k] = pick_pieces(x, k + 1);
+        probs = std::max(probs, (k + 1) * 2 * x.tokens * l.pieces[k].size);
+        splits = std::max(splits, l.pieces[k].splits);
     }
-    l.probs = take(2 * x.tokens * l.piece);
-    l.partial = take(int64_t(l.splits) * x.tokens * l.ld * 4);
+    l.probs = take(probs);
+    l.partial = take(int64_t(splits) * x.tokens * l.ld * 4);
     l.bytes = at;
     return l;
 }
@@ -304,24 +317,27 @@ lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
     if (st != LAMB_OK)
         return st;
     float *partial = reinterpret_cast<float *>(work + l.partial);
+    const bool two = g.grad_table && !bf16;
+    const Pieces &p = l.pieces[two];
     hipError_t err = hipSuccess;
-    for (int64_t first = 0; first < x.vocab && err == hipSuccess; first += l.piece) {
+    for (int64_t first = 0; first < x.vocab && err == hipSuccess; first += p.size) {
         XentPiece piece{};
         piece.first = int32_t(first);
-        piece.count = int32_t(std::min(l.piece, x.vocab - first));
+        piece.count = int32_t(std::min(p.size, x.vocab - first));
         piece.ld = int32_t(round_up(piece.count, 8));
         piece.probs = reinterpret_cast<uint16_t *>(work + l.probs);
+        piece.low = two ? piece.probs + x.tokens * p.size : nullptr;
         if (x.tokens)
-            err = launch_xent_probs(args, l.probs_shape, piece, lse, stream);
+            err = launch_xent_probs(args, p.probs_shape, piece, lse, stream);
         if (err == hipSuccess && x.tokens && g.grad_hidden)
-            err = launch_xent_hidden(args, l.hidden_shape, piece, l.splits, first > 0, partial,
+            err = launch_xent_hidden(args, p.hidden_shape, piece, p.splits, first > 0, partial,
                                      stream);
         if (err == hipSuccess && g.grad_table)
-            err = launch_xent_table(args, l.table_shape, piece, g.grad_loss, g.grad_scale, g.mean,
+            err = launch_xent_table(args, p.table_shape, piece, g.grad_loss, g.grad_scale, g.mean,
                                     bf16, g.add_table, g.grad_table, g.grad_table_stride, stream);
     }
     if (err == hipSuccess && x.tokens && g.grad_hidden)
-        err = launch_xent_hidden_out(args, l.splits, partial, g.grad_loss, g.grad_scale, g.mean,
+        err = launch_xent_hidden_out(args, p.splits, partial, g.grad_loss, g.grad_scale, g.mean,
                                      static_cast<uint16_t *>(g.grad_hidden), g.grad_hidden_stride,
                                      stream);
     return err == hipSuccess ? LAMB_OK : fail_hip(err, "kernel launch");

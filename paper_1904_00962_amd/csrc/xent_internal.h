@@ -72,13 +72,14 @@ hipError_t launch_xent_mean(const float *loss, int32_t tokens, const int32_t *ke
                             hipStream_t stream);
 
 // One piece of the vocabulary: rows [first, first + count) of the table; probs is
-// [tokens][ld] with zeros from count to ld.
+// [tokens][ld] with zeros from count to ld, and so is low, what the rounding of probs
+// leaves, where the table's gradient is fp32 (else null).
 struct XentPiece {
     int32_t first, count, ld;
-    uint16_t *probs;
+    uint16_t *probs, *low;
 };
 
-// probs = softmax - one at the target, in bf16.
+// probs = softmax - one at the target, in bf16; low = the rest of it, in bf16 again.
 hipError_t launch_xent_probs(const XentArgs &args, int shape, const XentPiece &piece,
                              const float *lse, hipStream_t stream);
 // partial[split] (tokens x dim, fp32) = or += probs' share of the piece times the table.
@@ -88,7 +89,7 @@ hipError_t launch_xent_hidden(const XentArgs &args, int shape, const XentPiece &
 hipError_t launch_xent_hidden_out(const XentArgs &args, int32_t splits, const float *partial,
                                   const float *grad_loss, float grad_scale, bool mean,
                                   uint16_t *grad_hidden, int64_t stride, hipStream_t stream);
-// grad_table's rows of the piece = (or +=) scale probs^T hidden.
+// grad_table's rows of the piece = (or +=) scale probs^T hidden; fp32: (probs + low)^T hidden.
 hipError_t launch_xent_table(const XentArgs &args, int shape, const XentPiece &piece,
                              const float *grad_loss, float grad_scale, bool mean, bool bf16_out,
                              bool add, void *grad_table, int64_t stride, hipStream_t stream);

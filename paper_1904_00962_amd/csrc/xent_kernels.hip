@@ -15,7 +15,10 @@
 // reaches no result.
 //
 // Q's rounding to bf16 (2^-8 at most, relative, each entry by itself) is the one to
-// fewer bits; sums are fp32.
+// fewer bits; sums are fp32. It is as large as the rounding of a bf16 gradient: 8192 tokens
+// of 64 columns against 500 words end 2.4e-3 off, 1.7e-3 by the result's rounding alone;
+// 1229 against 30522 words, where few words carry the sums, 1.66e-3 and 1.66e-3. An fp32
+// gradient of the table is promised more, and gets Q in two parts (2^-16) for a product more.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -287,7 +290,8 @@ __global__ __launch_bounds__(1024) void xent_mean_kernel(const float *loss, int3
 // LDS in whole lines (128 x 128 tiles, 1190 tokens of 1024 against 30522 words: 128 us,
 // 132 from registers; 256 x 256, 8192 of 1600 against a sixth of 50257: 245 and 240).
 // Bound by the matrix cores: 0.58 and 0.90 PFLOP/s.
-template <class Shape>
+// LOW: the rest of each entry too, a plane of its own.
+template <class Shape, bool LOW>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_probs_kernel(
     XentArgs a, XentPiece piece, const float *lse) {
     __shared__ __align__(1024) short lds[Shape::kLds];
@@ -300,27 +304,34 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_probs_ker
     logits_tile<Shape>(acc, lds, a, m0, int64_t(piece.first) + n0, kept);
     const Place<Shape> at;
     const TileStore<Shape::BM, Shape::BN, Shape::kThreads> store(lds);
+#pragma unroll 1
+    for (int part = 0; part <= int(LOW); ++part) {
 #pragma unroll
-    for (int i = 0; i < Shape::MI; ++i) {
-        const int m = m0 + at.row + 16 * i;
-        const int target = m < kept ? a.target[m] - piece.first : -1;
-        const float from = m < kept ? lse[a.source[m]] : 0.0f;
+        for (int i = 0; i < Shape::MI; ++i) {
+            const int m = m0 + at.row + 16 * i;
+            const int target = m < kept ? a.target[m] - piece.first : -1;
+            const float from = m < kept ? lse[a.source[m]] : 0.0f;
 #pragma unroll
-        for (int j = 0; j < Shape::NI; ++j) {
-            const int n = n0 + at.col + 16 * j;
-            float v[4];
+            for (int j = 0; j < Shape::NI; ++j) {
+                const int n = n0 + at.col + 16 * j;
+                float v[4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
-                v[r] = __builtin_amdgcn_exp2f((acc[i][j][r] - from) * kLog2e);
-                v[r] = n + r == target ? v[r] - 1.0f : v[r];
-                v[r] = n + r < piece.count ? v[r] : 0.0f;
+                for (int r = 0; r < 4; ++r) {
+                    v[r] = __builtin_amdgcn_exp2f((acc[i][j][r] - from) * kLog2e);
+                    v[r] = n + r == target ? v[r] - 1.0f : v[r];
+                    v[r] = n + r < piece.count ? v[r] : 0.0f;
+                    if (LOW && part)
+                        v[r] -= widen(to_bf16(v[r]));
+                }
+                store.put(at.row + 16 * i, at.col + 16 * j,
+                          make_ushort4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]),
+                                       to_bf16(v[3])));
             }
-            store.put(at.row + 16 * i, at.col + 16 * j,
-                      make_ushort4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3])));
         }
+        uint16_t *plane = LOW && part ? piece.low : piece.probs;
+        store.template flush<false>(plane + int64_t(m0) * piece.ld + n0, piece.ld, kept - m0,
+                                    piece.ld - n0);
     }
-    store.template flush<false>(piece.probs + int64_t(m0) * piece.ld + n0, piece.ld, kept - m0,
-                                piece.ld - n0);
 }
 
 // dH += Q W over a piece, in fp32; few rows split the piece's columns over workgroups, each
@@ -419,9 +430,10 @@ __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_table_ker
     const TileAt tile(tiles_of(piece.count, Shape::BM), tiles_of(a.dim, Shape::BN));
     const int m0 = tile.row * Shape::BM, n0 = tile.col * Shape::BN;
     float4v acc[Shape::MI][Shape::NI] = {};
-    if (kept > 0)
+#pragma unroll 1
+    for (int part = BF16 ? 1 : 0; part < 2 && kept > 0; ++part)  // small products first
         tile_product<Bf16Math, Shape, true, true>(
-            acc, lds, columns_at(piece.probs, piece.ld, m0, piece.ld),
+            acc, lds, columns_at(part ? piece.probs : piece.low, piece.ld, m0, piece.ld),
             columns_at(a.hidden, a.ld, n0, int32_t(a.ld)), kept);
     const float scale = final_scale(grad_loss, grad_scale, mean, kept);
     const Place<Shape> at;
@@ -535,9 +547,9 @@ hipError_t launch_xent_probs(const XentArgs &args, int shape, const XentPiece &p
                              const float *lse, hipStream_t stream) {
     return with_shape(shape, [&](auto s) {
         using Shape = decltype(s);
-        xent_probs_kernel<Shape>
-            <<<uint32_t(tiles(args.tokens, piece.ld, shape)), Shape::kThreads, 0, stream>>>(
-                args, piece, lse);
+        auto kernel = piece.low ? xent_probs_kernel<Shape, true> : xent_probs_kernel<Shape, false>;
+        kernel<<<uint32_t(tiles(args.tokens, piece.ld, shape)), Shape::kThreads, 0, stream>>>(
+            args, piece, lse);
     });
 }
 

@@ -1,0 +1,54 @@
+"""How exact the gradient of the vocabulary table is that a caller asks for in fp32.
+
+Tolerances. The gradient is the sum over the tokens of q h, q softmax less one at the
+target. q comes in two bf16 parts, off by 2^-16 of itself at most, each by itself, and from
+logits whose fp32 errors (2^-24 of a few units, here) move it by less than that. The sums
+are fp32, of products that are exact. Independent errors of the terms add up in squares:
+2^-15 of the root of the sum of (q h)^2, twice what they are at most, and 2^-22 of the sum
+of |q h| for the fp32 sums of up to 8192 terms, whose roundings change sign."""
+
+import math
+
+import pytest
+
+from gpu_harness import torch_cuda
+from test_gpu_xent import _problem
+
+pytestmark = pytest.mark.gpu
+
+
+def _terms(torch, h, w, t, mean=True):
+    """(gradient, its bound) in 64 bits."""
+    keep = (t != -100).nonzero()[:, 0]
+    h, w, t = h[keep].double(), w.double(), t[keep].long()
+    z = h @ w.t().contiguous()
+    q = torch.exp(z - torch.logsumexp(z, dim=1, keepdim=True))
+    q.scatter_add_(1, t[:, None], -torch.ones_like(z[:, :1]))
+    if mean:
+        q /= max(1, len(keep))
+    qt = q.t().contiguous()
+    size = (qt.square() @ h.square()).sqrt() * 2.0 ** -15 + (qt.abs() @ h.abs()) * 2.0 ** -22
+    return qt @ h, size
+
+
+@pytest.mark.parametrize("tokens,dim,vocab", [(1, 64, 300), (3, 256, 2003), (64, 33, 500),
+                                              (300, 512, 5000), (1200, 256, 30522),
+                                              (8192, 64, 500), (4096, 128, 20000)])
+@pytest.mark.parametrize("ignored,accumulate", [(0.0, False), (0.3, True)])
+def test_fp32_table_gradients_are_more_than_bf16_ones(tokens, dim, vocab, ignored, accumulate):
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    h, w, t = _problem(torch, tokens, dim, vocab, seed=tokens, ignored=ignored)
+    _, _, lse = ops.linear_cross_entropy(h, w, t)
+    gw = torch.full(w.shape, 0.0 if accumulate else math.nan, device="cuda")
+    gh = torch.empty_like(h)
+    ops.linear_cross_entropy_grad(h, w, t, lse, gh, gw, accumulate=accumulate)
+    want, size = _terms(torch, h, w, t)
+    off = float(torch.linalg.vector_norm(gw.double() - want))
+    assert off <= float(torch.linalg.vector_norm(size)) + 1e-12
+    # the hidden gradient beside it is the one beside a bf16 table gradient, up to the
+    # order of its sums
+    other = torch.empty_like(h)
+    ops.linear_cross_entropy_grad(h, w, t, lse, other, torch.empty_like(w))
+    assert float((other.float() - gh.float()).abs().max()) <= \
+        2.0 ** -7 * float(gh.float().abs().max())
