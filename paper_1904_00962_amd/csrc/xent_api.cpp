@@ -117,7 +117,7 @@ struct Layout {
     Pieces pieces[2];  // Q in one part, and in two
     // offsets, and the end
     size_t kept = 0, source = 0, target = 0, packed = 0, table = 0, parts_at = 0, at_target = 0,
-           probs = 0, partial = 0, bytes = 0;
+           probs = 0, partial = 0, table_sum = 0, bytes = 0;
 };
 
 Layout layout_of(const lamb_xent &x, bool backward) {
@@ -153,6 +153,9 @@ Layout layout_of(const lamb_xent &x, bool backward) {
     }
     l.probs = take(probs);
     l.partial = take(int64_t(splits) * x.tokens * l.ld * 4);
+    l.table_sum = take(x.tokens > kChainTokens
+                           ? std::max(l.pieces[0].size, l.pieces[1].size) * l.ld * 4
+                           : 0);
     l.bytes = at;
     return l;
 }
@@ -334,7 +337,8 @@ lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
                                      stream);
         if (err == hipSuccess && g.grad_table)
             err = launch_xent_table(args, p.table_shape, piece, g.grad_loss, g.grad_scale, g.mean,
-                                    bf16, g.add_table, g.grad_table, g.grad_table_stride, stream);
+                                    bf16, g.add_table, g.grad_table, g.grad_table_stride,
+                                    reinterpret_cast<float *>(work + l.table_sum), stream);
     }
     if (err == hipSuccess && x.tokens && g.grad_hidden)
         err = launch_xent_hidden_out(args, p.splits, partial, g.grad_loss, g.grad_scale, g.mean,

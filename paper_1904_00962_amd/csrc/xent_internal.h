@@ -23,6 +23,11 @@ constexpr int32_t pack_rounds(int64_t tokens) {
                ? int32_t((tokens + 1024 * kPackTokens - 1) / (1024 * kPackTokens))
                : 1;
 }
+// Tokens that one chain of fp32 sums takes: a matrix instruction rounds each product to the
+// sum's last place, which costs a column of equal values (0.7 times the same probability)
+// 5e-5 after 65536 tokens, 7e-4 after 2^20 and 8e-3 after 2^22. More tokens are summed in
+// chains of this many, which add up in memory.
+constexpr int32_t kChainTokens = 32768;
 constexpr int kReduceTokens = 16;  // tokens per workgroup of the logsumexp pass
 
 // What every pass of a call reads. `hidden` is the packed copy of the tokens that
@@ -90,8 +95,10 @@ hipError_t launch_xent_hidden_out(const XentArgs &args, int32_t splits, const fl
                                   const float *grad_loss, float grad_scale, bool mean,
                                   uint16_t *grad_hidden, int64_t stride, hipStream_t stream);
 // grad_table's rows of the piece = (or +=) scale probs^T hidden; fp32: (probs + low)^T hidden.
+// partial: [piece.count][ld] in fp32, for more than kChainTokens tokens.
 hipError_t launch_xent_table(const XentArgs &args, int shape, const XentPiece &piece,
                              const float *grad_loss, float grad_scale, bool mean, bool bf16_out,
-                             bool add, void *grad_table, int64_t stride, hipStream_t stream);
+                             bool add, void *grad_table, int64_t stride, float *partial,
+                             hipStream_t stream);
 
 }  // namespace lamb_mi355x

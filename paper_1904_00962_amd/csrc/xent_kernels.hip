@@ -418,25 +418,52 @@ __global__ __launch_bounds__(256) void xent_hidden_out_kernel(XentArgs a, int32_
             out[r] = to_bf16(v[r] * scale);
 }
 
-// dW's rows of a piece = Q^T H, the sum over the tokens that count. Both operands are read
-// transposed from LDS. Bound by the matrix cores: 208 us for a sixth of 50257 words, 8192
+// dW's rows of a piece = Q^T H, the sum over the tokens that count, in chains of
+// kChainTokens. Both operands are read transposed from LDS. Bound by the matrix cores: 208 us for a sixth of 50257 words, 8192
 // tokens of 1600, 1.06 PFLOP/s.
 template <class Shape, bool BF16, bool ADD>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_table_kernel(
     XentArgs a, XentPiece piece, const float *grad_loss, float grad_scale, bool mean,
-    void *grad_table, int64_t stride, bool vector) {
+    void *grad_table, int64_t stride, bool vector, float *partial) {
     __shared__ __align__(1024) short lds[Shape::kLds];
     const int32_t kept = *a.kept;
     const TileAt tile(tiles_of(piece.count, Shape::BM), tiles_of(a.dim, Shape::BN));
     const int m0 = tile.row * Shape::BM, n0 = tile.col * Shape::BN;
+    const Place<Shape> at;
     float4v acc[Shape::MI][Shape::NI] = {};
 #pragma unroll 1
-    for (int part = BF16 ? 1 : 0; part < 2 && kept > 0; ++part)  // small products first
-        tile_product<Bf16Math, Shape, true, true>(
-            acc, lds, columns_at(part ? piece.probs : piece.low, piece.ld, m0, piece.ld),
-            columns_at(a.hidden, a.ld, n0, int32_t(a.ld)), kept);
+    for (int32_t k0 = 0; k0 < kept; k0 += kChainTokens) {
+        const int32_t depth = kept - k0 < kChainTokens ? kept - k0 : kChainTokens;
+#pragma unroll 1
+        for (int part = BF16 ? 1 : 0; part < 2; ++part) {  // small products first
+            const uint16_t *q = (part ? piece.probs : piece.low) + int64_t(k0) * piece.ld;
+            tile_product<Bf16Math, Shape, true, true>(
+                acc, lds, columns_at(q, piece.ld, m0, piece.ld),
+                columns_at(a.hidden + int64_t(k0) * a.ld, a.ld, n0, int32_t(a.ld)), depth);
+        }
+        if (kept <= kChainTokens)
+            break;
+        // the chains before are in memory; the last one's sum stays in registers
+        const bool last = k0 + depth == kept;
+#pragma unroll
+        for (int i = 0; i < Shape::MI; ++i) {
+            const int m = m0 + at.row + 16 * i;
+#pragma unroll
+            for (int j = 0; j < Shape::NI; ++j) {
+                const int n = n0 + at.col + 16 * j;
+                if (m >= piece.count || n >= a.ld)
+                    continue;
+                float4v *sum = (float4v *)(partial + int64_t(m) * a.ld + n);
+                if (k0 > 0)
+                    acc[i][j] += *sum;
+                if (!last) {
+                    *sum = acc[i][j];
+                    acc[i][j] = float4v{};
+                }
+            }
+        }
+    }
     const float scale = final_scale(grad_loss, grad_scale, mean, kept);
-    const Place<Shape> at;
 #pragma unroll
     for (int i = 0; i < Shape::MI; ++i) {
         const int m = m0 + at.row + 16 * i;
@@ -574,7 +601,8 @@ hipError_t launch_xent_hidden_out(const XentArgs &args, int32_t splits, const fl
 
 hipError_t launch_xent_table(const XentArgs &args, int shape, const XentPiece &piece,
                              const float *grad_loss, float grad_scale, bool mean, bool bf16_out,
-                             bool add, void *grad_table, int64_t stride, hipStream_t stream) {
+                             bool add, void *grad_table, int64_t stride, float *partial,
+                             hipStream_t stream) {
     const int64_t size = bf16_out ? 2 : 4;
     const bool vector = stride * size % 16 == 0 && (uintptr_t(grad_table) & 15) == 0;
     return with_shape(shape, [&](auto s) {
@@ -584,7 +612,7 @@ hipError_t launch_xent_table(const XentArgs &args, int shape, const XentPiece &p
                                : (add ? xent_table_kernel<Shape, false, true>
                                       : xent_table_kernel<Shape, false, false>);
         kernel<<<uint32_t(tiles(piece.count, args.dim, shape)), Shape::kThreads, 0, stream>>>(
-            args, piece, grad_loss, grad_scale, mean, grad_table, stride, vector);
+            args, piece, grad_loss, grad_scale, mean, grad_table, stride, vector, partial);
     });
 }
 

@@ -52,3 +52,53 @@ def test_fp32_table_gradients_are_more_than_bf16_ones(tokens, dim, vocab, ignore
     ops.linear_cross_entropy_grad(h, w, t, lse, other, torch.empty_like(w))
     assert float((other.float() - gh.float()).abs().max()) <= \
         2.0 ** -7 * float(gh.float().abs().max())
+
+
+@pytest.mark.parametrize("dtype,result", [("float32", 2.0 ** -16), ("bfloat16", 2.0 ** -8)])
+@pytest.mark.parametrize("tokens,dim", [(30000, 8), (32769, 264), (100000, 520), (1 << 20, 72),
+                                        ((1 << 22) + 5, 8)])
+def test_sums_over_many_tokens_do_not_stall(dtype, result, tokens, dim):
+    """Columns of hidden states that are the same for every token, against a table of zeros:
+    every q is 1 / 8, less one at the target, and no rounding takes another's place. A
+    chain of fp32 sums takes at most 2^15 tokens, so 2^15 roundings of half a unit (2^-25 of
+    the sum) at most: 2^-10."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    h = torch.ones(tokens, dim, dtype=torch.bfloat16, device="cuda")
+    h *= torch.linspace(0.6, 3.3, dim, device="cuda").bfloat16()
+    h[:, dim // 2:] *= -1
+    w = torch.zeros(8, dim, dtype=torch.bfloat16, device="cuda")
+    t = torch.full((tokens,), 2, device="cuda")
+    t[::7] = -100
+    kept = int((t != -100).sum())
+    _, _, lse = ops.linear_cross_entropy(h, w, t)
+    gw = torch.full(w.shape, math.nan, dtype=getattr(torch, dtype), device="cuda")
+    ops.linear_cross_entropy_grad(h, w, t, lse, None, gw, reduction="sum")
+    want = h[0].double()[None, :] * kept / 8
+    want = want.repeat(8, 1)
+    want[2] *= -7
+    off = (gw.double() / want - 1).abs()
+    assert float(off.max()) <= result + 2.0 ** -10
+
+
+def test_many_tokens_add_to_an_older_gradient():
+    """The bound of the fp32 gradients, over several chains of tokens and pieces of words."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    h, w, t = _problem(torch, 70000, 64, 3000, ignored=0.05)
+    _, _, lse = ops.linear_cross_entropy(h, w, t)
+    old = torch.randn(w.shape, device="cuda") * 1e-3
+    want, size = 0, 0
+    kept = int((t != -100).sum())
+    for first in range(0, 70000, 8192):
+        a, b = _terms(torch, h[first:first + 8192], w, t[first:first + 8192], mean=False)
+        want, size = want + a / kept, size + (b / kept).square()
+    for dtype in (torch.float32, torch.bfloat16):
+        gw = old.to(dtype)
+        before = gw.double()
+        ops.linear_cross_entropy_grad(h, w, t, lse, None, gw, accumulate=True)
+        off = torch.linalg.vector_norm(gw.double() - before - want)
+        bound = torch.linalg.vector_norm(size.sqrt()) + 2.0 ** -24 * torch.linalg.vector_norm(old)
+        if dtype == torch.bfloat16:  # q's rounding, 2^-8 in place of 2^-16, and the result's
+            bound = 2 ** 8 * bound + 2.0 ** -8 * torch.linalg.vector_norm(before + want)
+        assert float(off) <= float(bound)
