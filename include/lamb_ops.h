@@ -125,7 +125,8 @@ typedef enum lamb_muon_scale {
 typedef struct lamb_muon_hparams {
     lamb_ns_params ns;
     float lr;            /* >= 0                                                 */
-    float momentum;      /* in [0, 1)                                            */
+    double momentum;     /* in [0, 1); 1 - momentum is taken of this, where that of
+                            a float near 0.95 would be 2.4e-7 off             */
     float weight_decay;  /* >= 0, decoupled: x <- (1 - lr weight_decay) x first   */
     float grad_scale;    /* > 0: every gradient element is multiplied by it       */
     int32_t nesterov;    /* 0 or 1                                               */

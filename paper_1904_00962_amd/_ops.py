@@ -52,7 +52,7 @@ class lamb_muon_tensor(ctypes.Structure):
 
 
 class lamb_muon_hparams(ctypes.Structure):
-    _fields_ = [("ns", lamb_ns_params), ("lr", ctypes.c_float), ("momentum", ctypes.c_float),
+    _fields_ = [("ns", lamb_ns_params), ("lr", ctypes.c_float), ("momentum", ctypes.c_double),
                 ("weight_decay", ctypes.c_float), ("grad_scale", ctypes.c_float),
                 ("nesterov", ctypes.c_int32), ("scale", ctypes.c_int32),
                 ("skip_nonfinite", ctypes.c_int32), ("reserved", ctypes.c_int32)]

@@ -398,7 +398,7 @@ lamb_status lamb_muon_hparams_init(lamb_muon_hparams *hp) {
     *hp = lamb_muon_hparams{};
     (void)lamb_ns_params_init(&hp->ns);
     hp->lr = 1e-3f;
-    hp->momentum = 0.95f;
+    hp->momentum = 0.95;
     hp->grad_scale = 1.0f;
     hp->nesterov = 1;
     hp->scale = LAMB_MUON_RMS;
@@ -547,8 +547,8 @@ lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void
         return st;
     if (!std::isfinite(hp->lr) || hp->lr < 0.0f)
         return fail(LAMB_EINVAL, "lr = %g, need finite and >= 0", double(hp->lr));
-    if (!(hp->momentum >= 0.0f && hp->momentum < 1.0f))
-        return fail(LAMB_EINVAL, "momentum = %g outside [0, 1)", double(hp->momentum));
+    if (!(hp->momentum >= 0.0 && hp->momentum < 1.0))
+        return fail(LAMB_EINVAL, "momentum = %g outside [0, 1)", hp->momentum);
     if (!std::isfinite(hp->weight_decay) || hp->weight_decay < 0.0f)
         return fail(LAMB_EINVAL, "weight_decay = %g, need finite and >= 0",
                     double(hp->weight_decay));
@@ -564,8 +564,7 @@ lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void
     DeviceScope scope(plan->device);
     NsStep step{};
     step.momentum = hp->momentum;
-    step.one_minus = float(1.0 - double(hp->momentum));
-    step.grad_scale = hp->grad_scale;
+    step.from_grad = (1.0 - hp->momentum) * double(hp->grad_scale);
     step.decay = float(1.0 - double(hp->lr) * double(hp->weight_decay));
     step.lr = hp->lr;
     step.nesterov = hp->nesterov;

@@ -74,9 +74,8 @@ struct NsStep {
     float a, b, c;
     float eps;
     // Muon
-    float momentum, one_minus;  // m <- momentum m + one_minus grad_scale g
-    float grad_scale;
-    float decay;                // x <- decay x - lr s O (decay 1 where the mask is off)
+    double momentum, from_grad;  // m <- momentum m + from_grad g
+    float decay;                 // x <- decay x - lr s O (decay 1 where the mask is off)
     float lr;
     int32_t nesterov;
     int32_t scale;              // a lamb_muon_scale

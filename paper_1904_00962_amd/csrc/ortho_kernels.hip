@@ -143,6 +143,11 @@ __global__ __launch_bounds__(kNsBlock) void ns_check_kernel(const NsMatrix *matr
         atomicOr(flag, 1u);
 }
 
+// momentum m + from_grad g, rounded once: in fp64, which costs these passes nothing.
+__device__ inline float mix(const NsStep &step, float m, float g) {
+    return float(__builtin_fma(step.momentum, double(m), step.from_grad * double(g)));
+}
+
 // Each workgroup's sum of squares of the matrix to orthogonalize, in fp64. Muon:
 // m <- momentum m + (1 - momentum) g first; the matrix is momentum m + (1 - momentum) g
 // (Nesterov) or m. Bound by HBM: 8 B read (6 with bf16 gradients) and 4 written per
@@ -173,9 +178,8 @@ __global__ __launch_bounds__(kNsBlock) void ns_norm_kernel(const NsMatrix *matri
             load_row<false>(mat.m, row * mat.cols + col, n, mat.vector, m);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float scaled = g[i] * step.grad_scale * step.one_minus;
-                m[i] = __builtin_fmaf(step.momentum, m[i], scaled);
-                g[i] = step.nesterov ? __builtin_fmaf(step.momentum, m[i], scaled) : m[i];
+                m[i] = mix(step, m[i], g[i]);
+                g[i] = step.nesterov ? mix(step, m[i], g[i]) : m[i];
             }
             if (!skip)
                 store_row(at, n, mat.vector, m);
@@ -214,11 +218,7 @@ __global__ __launch_bounds__(kNsBlock) void ns_convert_kernel(const NsMatrix *ma
             float m[8];
             load_row<false>(mat.m, row * mat.cols + col, n, mat.vector, m);
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                g[i] = step.nesterov
-                           ? __builtin_fmaf(step.momentum, m[i],
-                                            g[i] * step.grad_scale * step.one_minus)
-                           : m[i];
+            for (int i = 0; i < 8; ++i) g[i] = step.nesterov ? mix(step, m[i], g[i]) : m[i];
         }
         uint16_t *x = mat.x[0] + row * mat.ld + col;
         ushort4 hi[2], lo[2];

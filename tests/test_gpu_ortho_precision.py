@@ -96,3 +96,19 @@ def test_half_lists_of_every_tile(steps):
         outs = ops.Orthogonalizer(gs, steps=steps, precision="half").run()
         for i in list(range(0, len(gs), 37)) + [len(gs) - 1]:
             assert R.relative(outs[i], R.newton_schulz(gs[i], steps)) < HALF, (i, shapes[i])
+
+
+@pytest.mark.parametrize("momentum", [0.9, 0.95, 0.99, 0.999])
+@pytest.mark.parametrize("nesterov", [False, True])
+def test_muons_momentum_is_the_one_asked_for(momentum, nesterov):
+    """m, rounded once (2^-24 of it): within 2^-23 of the sum of its terms' magnitudes."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import Muon
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    for scale in (0.0, 1e-3, 1.0):  # of the old momentum; 0: m is (1 - momentum) g
+        x, g, m = (torch.randn(70, 90, generator=gen, device="cuda") for _ in range(3))
+        m.mul_(scale)
+        want = momentum * m.double() + (1.0 - momentum) * g.double()
+        size = momentum * m.double().abs() + (1.0 - momentum) * g.double().abs()
+        Muon([x], [g], m=[m], momentum=momentum, nesterov=nesterov).step()
+        assert bool(((m.double() - want).abs() <= 2.0 ** -23 * size).all())
