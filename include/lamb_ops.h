@@ -48,7 +48,7 @@ typedef enum lamb_ns_precision { LAMB_NS_HALF = 0, LAMB_NS_SPLIT = 1 } lamb_ns_p
 /*
  * The iteration: X = G / (||G||_F + eps), then `steps` times
  *   A = X X^T (or X^T X, on the shorter side),  X <- (a I + b A + c A A) X.
- * steps 1 to 64, eps >= 0 (with eps = 0 a zero matrix gives NaN), and a, b, c such
+ * steps 1 to 64, eps >= 0 (with eps = 0 a matrix of zeros gives NaN), and a, b, c such
  * that no singular value that starts in [0, 1] passes 2.75, nor the polynomial
  * 7.75, on the way (LAMB_EINVAL): the iteration's 16-bit numbers hold no more.
  */

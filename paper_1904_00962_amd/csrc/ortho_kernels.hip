@@ -209,7 +209,10 @@ __global__ __launch_bounds__(kNsBlock) void ns_convert_kernel(const NsMatrix *ma
     double sum = 0.0;
     for (int i = threadIdx.x; i < mat.blocks; i += kNsBlock) sum += partials[mat.first_block + i];
     sum = block_sum(sum, shared);
-    const float to_x = float(double(kNsScale) / (sqrt(sum) + double(step.eps)));
+    // below 2^-100 the quotient may pass fp32's range (eps 0): a power of two goes first
+    const double norm = sqrt(sum) + double(step.eps);
+    const float first = norm < 0x1p-100 ? 0x1p64f : 1.0f;
+    const float to_x = float(double(kNsScale) / (norm * double(first)));
     for_units(mat, [&](int64_t row, int col, int n) {
         float g[8];
         if (!MUON || step.nesterov)
@@ -226,7 +229,7 @@ __global__ __launch_bounds__(kNsBlock) void ns_convert_kernel(const NsMatrix *ma
         for (int h = 0; h < 2; ++h) {
             float v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = g[4 * h + i] * to_x;
+            for (int i = 0; i < 4; ++i) v[i] = g[4 * h + i] * first * to_x;
             hi[h] = high_halves(v);
             lo[h] = low_halves(v, hi[h]);
         }

@@ -112,3 +112,17 @@ def test_muons_momentum_is_the_one_asked_for(momentum, nesterov):
         size = momentum * m.double().abs() + (1.0 - momentum) * g.double().abs()
         Muon([x], [g], m=[m], momentum=momentum, nesterov=nesterov).step()
         assert bool(((m.double() - want).abs() <= 2.0 ** -23 * size).all())
+
+
+@pytest.mark.parametrize("sigma", [1e-30, 1e-34, 1e-37, 1e-40, 1e-43])
+@pytest.mark.parametrize("shape", [(40, 60), (1, 7), (3, 2)])
+def test_without_eps_no_matrix_is_too_small(sigma, shape):
+    """Down to denormal entries, which the input's rounding makes other numbers; the result
+    is that of these numbers, at any scale."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    g = (torch.randn(shape, generator=gen, dtype=torch.float64, device="cuda") * sigma).float()
+    assert bool(g.any())
+    o = ops.Orthogonalizer([g], eps=0.0).run()[0]
+    assert _off(torch, o, R.newton_schulz(g, eps=0.0)) <= SPLIT_OFF
