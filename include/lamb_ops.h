@@ -79,7 +79,9 @@ typedef struct lamb_matrix {
 /* A list of matrices that are worked on together, with their workspace: about
  * 4 bytes per element and 4 per entry of the short sides' squares (12 for matrices
  * at least twice as long as wide in lists with much to do), twice that with
- * LAMB_NS_SPLIT. One call may be in flight per plan; not thread-safe. */
+ * LAMB_NS_SPLIT. Calls share the workspace: one on another stream than the plan's last
+ * call waits for that one's work. Replays of a captured call are not seen; the caller
+ * orders them among themselves and with other calls. Not thread-safe. */
 typedef struct lamb_ns_plan lamb_ns_plan;
 
 /*

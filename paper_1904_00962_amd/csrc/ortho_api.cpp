@@ -28,6 +28,10 @@ struct lamb_ns_plan {
     TileList both, only_q, only_t, next_gram;  // of those with: Q and T, Q, T, A
     double *partials = nullptr;
     uint32_t *flag = nullptr;  // see launch_ns_check
+    // The end of the last call outside a capture, and its stream: see ordered().
+    hipEvent_t done = nullptr;
+    hipStream_t stream = nullptr;
+    bool used = false;
 };
 
 namespace {
@@ -249,6 +253,10 @@ lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
     hipError_t err = hipGetDevice(&plan->device);
     if (err != hipSuccess)
         return fail_hip(err, "hipGetDevice");
+    // only orders kernels of this device: no system-scope fence
+    err = hipEventCreateWithFlags(&plan->done, hipEventDisableTiming | hipEventDisableSystemFence);
+    if (err != hipSuccess)
+        return fail_hip(err, "hipEventCreateWithFlags");
     err = hipMalloc(&plan->block, bytes);
     if (err != hipSuccess) {
         plan->block = nullptr;
@@ -307,6 +315,31 @@ struct DeviceScope {
             (void)hipSetDevice(previous);
     }
 };
+
+// Calls of one plan share its workspace: one on another stream than the last waits for
+// that one. A captured call is left out; when its graph runs is the caller's to order.
+template <class F>
+lamb_status ordered(lamb_ns_plan *plan, hipStream_t stream, F enqueue) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    hipError_t err = hipStreamIsCapturing(stream, &capture);
+    if (err != hipSuccess)
+        return fail_hip(err, "hipStreamIsCapturing");
+    if (capture != hipStreamCaptureStatusNone)
+        return enqueue();
+    if (plan->used && plan->stream != stream) {
+        err = hipStreamWaitEvent(stream, plan->done, 0);
+        if (err != hipSuccess)
+            return fail_hip(err, "hipStreamWaitEvent");
+    }
+    const lamb_status st = enqueue();
+    // also after a failure: what went out before it uses the workspace
+    err = hipEventRecord(plan->done, stream);
+    plan->stream = stream;
+    plan->used = true;
+    if (st == LAMB_OK && err != hipSuccess)
+        return fail_hip(err, "hipEventRecord");
+    return st;
+}
 
 lamb_status run(lamb_ns_plan *plan, const lamb_ns_params &ns, NsStep step, uint32_t *flag,
                 int32_t *nonfinite_out, hipStream_t stream) {
@@ -368,6 +401,8 @@ lamb_status finish(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices, lamb_ns_
     if (st != LAMB_OK) {
         if (plan->block)
             (void)hipFree(plan->block);
+        if (plan->done)
+            (void)hipEventDestroy(plan->done);
         delete plan;
         return st;
     }
@@ -533,7 +568,8 @@ lamb_status lamb_orthogonalize(lamb_ns_plan *plan, const lamb_ns_params *params,
     if (st != LAMB_OK)
         return st;
     DeviceScope scope(plan->device);
-    return run(plan, *params, NsStep{}, nullptr, nullptr, static_cast<hipStream_t>(stream));
+    hipStream_t on = static_cast<hipStream_t>(stream);
+    return ordered(plan, on, [&] { return run(plan, *params, NsStep{}, nullptr, nullptr, on); });
 }
 
 lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void *stream_in,
@@ -569,25 +605,31 @@ lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void
     step.lr = hp->lr;
     step.nesterov = hp->nesterov;
     step.scale = hp->scale;
-    uint32_t *flag = nullptr;
-    if (hp->skip_nonfinite) {
-        const hipError_t err = launch_ns_check(plan->matrices, plan->block_matrix, plan->blocks,
-                                               plan->bf16_in, hp->grad_scale, plan->flag, stream);
-        if (err != hipSuccess)
-            return fail_hip(err, "kernel launch");
-        flag = plan->flag;
-    }
-    return run(plan, hp->ns, step, flag, nonfinite_out, stream);
+    return ordered(plan, stream, [&] {
+        uint32_t *flag = nullptr;
+        if (hp->skip_nonfinite) {
+            const hipError_t err =
+                launch_ns_check(plan->matrices, plan->block_matrix, plan->blocks, plan->bf16_in,
+                                hp->grad_scale, plan->flag, stream);
+            if (err != hipSuccess)
+                return fail_hip(err, "kernel launch");
+            flag = plan->flag;
+        }
+        return run(plan, hp->ns, step, flag, nonfinite_out, stream);
+    });
 }
 
 lamb_status lamb_ns_plan_destroy(lamb_ns_plan *plan) {
     if (!plan)
         return LAMB_OK;
     DeviceScope scope(plan->device);
-    const hipError_t err = hipFree(plan->block);
+    hipError_t err = hipFree(plan->block);  // waits for what still uses it
+    const hipError_t event = hipEventDestroy(plan->done);
+    if (err == hipSuccess)
+        err = event;
     delete plan;
     if (err != hipSuccess)
-        return fail_hip(err, "hipFree");
+        return fail_hip(err, "hipFree, hipEventDestroy");
     return LAMB_OK;
 }
 

@@ -82,15 +82,20 @@ class Orthogonalizer:
 
     ``inputs`` and ``outputs`` are persistent 2-D tensors (float32 or bfloat16, one
     type each, rows contiguous); ``run()`` reads the inputs as they are then. An
-    output may be its own input. ``precision``: "split" (the default) rounds the products'
-    operands to pairs of 16-bit floats (22 bits, an error as of fp32), "half" to one (11
-    bits, a third of the work). "half" has to be asked for: its error depends on the singular values.
-    The steps multiply the small ones by up to 485 (by default), and the rounding of the
-    large ones with them: 1.3e-3 off (2-norm, relative) for independent entries, 1e-2
-    where the singular values span decades, 1e-1 where a few outweigh the rest, as a
-    network's gradients and momenta often have it.
+    output may be its own input.
+
+    ``precision``: "split" (the default) rounds the products' operands to pairs of 16-bit
+    floats (22 bits, an error as of fp32), "half" to one (11 bits, a third of the work).
+    "half" has to be asked for: its error depends on the singular values. The steps
+    multiply the small ones by up to 485 (by default), and the rounding of the large ones
+    with them: 1.3e-3 off (2-norm, relative) for independent entries, 1e-2 where the
+    singular values span decades, 1e-1 where a few outweigh the rest, as a network's
+    gradients and momenta often have it.
+
     The plan keeps a workspace of about 4 bytes per element, and 4 to 12 per entry of the
-    short sides' squares; twice that for "split".
+    short sides' squares; twice that for "split". Calls share it, so one on another stream
+    than the last waits for that one; replays of a captured call are the caller's to
+    order, and so is what else uses the inputs and outputs.
     """
 
     def __init__(self, inputs: Sequence, outputs: Optional[Sequence] = None, steps: int = 5,

@@ -350,7 +350,9 @@ class Muon:
     fp32's accuracy; "half" is up to three times faster and moves the direction, as
     ``ops.Orthogonalizer`` says, by 1e-3 to 1e-1: least for independent entries, most where
     a few singular values outweigh the rest. ``grad_scale``, ``skip_nonfinite`` and
-    ``schedule`` as for ``LAMB``; a skipped step sets ``found_nonfinite``.
+    ``schedule`` as for ``LAMB``; a skipped step sets ``found_nonfinite``. A step on another
+    stream than the last waits for that one; replays of a captured step are the caller's to
+    order.
     """
 
     def __init__(self, params: Sequence, grads: Sequence, lr: float = 1e-3,
