@@ -7,7 +7,9 @@
  * unless marked host; the caller owns every tensor; arguments are validated on
  * the host before any HIP call; work is enqueued on `stream` and nothing is
  * synchronised, allocated or copied to the host (plan creation and destruction
- * aside); lamb_last_error() describes a failure. Nothing throws.
+ * aside); lamb_last_error() describes a failure. Nothing throws. Memory that a call
+ * writes may not overlap any other of its operands (LAMB_EOVERLAP); operands of one row
+ * stride may lie between each other's rows, as the column slices of a buffer do.
  */
 #ifndef LAMB_OPS_H
 #define LAMB_OPS_H
@@ -65,7 +67,7 @@ LAMB_API lamb_status lamb_ns_params_init(lamb_ns_params *params);
 /*
  * One matrix to orthogonalize, row-major with rows `*_stride` elements apart
  * (>= cols, at most 2^36). rows and cols 1 to 2^20, aligned to their element. A row or column
- * vector is a matrix of short side 1. No output may overlap an input of the plan
+ * vector is a matrix of short side 1. No output may share memory with an input of the plan
  * or another output, but for an input that has the output's address, type and
  * stride (in place).
  */

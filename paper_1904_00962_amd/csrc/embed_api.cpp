@@ -88,9 +88,8 @@ lamb_status lamb_embed_forward(const lamb_embed *embed, const void *table, int64
         return st;
     Span spans[] = {
         span_of(e.ids, uint64_t(e.tokens * size_of(e.id_dtype)), false, 0, "ids"),
-        span_of(table, rows_bytes(e.vocab, table_stride, e.dim, size_of(table_dtype)), false, 0,
-                "table"),
-        span_of(out, rows_bytes(e.tokens, out_stride, e.dim, size_of(out_dtype)), true, 0, "out")};
+        span_of_rows(table, e.vocab, table_stride, e.dim, size_of(table_dtype), false, 0, "table"),
+        span_of_rows(out, e.tokens, out_stride, e.dim, size_of(out_dtype), true, 0, "out")};
     st = check_spans(spans, sizeof spans / sizeof spans[0]);
     if (st != LAMB_OK || e.tokens == 0)
         return st;
@@ -139,11 +138,10 @@ lamb_status lamb_embed_backward(const lamb_embed *embed, const void *grad_out,
         return st;
     Span spans[] = {
         span_of(e.ids, uint64_t(e.tokens * size_of(e.id_dtype)), false, 0, "ids"),
-        span_of(grad_out, rows_bytes(e.tokens, grad_out_stride, e.dim, size_of(grad_out_dtype)),
-                false, 0, "grad_out"),
-        span_of(grad_table,
-                rows_bytes(e.vocab, grad_table_stride, e.dim, size_of(grad_table_dtype)), true, 0,
-                "grad_table"),
+        span_of_rows(grad_out, e.tokens, grad_out_stride, e.dim, size_of(grad_out_dtype), false, 0,
+                     "grad_out"),
+        span_of_rows(grad_table, e.vocab, grad_table_stride, e.dim, size_of(grad_table_dtype), true,
+                     0, "grad_table"),
         span_of(workspace, l.bytes, true, 0, "workspace")};
     st = check_spans(spans, sizeof spans / sizeof spans[0]);
     if (st != LAMB_OK || (e.tokens == 0 && add))

@@ -58,17 +58,42 @@ inline bool aligned_to(const void *p, uintptr_t bytes) {
 
 inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 
-// Memory that a call reads or writes, for the overlap check.
+// Memory that a call reads or writes, for the overlap check: bytes lo to hi, or of these
+// `row` at every multiple of `stride` from lo on.
 struct Span {
     uintptr_t lo, hi;
     bool written;
     int32_t index;
     const char *what;
+    uint64_t row, stride;  // stride 0: every byte
 };
 
 inline Span span_of(const void *p, uint64_t bytes, bool written, int32_t index, const char *what) {
     const uintptr_t lo = reinterpret_cast<uintptr_t>(p);
-    return Span{lo, lo + uintptr_t(bytes), written, index, what};
+    return Span{lo, lo + uintptr_t(bytes), written, index, what, bytes, 0};
+}
+
+// `rows` rows of `cols` elements, `stride` elements apart; rows 0: no memory.
+inline Span span_of_rows(const void *p, int64_t rows, int64_t stride, int64_t cols, int64_t size,
+                         bool written, int32_t index, const char *what) {
+    const uint64_t bytes = rows ? uint64_t((rows - 1) * stride + cols) * uint64_t(size) : 0;
+    Span s = span_of(p, bytes, written, index, what);
+    if (rows > 1) {
+        s.row = uint64_t(cols * size);
+        s.stride = uint64_t(stride * size);
+    }
+    return s;
+}
+
+// Whether two spans, s.lo <= t.lo, share a byte. Rows of one stride may lie between each
+// other, as column slices of one buffer do; of two strides only the ends are looked at.
+inline bool share_bytes(const Span &s, const Span &t) {
+    if (t.lo >= s.hi || t.lo == t.hi)
+        return false;
+    if (s.stride == 0 || (t.stride != 0 && t.stride != s.stride))
+        return true;
+    const uint64_t at = uint64_t(t.lo - s.lo) % s.stride;
+    return at < s.row || t.row > s.stride - at;
 }
 
 // Written memory overlaps nothing; what is only read may overlap. Sorts the spans.
@@ -76,18 +101,16 @@ inline lamb_status check_spans(Span *spans, size_t n) {
     std::sort(spans, spans + n, [](const Span &p, const Span &q) {
         return p.lo != q.lo ? p.lo < q.lo : p.hi < q.hi;
     });
-    const Span *read = nullptr, *wrote = nullptr;  // the furthest-reaching so far
+    uintptr_t read_to = 0, written_to = 0;  // the furthest ends so far
     for (size_t i = 0; i < n; ++i) {
         const Span &s = spans[i];
-        const Span *other = wrote && s.lo < wrote->hi               ? wrote
-                            : s.written && read && s.lo < read->hi ? read
-                                                                    : nullptr;
-        if (other && s.hi > s.lo)
-            return fail(LAMB_EOVERLAP, "%s (%d) overlaps %s (%d)", s.what, s.index, other->what,
-                        other->index);
-        const Span *&far = s.written ? wrote : read;
-        if (!far || s.hi > far->hi)
-            far = &s;
+        const bool near = s.lo < written_to || (s.written && s.lo < read_to);
+        for (size_t k = 0; near && k < i; ++k)
+            if ((s.written || spans[k].written) && share_bytes(spans[k], s))
+                return fail(LAMB_EOVERLAP, "%s (%d) overlaps %s (%d)", s.what, s.index,
+                            spans[k].what, spans[k].index);
+        uintptr_t &far = s.written ? written_to : read_to;
+        far = std::max(far, s.hi);
     }
     return LAMB_OK;
 }
@@ -103,11 +126,6 @@ inline bool is_float(int32_t dtype) {
 inline bool is_id(int32_t dtype) { return dtype == LAMB_DTYPE_I32 || dtype == LAMB_DTYPE_I64; }
 inline int64_t size_of(int32_t dtype) {
     return dtype == LAMB_DTYPE_BF16 ? 2 : dtype == LAMB_DTYPE_I64 ? 8 : 4;
-}
-
-// Bytes from the first to the last element of `rows` rows.
-inline uint64_t rows_bytes(int64_t rows, int64_t stride, int64_t cols, int64_t size) {
-    return rows ? uint64_t((rows - 1) * stride + cols) * uint64_t(size) : 0;
 }
 
 inline lamb_status check_workspace(const void *workspace, size_t bytes, size_t need) {

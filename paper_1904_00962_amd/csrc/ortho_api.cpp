@@ -475,10 +475,10 @@ lamb_status lamb_ortho_plan_create(const lamb_matrix *matrices, int32_t n, int32
             const bool in_place =
                 t.in == t.out && in_dtype == out_dtype && t.in_stride == t.out_stride;
             if (!in_place)
-                spans.push_back(span_of(
-                    t.in, rows_bytes(t.rows, t.in_stride, t.cols, in_size), false, i, "in"));
-            spans.push_back(span_of(
-                t.out, rows_bytes(t.rows, t.out_stride, t.cols, out_size), true, i, "out"));
+                spans.push_back(
+                    span_of_rows(t.in, t.rows, t.in_stride, t.cols, in_size, false, i, "in"));
+            spans.push_back(
+                span_of_rows(t.out, t.rows, t.out_stride, t.cols, out_size, true, i, "out"));
             NsMatrix m{};
             m.in = t.in;
             m.out = t.out;

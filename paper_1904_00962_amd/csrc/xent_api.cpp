@@ -238,8 +238,8 @@ lamb_status lamb_xent_forward(const lamb_xent *xent, float *loss, float *lse, fl
         return st;
     const int64_t id = size_of(x.target_dtype);
     Span spans[] = {
-        span_of(x.hidden, rows_bytes(x.tokens, x.hidden_stride, x.dim, 2), false, 0, "hidden"),
-        span_of(x.table, rows_bytes(x.vocab, x.table_stride, x.dim, 2), false, 0, "table"),
+        span_of_rows(x.hidden, x.tokens, x.hidden_stride, x.dim, 2, false, 0, "hidden"),
+        span_of_rows(x.table, x.vocab, x.table_stride, x.dim, 2, false, 0, "table"),
         span_of(x.targets, uint64_t(x.tokens * id), false, 0, "targets"),
         span_of(loss, uint64_t(x.tokens) * 4, true, 0, "loss"),
         span_of(lse, uint64_t(x.tokens) * 4, true, 0, "lse"),
@@ -298,17 +298,15 @@ lamb_status lamb_xent_backward(const lamb_xent *xent, const float *lse,
         return st;
     const int64_t id = size_of(x.target_dtype);
     Span spans[] = {
-        span_of(x.hidden, rows_bytes(x.tokens, x.hidden_stride, x.dim, 2), false, 0, "hidden"),
-        span_of(x.table, rows_bytes(x.vocab, x.table_stride, x.dim, 2), false, 0, "table"),
+        span_of_rows(x.hidden, x.tokens, x.hidden_stride, x.dim, 2, false, 0, "hidden"),
+        span_of_rows(x.table, x.vocab, x.table_stride, x.dim, 2, false, 0, "table"),
         span_of(x.targets, uint64_t(x.tokens * id), false, 0, "targets"),
         span_of(lse, uint64_t(x.tokens) * 4, false, 0, "lse"),
         span_of(g.grad_loss, g.grad_loss ? 4 : 0, false, 0, "grad_loss"),
-        span_of(g.grad_hidden,
-                g.grad_hidden ? rows_bytes(x.tokens, g.grad_hidden_stride, x.dim, 2) : 0, true, 0,
-                "grad_hidden"),
-        span_of(g.grad_table,
-                g.grad_table ? rows_bytes(x.vocab, g.grad_table_stride, x.dim, bf16 ? 2 : 4) : 0,
-                true, 0, "grad_table"),
+        span_of_rows(g.grad_hidden, g.grad_hidden ? x.tokens : 0, g.grad_hidden_stride, x.dim, 2,
+                     true, 0, "grad_hidden"),
+        span_of_rows(g.grad_table, g.grad_table ? x.vocab : 0, g.grad_table_stride, x.dim,
+                     bf16 ? 2 : 4, true, 0, "grad_table"),
         span_of(workspace, l.bytes, true, 0, "workspace")};
     st = check_spans(spans, sizeof spans / sizeof spans[0]);
     if (st != LAMB_OK)
