@@ -76,6 +76,15 @@ def _on_gpu(name, t, device=None):
         raise ValueError("%s is on another device" % name)
 
 
+def _no_graph(name, *tensors):
+    """The operators record nothing for autograd: a result whose gradient would be lost
+    without a word is refused."""
+    if _torch().is_grad_enabled() and any(t.requires_grad for t in tensors):
+        raise ValueError("%s records no gradient for a tensor that requires one: pass "
+                         "tensor.detach(), or call it under torch.no_grad(), and take the "
+                         "gradient from %s_grad" % (name, name))
+
+
 class Orthogonalizer:
     """X of each input G after ``steps`` times X <- (a I + b A + c A A) X, A = X X^T,
     from X = G / (||G||_F + eps): G with its singular values moved towards 1.
@@ -195,8 +204,12 @@ def linear_cross_entropy(hidden, table, targets, *, ignore_index: int = -100):
     rows, ``targets`` int32 or int64. Tokens whose target is ``ignore_index`` do not
     count: loss 0, and the mean is over the others (0 without any). A target outside
     the vocabulary gives NaN. ``lse`` is what :func:`linear_cross_entropy_grad` needs.
+
+    Autograd does not see the call: tensors that require gradients are refused where
+    grad mode is on (pass them detached).
     """
     torch = _torch()
+    _no_graph("linear_cross_entropy", hidden, table)
     x = _xent(hidden, table, targets, ignore_index)
     need = _ops.lamb_xent_workspace(x, False)
     out = torch.empty(2, hidden.shape[0], dtype=torch.float32, device=hidden.device)
@@ -263,8 +276,10 @@ def embedding(ids, table, *, scale: float = 1.0, out_dtype=None, out=None):
     """``scale`` x the rows of ``table`` [vocab, dim] (float32 or bfloat16) that ``ids``
     (int32 or int64, any shape) name: a tensor [*ids.shape, dim] of ``out_dtype`` (the
     table's by default), or ``out`` [ids.numel(), dim]. An id outside the table gives a
-    row of NaN."""
+    row of NaN. Autograd does not see the call: a table that requires a gradient is refused
+    where grad mode is on (pass it detached)."""
     torch = _torch()
+    _no_graph("embedding", table, *(() if out is None else (out,)))
     device, dtype = table.device, table.dtype
     stride = _rows("table", table, dtype)
     e = _embed(ids, table, scale, device)
