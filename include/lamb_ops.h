@@ -160,8 +160,9 @@ LAMB_API lamb_status lamb_ns_plan_destroy(lamb_ns_plan *plan);
  * Softmax cross entropy of hidden states against a vocabulary table:
  * logits = hidden table^T, loss_i = logsumexp(logits_i) - logits_i[target_i].
  * hidden [tokens][dim] and table [vocab][dim] are bfloat16, rows `*_stride` elements
- * apart (>= dim), 2-byte aligned. They are read in place where rows are 16-byte
- * aligned and dim is a multiple of 8; else the table is copied to the workspace first.
+ * apart (>= dim), 2-byte aligned. Every call copies the rows of hidden whose tokens count
+ * to the workspace. The table is read in place where its rows are 16-byte aligned and at
+ * most 2^21 elements apart and dim is a multiple of 8; else it is copied too.
  * targets: LAMB_DTYPE_I32 or _I64. A token whose target is ignore_index does not
  * count: its loss and gradient are 0 and nothing that its row holds reaches any
  * result. Any other target outside [0, vocab) makes that token's loss and lse NaN, and
@@ -180,8 +181,18 @@ typedef struct lamb_xent {
 } lamb_xent;
 
 /* Bytes of device workspace (256-byte aligned) that a forward and a backward call need;
- * host only. The backward holds a piece of the vocabulary's softmax, at most about
- * 160 MiB, beside the hidden states and their gradient in fp32. */
+ * host only. For T tokens, V words and rows of D columns (dim rounded up to 8), at most,
+ * beside a few KiB of alignment:
+ *  both      (2 D + 8) T for the rows that count, packed together, and 2 D V for the table
+ *            where it is copied
+ *  forward   8 T for every tile of 64 words, and 4 T (large calls take tiles of 128 or 256
+ *            words: 1.6 GiB for 2^20 tokens against 50257)
+ *  backward  160 MiB, or 512 T where that is more (from 327,681 tokens on), for a piece of
+ *            the vocabulary's softmax; 4 D T for the hidden states' gradient in fp32,
+ *            whether it is asked for or not, and 128 MiB of parts of it where workgroups
+ *            share the sums of few rows; from 32,769 tokens on 10,240 D for a piece of the
+ *            table's gradient
+ */
 LAMB_API lamb_status lamb_xent_workspace(const lamb_xent *xent, size_t *forward_bytes,
                                          size_t *backward_bytes);
 

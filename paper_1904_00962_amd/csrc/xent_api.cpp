@@ -11,7 +11,7 @@ namespace {
 
 constexpr int64_t kMaxReadStride = int64_t(1) << 21;  // a tile's rows within 32-bit offsets
 // A piece of the vocabulary's softmax: written once and read twice, so kept within
-// the 256 MiB last-level cache.
+// the 256 MiB last-level cache, unless so many tokens leave it fewer than kPieceAlign words.
 constexpr int64_t kPieceBytes = int64_t(160) << 20;
 constexpr int64_t kPieceAlign = 256;  // half of it where Q is in two parts
 
@@ -91,7 +91,8 @@ struct Pieces {
 // the one whose products fill their last rounds of workgroups best.
 Pieces pick_pieces(const lamb_xent &x, int32_t q_parts) {
     const int64_t rows = x.tokens ? x.tokens : 1, align = kPieceAlign / q_parts;
-    const int64_t most = std::max<int64_t>(align, kPieceBytes / 2 / q_parts / rows);
+    const int64_t most =
+        std::max<int64_t>(align, kPieceBytes / 2 / q_parts / rows / align * align);
     const int64_t least = (x.vocab + most - 1) / most;
     Pieces best;
     for (int64_t count = least; count < least + 4; ++count) {
