@@ -250,8 +250,8 @@ LAMB_API lamb_status lamb_embed_forward(const lamb_embed *embed, const void *tab
 
 /*
  * The table's gradient: grad_table[v] = (or, with `add` 1, +=) scale times the sum of
- * grad_out[i] over the tokens with ids[i] = v, in the tokens' order and in fp32: the
- * same inputs give the same bits. Tokens whose id is outside the table or equals
+ * grad_out[i] over the tokens with ids[i] = v, in the tokens' order and in fp32, 16 tokens,
+ * then 64 such sums at a time: the same inputs give the same bits. Tokens whose id is outside the table or equals
  * padding_id (-1 for none) add nothing. Without `add` every row is written; with it,
  * only rows that tokens name are touched. lamb_embed_workspace gives the device
  * workspace's bytes (256-byte aligned; host only).

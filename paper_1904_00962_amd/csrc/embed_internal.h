@@ -40,6 +40,9 @@ constexpr int32_t sort_ids(int64_t tokens) {
 constexpr int32_t kSumTokens = 16;
 constexpr int32_t kZeroRows = 8;
 constexpr int32_t kSumColumns = 512;
+// Joining: chunks' sums that are added up by themselves, before they join the others, so
+// that a chain of fp32 sums stays short: 2^20 like rows of one id end 6e-4 off in one chain.
+constexpr int64_t kJoinChunks = 64;
 
 // order[0 .. first[vocab]): the tokens in the order of their ids, those of one id in
 // theirs; first[v]: where id v's tokens begin. Ids outside the table and `skip` are

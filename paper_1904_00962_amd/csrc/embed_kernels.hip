@@ -7,13 +7,13 @@
 // Sorting takes one launch. Each workgroup owns a range of ids and reads all ids twice:
 // once to count its own (per wave's share of the tokens) and the smaller ones, which
 // gives every id its place, and once to put its tokens there. The ids are read from L2,
-// up to 8192 of them only once.
+// up to 8192 of them only once: with many, tokens x vocab / 512 readings.
 //
-// Summing cuts the sorted order, not the table, into equal chunks, so that a frequent
-// id (or a batch of padding) is spread over many waves. An id's tokens that lie within
-// a chunk are summed and written; what reaches over a chunk's ends goes to a partial
-// sum, and a second pass joins these. Rows without tokens are written as zeros by the
-// first pass, unless the gradient is added to what is there.
+// Summing cuts the sorted order, not the table, into equal chunks, so that the rows of a
+// frequent id (or a batch of padding) are read by many waves. An id's tokens that lie
+// within a chunk are summed and written; what reaches over a chunk's ends goes to a
+// partial sum, and a second pass joins these, an id's in one wave. Rows without tokens are
+// written as zeros by the first pass, unless the gradient is added to what is there.
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -253,9 +253,10 @@ __device__ inline void finish(const EmbedArgs &a, const EmbedGrad &g, int64_t id
 }
 
 // Waves of the first `chunks` x (columns / kSumColumns) sum a chunk's columns; where the
-// gradient is not added, the waves after them write the rows without tokens. Bound by HBM
-// where it writes the whole table: 8192 bf16 rows of 1024 into 30522 fp32 ones take 22 us,
-// 6.4 TB/s (23.4 where ADD was no template argument: the old rows hold 64 registers).
+// gradient is not added, the waves after them write the rows without tokens. Bound by
+// writing where it writes the whole table: 8192 bf16 rows of 1024 into 30522 fp32 ones take
+// 22 us, 6.4 TB/s, in runs that follow one another, whose table the last-level cache holds
+// in part (a fill of 4 GiB writes 6.9 TB/s, a copy of 1 GiB moves 5.1) (23.4 us where ADD was no template argument: the old rows hold 64 registers).
 // Added to 50257 bf16 rows of 1600, 18.7 us, 2.6 TB/s: latency, few rows are touched.
 template <bool ROWS_BF16, bool TABLE_BF16, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedGrad g) {
@@ -346,7 +347,10 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedGrad g
 }
 
 // A wave per chunk and kSumColumns columns: if an id begins in the chunk and goes on,
-// its partial sums from there on, in order. Bound by latency: 5 us for 8192 tokens.
+// its partial sums from there on, in order, kJoinChunks at a time. Bound by latency: 5 us
+// for 8192 tokens of text. An id that holds all tokens is one wave's for each kSumColumns
+// columns, with a partial sum for every 16 tokens: calls of 2^17 and 2^20 tokens of 64
+// columns take 0.70 and 5.5 ms so, 0.10 and 0.83 where the ids are spread over 50257.
 template <bool TABLE_BF16, bool ADD>
 __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, EmbedGrad g) {
     const int lane = threadIdx.x & 63;
@@ -366,12 +370,19 @@ __global__ __launch_bounds__(256) void embed_join_kernel(EmbedArgs a, EmbedGrad 
     if (ADD)
         load8<TABLE_BF16>(g.table, id * g.table_stride + c, a.dim - c, g.vector, old);
     load8<false>(g.partial, (2 * chunk + 1) * g.columns + c, 8, true, sum);
-#pragma unroll 8
-    for (int64_t k = chunk + 1; k <= last; ++k) {
-        float part[8];
-        load8<false>(g.partial, 2 * k * g.columns + c, 8, true, part);
+    for (int64_t k0 = chunk + 1; k0 <= last; k0 += kJoinChunks) {
+        const int64_t end = k0 + kJoinChunks <= last ? k0 + kJoinChunks : last + 1;
+        float part[8], group[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum[i] += part[i];
+        for (int i = 0; i < 8; ++i) group[i] = k0 == chunk + 1 ? sum[i] : 0.0f;
+#pragma unroll 8
+        for (int64_t k = k0; k < end; ++k) {
+            load8<false>(g.partial, 2 * k * g.columns + c, 8, true, part);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) group[i] += part[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] = k0 == chunk + 1 ? group[i] : sum[i] + group[i];
     }
     finish<TABLE_BF16, ADD>(a, g, id, c, sum, old);
 }
