@@ -34,7 +34,7 @@ typedef enum lamb_dtype {
 /*
  * How the products of the Newton-Schulz iteration round their operands.
  *  LAMB_NS_SPLIT  to the sum of two 16-bit floats (22 bits), three products for one:
- *                 errors as of fp32 arithmetic.
+ *                 errors as of fp32 arithmetic that rounds a sum once in 32 terms.
  *  LAMB_NS_HALF   to one (11 bits). X, of norm 1, is so rounded to 2^-11 of itself at
  *                 most, and the iteration multiplies what is small in it by up to
  *                 |a|^steps (485 by default): the result is off by up to 0.25, beside

@@ -137,7 +137,8 @@ void for_tiles(int32_t rows, int32_t cols, int shape, F f) {
 // their launches cost: BERT-Large's matrices (split, a third of them
 // 1024 x 4096 or turned) take 15.0 ms a Muon step with chains and 18.6 without,
 // ResNet-50's 1.00 and 1.16. Where the estimate says no: four matrices up to 256 x 1024
-// would take 111 us in place of 94, a list around one of 2048 x 2048 979 in place of 900.
+// would take 111 us in place of 94 (16-bit), a list around one of 2048 x 2048 979 in place
+// of 900 (split).
 void pick_chains(std::vector<NsMatrix> &matrices, bool split) {
     constexpr double kFlopsPerUs = 1e9, kChainUs = 100.0;
     const double turns = split ? kNsChainSplit : kNsChainHalf;

@@ -55,8 +55,9 @@ struct NsTile {
 // iteration beside S^3 for Q, in place of 3 L S^2. The rounding of A hides singular
 // values below its square root, and n iterations multiply what it hides by up to
 // 3.4^(2 n): chains are kept to kNsChainSplit and kNsChainHalf iterations, which leave
-// the result as exact as direct iterations do (256 x 1024 matrices of rank 32 and noise:
-// 3.1e-6 and 3.3e-3 off, 2.5e-6 and 3.3e-3 directly; five at once: 1e-4 and 8e-2).
+// the result as exact as direct iterations do (256 x 1024 matrices of rank 32 and 1e-2 of
+// noise: 6.9e-6 and 1.7e-2 off, 9.7e-6 and 2.1e-2 directly; rank 1 and 1e-4: 6.6e-5 and
+// 1.4e-1, 5.9e-5 and 1.5e-1. Five at once ended some 30 times as far off).
 constexpr int32_t kNsChainSplit = 3, kNsChainHalf = 2;
 // Q is held times kNsQScale: its entries reach those of P to the third power.
 constexpr float kNsQScale = 128.0f;
@@ -78,7 +79,7 @@ struct NsStep {
     float decay;                 // x <- decay x - lr s O (decay 1 where the mask is off)
     float lr;
     int32_t nesterov;
-    int32_t scale;              // a lamb_muon_scale
+    int32_t scale;               // a lamb_muon_scale
 };
 
 // Elementwise passes over `blocks` workgroups (block_matrix: each one's matrix).
