@@ -37,7 +37,7 @@ typedef enum lamb_dtype {
  *                 errors as of fp32 arithmetic that rounds a sum once in 32 terms.
  *  LAMB_NS_HALF   to one (11 bits). X, of norm 1, is so rounded to 2^-11 of itself at
  *                 most, and the iteration multiplies what is small in it by up to
- *                 |a|^steps (485 by default): the result is off by up to 0.25, beside
+ *                 |a|^steps (485 by default): the result is off by up to 0.3, beside
  *                 its own norm of about sqrt(min(rows, cols)) where most singular
  *                 values reach 1. Relative, as 2-norms: 1.3e-3 for independent entries,
  *                 4e-3 to 1.5e-2 for singular values that fall evenly over 2 to 6
@@ -250,11 +250,11 @@ LAMB_API lamb_status lamb_embed_forward(const lamb_embed *embed, const void *tab
 
 /*
  * The table's gradient: grad_table[v] = (or, with `add` 1, +=) scale times the sum of
- * grad_out[i] over the tokens with ids[i] = v, in the tokens' order and in fp32, 16 tokens,
- * then 64 such sums at a time: the same inputs give the same bits. Tokens whose id is outside the table or equals
- * padding_id (-1 for none) add nothing. Without `add` every row is written; with it,
- * only rows that tokens name are touched. lamb_embed_workspace gives the device
- * workspace's bytes (256-byte aligned; host only).
+ * grad_out[i] over the tokens with ids[i] = v, in the tokens' order and in fp32, at most
+ * 16 tokens, then 64 such sums at a time: the same inputs give the same bits. Tokens whose
+ * id is outside the table or equals padding_id (-1 for none) add nothing. Without `add`
+ * every row is written; with it, only rows that tokens name are touched.
+ * lamb_embed_workspace gives the device workspace's bytes (256-byte aligned; host only).
  */
 LAMB_API lamb_status lamb_embed_workspace(const lamb_embed *embed, size_t *bytes);
 

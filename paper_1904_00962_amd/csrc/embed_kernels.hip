@@ -256,8 +256,8 @@ __device__ inline void finish(const EmbedArgs &a, const EmbedGrad &g, int64_t id
 // gradient is not added, the waves after them write the rows without tokens. Bound by
 // writing where it writes the whole table: 8192 bf16 rows of 1024 into 30522 fp32 ones take
 // 22 us, 6.4 TB/s, in runs that follow one another, whose table the last-level cache holds
-// in part (a fill of 4 GiB writes 6.9 TB/s, a copy of 1 GiB moves 5.1) (23.4 us where ADD was no template argument: the old rows hold 64 registers).
-// Added to 50257 bf16 rows of 1600, 18.7 us, 2.6 TB/s: latency, few rows are touched.
+// in part (a fill of 4 GiB writes 6.9 TB/s, a copy of 1 GiB moves 5.1); 23.4 us where ADD was
+// no template argument, as the old rows hold 64 registers. Added to 50257 bf16 rows of 1600, 18.7 us, 2.6 TB/s: latency, few rows are touched.
 template <bool ROWS_BF16, bool TABLE_BF16, bool ADD>
 __global__ __launch_bounds__(256) void embed_sum_kernel(EmbedArgs a, EmbedGrad g) {
     const int lane = threadIdx.x & 63;

@@ -420,7 +420,8 @@ __global__ __launch_bounds__(256) void xent_hidden_out_kernel(XentArgs a, int32_
 
 // dW's rows of a piece = Q^T H, the sum over the tokens that count, in chains of
 // kChainTokens. Both operands are read transposed from LDS. Bound by the matrix cores: 208 us
-// for a sixth of 50257 words, 8192 tokens of 1600, 1.06 PFLOP/s. An fp32 result takes the products with both parts of Q.
+// for a sixth of 50257 words, 8192 tokens of 1600, 1.06 PFLOP/s. An fp32 result takes the
+// products with both parts of Q.
 template <class Shape, bool BF16, bool ADD>
 __global__ __launch_bounds__(Shape::kThreads, Shape::kPerCu) void xent_table_kernel(
     XentArgs a, XentPiece piece, const float *grad_loss, float grad_scale, bool mean,
