@@ -213,7 +213,8 @@ LAMB_API lamb_status lamb_xent_forward(const lamb_xent *xent, float *loss, float
  * Both are sums of the softmax less one at the target, times rows. For 16-bit gradients
  * it is rounded to bfloat16, each entry by itself: as 2-norms they are 1.7e-3 off, by
  * their own rounding, to 2.5e-3, where the terms are of one size and few. For an fp32
- * grad_table it is held in 16 bits (2^-16 of each entry at most), for a product more.
+ * grad_table it is held in 16 bits (2^-16 of each entry at most), for a product more. lse
+ * as an fp32 number adds 2^-24 of the largest logit to either.
  */
 typedef struct lamb_xent_grads {
     const float *grad_loss;

@@ -254,9 +254,11 @@ __global__ __launch_bounds__(256) void xent_reduce_kernel(XentArgs a, int32_t n_
         for (int g = 1; g < 16; ++g) sum = join(sum, shared[g][t]);
         const int token = a.source[m];
         const bool inside = a.target[m] >= 0;
-        const float total = sum.x + logf(sum.y);
-        const float mine = inside ? total - at_target[m] : NAN;
-        lse[token] = inside ? total : NAN;
+        // the loss not from lse, whose last place is that of the largest logit: a token whose
+        // target is far ahead has a loss much smaller than that
+        const float rest = logf(sum.y);
+        const float mine = inside ? (sum.x - at_target[m]) + rest : NAN;
+        lse[token] = inside ? sum.x + rest : NAN;
         loss[token] = mine;
         value = mine;
     }

@@ -102,3 +102,36 @@ def test_many_tokens_add_to_an_older_gradient():
         if dtype == torch.bfloat16:  # q's rounding, 2^-8 in place of 2^-16, and the result's
             bound = 2 ** 8 * bound + 2.0 ** -8 * torch.linalg.vector_norm(before + want)
         assert float(off) <= float(bound)
+
+
+@pytest.mark.parametrize("tokens,vocab", [(5, 300), (200, 3000), (1500, 50257)])
+@pytest.mark.parametrize("level", [0.0, 128.0, 2048.0])
+def test_losses_of_tokens_whose_target_is_far_ahead(tokens, vocab, level):
+    """Logits that are sums of few exact terms, one word's 1 to 16 above the others' and all
+    of them `level` higher. A loss is then off by the roundings of a sum of exponentials near
+    or above 1: some 16 in a tile's lanes, 8 joins in it, and vocab / 64 / 16 + 16 of the
+    tiles' parts, 2^-23 each (a product and a sum), and by three more of itself and the
+    logarithm."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    h = torch.zeros(tokens, 16, dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros(vocab, 16, dtype=torch.bfloat16, device="cuda")
+    h[:, 0], w[:, 0] = 1.0, level
+    t = torch.randint(0, vocab, (tokens,), generator=gen, device="cuda")
+    # column 1: every word but one is behind by the token's own factor; column 2: a little more
+    h[:, 1] = torch.randint(1, 17, (tokens,), generator=gen, device="cuda").bfloat16()
+    w[:, 2] = torch.randint(-8, 1, (vocab,), generator=gen, device="cuda").bfloat16() / 8
+    w[t, 2] = 0.0
+    h[:, 2] = 1.0
+    t[:] = t[0]
+    w[:, 1] = -1.0
+    w[t[0], 1] = 0.0
+    z = h.double() @ w.double().t().contiguous() - level
+    own = z[torch.arange(tokens, device="cuda"), t]
+    want = torch.log1p((torch.exp(z - own[:, None]).sum(dim=1) - 1.0).clamp(min=0.0))
+    mean, loss, _ = ops.linear_cross_entropy(h, w, t)
+    bound = (24 + vocab / 1024 + 16 + 3) * 2.0 ** -23 * (1.0 + want)
+    assert float(want.min()) < 0.1 < 1.0 < float(want.max())
+    assert bool(((loss.double() - want).abs() <= bound).all())
+    assert abs(float(mean) - float(want.mean())) <= float(bound.max())
