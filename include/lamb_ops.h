@@ -2,8 +2,9 @@
  * lamb_ops.h -- C ABI of the operators around the optimizer step, for AMD
  * Instinct MI355X (gfx950): Newton-Schulz orthogonalization and the Muon step
  * for a model's matrices, softmax cross entropy against a vocabulary table with
- * its gradients, and a token table's lookup with its gradient. Same library,
- * status codes and conventions as lamb_mi355x.h: pointers are device pointers
+ * its gradients, a token table's lookup with its gradient, the root-mean-square
+ * norm of rows with the residual's addition, its gradients and its result in 8 bits, and
+ * the norm of all gradients with clipping by it. Same library, status codes and conventions as lamb_mi355x.h: pointers are device pointers
  * unless marked host; the caller owns every tensor; arguments are validated on
  * the host before any HIP call; work is enqueued on `stream` and nothing is
  * synchronised, allocated or copied to the host (plan creation and destruction
@@ -264,6 +265,122 @@ LAMB_API lamb_status lamb_embed_backward(const lamb_embed *embed, const void *gr
                                          void *grad_table, int64_t grad_table_stride,
                                          int32_t grad_table_dtype, int64_t padding_id, int32_t add,
                                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Root-mean-square norm of rows, after the residual's addition where there is one:
+ *   h = x + residual, rounded to the residual's type (without a residual, h = x),
+ *   y_j = h_j w_j / sqrt(mean_i h_i^2 + eps).
+ * x, residual [tokens][dim] and weight [dim] are float32 or bfloat16 each (the residual of a
+ * float32 x is float32), rows `*_stride` elements apart (>= dim), aligned to their elements.
+ * residual NULL: none; weight NULL: ones. Rows' sums are taken in fp64, so that squares do
+ * not pass the range of fp32; y is rounded once to its type from fp32. A row that holds a NaN
+ * or an infinity gives NaN where the formula does; no row reaches another. With eps 0 a row
+ * of zeros gives NaN. tokens 0 to 2^24, dim 1 to 2^16, strides at most 2^36, eps >= 0.
+ */
+typedef struct lamb_rms {
+    const void *x;
+    const void *residual;
+    const void *weight;
+    int64_t x_stride, residual_stride;
+    int64_t tokens, dim;
+    int32_t x_dtype, residual_dtype, weight_dtype;
+    float eps;
+} lamb_rms;
+
+/*
+ * out: y, float32 or bfloat16 [tokens][dim]. summed: h, of the residual's type, or NULL;
+ * without a residual it must be NULL. Either result may take x's or the residual's place
+ * (the address, type and stride of one of them).
+ */
+LAMB_API lamb_status lamb_rms_forward(const lamb_rms *rms, void *summed, int64_t summed_stride,
+                                      void *out, int64_t out_stride, int32_t out_dtype,
+                                      void *stream);
+
+/*
+ * y in 8 bits: out are e4m3 numbers (4 exponent bits, bias 7, 3 mantissa bits, no
+ * infinities, up to 448), rows out_stride bytes apart, that stand for out times scale.
+ * group 0: one scale for a row; 32, 64, 128 or 256: one for as many columns, the last of a
+ * row for what is left. scales: float [tokens][groups], max(max |y| / 448, 2^-126) over its
+ * columns; out = y / scale, rounded to nearest even from fp32. NaN where y holds a NaN or an
+ * infinity: in the scale and the columns that share it, or, of an infinity, as y / scale has
+ * it.
+ */
+LAMB_API lamb_status lamb_rms_quantize(const lamb_rms *rms, void *summed, int64_t summed_stride,
+                                       void *out, int64_t out_stride, float *scales, int32_t group,
+                                       void *stream);
+
+/*
+ * Gradients, given that of y: with r = (mean(h^2) + eps)^-1/2 and g = grad_out w,
+ *   grad_x = r (g - h r mean(g h r)) + grad_sum,   grad_weight = sum of grad_out h r.
+ * rms.x is the normed h (summed, where there was a residual) and rms.residual NULL: the
+ * gradients of x and of the residual are both grad_x. grad_sum: what reaches h from elsewhere
+ * (the residual stream's own gradient), of grad_x's type, or NULL. grad_x: float32 or
+ * bfloat16, or NULL; it may take the place of x, grad_out or grad_sum. grad_weight: [dim],
+ * float32 or bfloat16, written, or added to (`add_weight` 1); NULL for none. Its sums are
+ * fp32 over 32 tokens, then over as many of those as a workgroup has, then fp64; the
+ * same inputs give the same bits.
+ * The workspace (256-byte aligned; lamb_rms_workspace, host only) is needed for grad_weight,
+ * and for grad_x where dim is over 8192; else NULL will do. It takes 4 bytes for each of the
+ * columns of at most 4096 rows (dim over 8192: of one row in 256, and 8 bytes for each row).
+ */
+typedef struct lamb_rms_grads {
+    const void *grad_out;
+    const void *grad_sum;
+    void *grad_x;
+    void *grad_weight;
+    int64_t grad_out_stride, grad_sum_stride, grad_x_stride;
+    int32_t grad_out_dtype, grad_x_dtype, grad_weight_dtype;
+    int32_t add_weight;
+    int64_t reserved; /* must be 0 */
+} lamb_rms_grads;
+
+LAMB_API lamb_status lamb_rms_workspace(const lamb_rms *rms, size_t *bytes);
+
+LAMB_API lamb_status lamb_rms_backward(const lamb_rms *rms, const lamb_rms_grads *grads,
+                                       void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * One gradient tensor of a list whose norm is taken: numel adjacent elements, float32 or
+ * bfloat16, aligned to their element (numel 0 to 2^40). out: where lamb_grad_clip writes, of
+ * out_dtype; `in` itself (the same type) for in place, NULL in a plan that only takes norms.
+ * No out may share memory with another tensor's in or out.
+ */
+typedef struct lamb_grad_tensor {
+    const void *in;
+    void *out;
+    int64_t numel;
+    int32_t in_dtype, out_dtype;
+} lamb_grad_tensor;
+
+/* A list of gradients with its workspace, 8 bytes for every 2048 to 65536 elements and
+ * some for each tensor. Streams, captures and threads as for lamb_ns_plan. */
+typedef struct lamb_grad_plan lamb_grad_plan;
+
+/* `tensors` (host) has n >= 1 entries; norm is a lamb_norm. */
+LAMB_API lamb_status lamb_grad_plan_create(const lamb_grad_tensor *tensors, int32_t n,
+                                           int32_t norm, lamb_grad_plan **out);
+
+/*
+ * The norm of each tensor (norms: device double[n], or NULL) and of all of them together
+ * (total: device double), from sums in fp64 in a fixed order. A NaN makes its tensor's norm
+ * and the total NaN, an infinity, without a NaN, infinite.
+ */
+LAMB_API lamb_status lamb_grad_norm(lamb_grad_plan *plan, double *norms, double *total,
+                                    void *stream);
+
+/*
+ * out = f in, f = scale min(1, max_norm / (|scale| total)): the scaled gradients have at most
+ * the norm max_norm. total: device double, from lamb_grad_norm or from a sum over workers.
+ * A total that is not finite limits nothing (f = scale), so that the NaN or the infinity
+ * stays to be seen; nonfinite_out (device int32, may be NULL) receives 1 then, else 0. In
+ * place nothing is written where f is 1. max_norm >= 0 (infinity: no limit), scale finite;
+ * f is rounded to fp32, the products once more to their type.
+ */
+LAMB_API lamb_status lamb_grad_clip(lamb_grad_plan *plan, const double *total, double max_norm,
+                                    double scale, int32_t *nonfinite_out, void *stream);
+
+/* NULL is fine. Waits for the device. */
+LAMB_API lamb_status lamb_grad_plan_destroy(lamb_grad_plan *plan);
 
 #ifdef __cplusplus
 }

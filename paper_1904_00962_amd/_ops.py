@@ -31,7 +31,9 @@ EXPORTS = ("lamb_ns_params_init", "lamb_ortho_plan_create", "lamb_orthogonalize"
            "lamb_muon_plan_create", "lamb_muon_hparams_init", "lamb_muon_step",
            "lamb_ns_plan_destroy", "lamb_xent_workspace", "lamb_xent_forward",
            "lamb_xent_backward", "lamb_embed_forward", "lamb_embed_workspace",
-           "lamb_embed_backward")
+           "lamb_embed_backward", "lamb_rms_forward", "lamb_rms_quantize", "lamb_rms_workspace",
+           "lamb_rms_backward", "lamb_grad_plan_create", "lamb_grad_norm", "lamb_grad_clip",
+           "lamb_grad_plan_destroy")
 
 
 class lamb_ns_params(ctypes.Structure):
@@ -80,6 +82,29 @@ class lamb_embed(ctypes.Structure):
                 ("dim", ctypes.c_int64), ("id_dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
 
 
+class lamb_rms(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("residual", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("x_stride", ctypes.c_int64),
+                ("residual_stride", ctypes.c_int64), ("tokens", ctypes.c_int64),
+                ("dim", ctypes.c_int64), ("x_dtype", ctypes.c_int32),
+                ("residual_dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+
+class lamb_rms_grads(ctypes.Structure):
+    _fields_ = [("grad_out", ctypes.c_void_p), ("grad_sum", ctypes.c_void_p),
+                ("grad_x", ctypes.c_void_p), ("grad_weight", ctypes.c_void_p),
+                ("grad_out_stride", ctypes.c_int64), ("grad_sum_stride", ctypes.c_int64),
+                ("grad_x_stride", ctypes.c_int64), ("grad_out_dtype", ctypes.c_int32),
+                ("grad_x_dtype", ctypes.c_int32), ("grad_weight_dtype", ctypes.c_int32),
+                ("add_weight", ctypes.c_int32), ("reserved", ctypes.c_int64)]
+
+
+class lamb_grad_tensor(ctypes.Structure):
+    _fields_ = [("input", ctypes.c_void_p), ("out", ctypes.c_void_p), ("numel", ctypes.c_int64),
+                ("in_dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32)]
+
+
 _lib_ops: Optional[ctypes.CDLL] = None
 
 
@@ -106,6 +131,15 @@ def load() -> ctypes.CDLL:
     lib.lamb_embed_workspace.argtypes = [P(lamb_embed), P(size)]
     lib.lamb_embed_backward.argtypes = [P(lamb_embed), vp, i64, i32, vp, i64, i32, i64, i32, vp,
                                         size, vp]
+    lib.lamb_rms_forward.argtypes = [P(lamb_rms), vp, i64, vp, i64, i32, vp]
+    lib.lamb_rms_quantize.argtypes = [P(lamb_rms), vp, i64, vp, i64, vp, i32, vp]
+    lib.lamb_rms_workspace.argtypes = [P(lamb_rms), P(size)]
+    lib.lamb_rms_backward.argtypes = [P(lamb_rms), P(lamb_rms_grads), vp, size, vp]
+    f64 = ctypes.c_double
+    lib.lamb_grad_plan_create.argtypes = [P(lamb_grad_tensor), i32, i32, P(vp)]
+    lib.lamb_grad_norm.argtypes = [vp, vp, vp, vp]
+    lib.lamb_grad_clip.argtypes = [vp, vp, f64, f64, vp, vp]
+    lib.lamb_grad_plan_destroy.argtypes = [vp]
     for name in EXPORTS:
         getattr(lib, name).restype = ctypes.c_int
     _lib_ops = lib
@@ -228,3 +262,60 @@ def lamb_embed_backward(embed: lamb_embed, grad_out: int, grad_out_stride: int,
                                       grad_out_dtype, grad_table, grad_table_stride,
                                       grad_table_dtype, padding_id, add, workspace,
                                       workspace_bytes, stream), "lamb_embed_backward")
+
+
+def lamb_rms_forward(rms: lamb_rms, summed: int, summed_stride: int, out: int, out_stride: int,
+                     out_dtype: int, stream: int = 0) -> None:
+    _check(load().lamb_rms_forward(ctypes.byref(rms), summed, summed_stride, out, out_stride,
+                                   out_dtype, stream), "lamb_rms_forward")
+
+
+def lamb_rms_quantize(rms: lamb_rms, summed: int, summed_stride: int, out: int, out_stride: int,
+                      scales: int, group: int, stream: int = 0) -> None:
+    _check(load().lamb_rms_quantize(ctypes.byref(rms), summed, summed_stride, out, out_stride,
+                                    scales, group, stream), "lamb_rms_quantize")
+
+
+def lamb_rms_workspace(rms: lamb_rms) -> int:
+    n = ctypes.c_size_t()
+    _check(load().lamb_rms_workspace(ctypes.byref(rms), ctypes.byref(n)), "lamb_rms_workspace")
+    return n.value
+
+
+def lamb_rms_backward(rms: lamb_rms, grads: lamb_rms_grads, workspace: int, workspace_bytes: int,
+                      stream: int = 0) -> None:
+    _check(load().lamb_rms_backward(ctypes.byref(rms), ctypes.byref(grads), workspace,
+                                    workspace_bytes, stream), "lamb_rms_backward")
+
+
+class GradPlan(_lib.Plan):
+    """Owning handle on a ``lamb_grad_plan``."""
+
+    def close(self) -> None:
+        if self.handle:
+            h, self.handle = self.handle, 0
+            _check(load().lamb_grad_plan_destroy(_vp(h)), "lamb_grad_plan_destroy")
+
+
+def lamb_grad_plan_create(tensors: Sequence[Tuple[int, int, int, int, int]],
+                          norm: int) -> GradPlan:
+    """tensors: (in_ptr, out_ptr, numel, in_dtype, out_dtype) each."""
+    n = len(tensors)
+    arr = (lamb_grad_tensor * max(n, 1))()
+    for i, (a, b, numel, in_dtype, out_dtype) in enumerate(tensors):
+        arr[i] = lamb_grad_tensor(int(a) or None, int(b) or None, int(numel), int(in_dtype),
+                                  int(out_dtype))
+    out = ctypes.c_void_p()
+    _check(load().lamb_grad_plan_create(arr, n, int(norm), ctypes.byref(out)),
+           "lamb_grad_plan_create")
+    return GradPlan(out.value)
+
+
+def lamb_grad_norm(plan: GradPlan, norms: int, total: int, stream: int = 0) -> None:
+    _check(load().lamb_grad_norm(plan.handle, norms, total, stream), "lamb_grad_norm")
+
+
+def lamb_grad_clip(plan: GradPlan, total: int, max_norm: float, scale: float = 1.0,
+                   nonfinite_out: int = 0, stream: int = 0) -> None:
+    _check(load().lamb_grad_clip(plan.handle, total, max_norm, scale, nonfinite_out, stream),
+           "lamb_grad_clip")

@@ -58,6 +58,52 @@ inline bool aligned_to(const void *p, uintptr_t bytes) {
 
 inline int64_t round_up(int64_t a, int64_t b) { return (a + b - 1) / b * b; }
 
+struct DeviceScope {
+    int previous = -1;
+    explicit DeviceScope(int device) {
+        if (hipGetDevice(&previous) == hipSuccess && previous != device)
+            (void)hipSetDevice(device);
+        else
+            previous = -1;
+    }
+    ~DeviceScope() {
+        if (previous >= 0)
+            (void)hipSetDevice(previous);
+    }
+};
+
+// The end of a plan's last call outside a capture, and its stream: see ordered().
+struct CallOrder {
+    hipEvent_t done = nullptr;
+    hipStream_t stream = nullptr;
+    bool used = false;
+};
+
+// Calls of one plan share its workspace: one on another stream than the last waits for
+// that one. A captured call is left out; when its graph runs is the caller's to order.
+template <class F>
+lamb_status ordered(CallOrder &order, hipStream_t stream, F enqueue) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    hipError_t err = hipStreamIsCapturing(stream, &capture);
+    if (err != hipSuccess)
+        return fail_hip(err, "hipStreamIsCapturing");
+    if (capture != hipStreamCaptureStatusNone)
+        return enqueue();
+    if (order.used && order.stream != stream) {
+        err = hipStreamWaitEvent(stream, order.done, 0);
+        if (err != hipSuccess)
+            return fail_hip(err, "hipStreamWaitEvent");
+    }
+    const lamb_status st = enqueue();
+    // also after a failure: what went out before it uses the workspace
+    err = hipEventRecord(order.done, stream);
+    order.stream = stream;
+    order.used = true;
+    if (st == LAMB_OK && err != hipSuccess)
+        return fail_hip(err, "hipEventRecord");
+    return st;
+}
+
 // Memory that a call reads or writes, for the overlap check: bytes lo to hi, or of these
 // `row` at every multiple of `stride` from lo on.
 struct Span {

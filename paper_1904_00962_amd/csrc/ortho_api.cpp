@@ -28,10 +28,7 @@ struct lamb_ns_plan {
     TileList both, only_q, only_t, next_gram;  // of those with: Q and T, Q, T, A
     double *partials = nullptr;
     uint32_t *flag = nullptr;  // see launch_ns_check
-    // The end of the last call outside a capture, and its stream: see ordered().
-    hipEvent_t done = nullptr;
-    hipStream_t stream = nullptr;
-    bool used = false;
+    CallOrder order;
 };
 
 namespace {
@@ -255,7 +252,8 @@ lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
     if (err != hipSuccess)
         return fail_hip(err, "hipGetDevice");
     // only orders kernels of this device: no system-scope fence
-    err = hipEventCreateWithFlags(&plan->done, hipEventDisableTiming | hipEventDisableSystemFence);
+    err = hipEventCreateWithFlags(&plan->order.done,
+                                  hipEventDisableTiming | hipEventDisableSystemFence);
     if (err != hipSuccess)
         return fail_hip(err, "hipEventCreateWithFlags");
     err = hipMalloc(&plan->block, bytes);
@@ -301,45 +299,6 @@ lamb_status build(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices) {
     if (err != hipSuccess)
         return fail_hip(err, "hipMemcpy");
     return LAMB_OK;
-}
-
-struct DeviceScope {
-    int previous = -1;
-    explicit DeviceScope(int device) {
-        if (hipGetDevice(&previous) == hipSuccess && previous != device)
-            (void)hipSetDevice(device);
-        else
-            previous = -1;
-    }
-    ~DeviceScope() {
-        if (previous >= 0)
-            (void)hipSetDevice(previous);
-    }
-};
-
-// Calls of one plan share its workspace: one on another stream than the last waits for
-// that one. A captured call is left out; when its graph runs is the caller's to order.
-template <class F>
-lamb_status ordered(lamb_ns_plan *plan, hipStream_t stream, F enqueue) {
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    hipError_t err = hipStreamIsCapturing(stream, &capture);
-    if (err != hipSuccess)
-        return fail_hip(err, "hipStreamIsCapturing");
-    if (capture != hipStreamCaptureStatusNone)
-        return enqueue();
-    if (plan->used && plan->stream != stream) {
-        err = hipStreamWaitEvent(stream, plan->done, 0);
-        if (err != hipSuccess)
-            return fail_hip(err, "hipStreamWaitEvent");
-    }
-    const lamb_status st = enqueue();
-    // also after a failure: what went out before it uses the workspace
-    err = hipEventRecord(plan->done, stream);
-    plan->stream = stream;
-    plan->used = true;
-    if (st == LAMB_OK && err != hipSuccess)
-        return fail_hip(err, "hipEventRecord");
-    return st;
 }
 
 lamb_status run(lamb_ns_plan *plan, const lamb_ns_params &ns, NsStep step, uint32_t *flag,
@@ -402,8 +361,8 @@ lamb_status finish(lamb_ns_plan *plan, std::vector<NsMatrix> &matrices, lamb_ns_
     if (st != LAMB_OK) {
         if (plan->block)
             (void)hipFree(plan->block);
-        if (plan->done)
-            (void)hipEventDestroy(plan->done);
+        if (plan->order.done)
+            (void)hipEventDestroy(plan->order.done);
         delete plan;
         return st;
     }
@@ -570,7 +529,8 @@ lamb_status lamb_orthogonalize(lamb_ns_plan *plan, const lamb_ns_params *params,
         return st;
     DeviceScope scope(plan->device);
     hipStream_t on = static_cast<hipStream_t>(stream);
-    return ordered(plan, on, [&] { return run(plan, *params, NsStep{}, nullptr, nullptr, on); });
+    return ordered(plan->order, on,
+                   [&] { return run(plan, *params, NsStep{}, nullptr, nullptr, on); });
 }
 
 lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void *stream_in,
@@ -606,7 +566,7 @@ lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void
     step.lr = hp->lr;
     step.nesterov = hp->nesterov;
     step.scale = hp->scale;
-    return ordered(plan, stream, [&] {
+    return ordered(plan->order, stream, [&] {
         uint32_t *flag = nullptr;
         if (hp->skip_nonfinite) {
             const hipError_t err =
@@ -625,7 +585,7 @@ lamb_status lamb_ns_plan_destroy(lamb_ns_plan *plan) {
         return LAMB_OK;
     DeviceScope scope(plan->device);
     hipError_t err = hipFree(plan->block);  // waits for what still uses it
-    const hipError_t event = hipEventDestroy(plan->done);
+    const hipError_t event = hipEventDestroy(plan->order.done);
     if (err == hipSuccess)
         err = event;
     delete plan;

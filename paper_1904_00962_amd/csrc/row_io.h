@@ -1,0 +1,134 @@
+// Eight elements of a row at a time, float32 or bfloat16, in the registers of one lane:
+// what the kernels that stream rows or lists of tensors share. Not installed.
+//
+// A lane's eight elements are loaded and stored in pieces of 16 bytes that are aligned to
+// an element only: the hardware takes them at any address, so rows of odd widths and
+// tensors that begin anywhere need no other path.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace lamb_mi355x {
+
+// A pointer that was read from memory, as one to device memory (its accesses need not look
+// which kind it is).
+template <class T>
+__device__ inline T *in_device_memory(T *p) {
+    return (T *)(__attribute__((address_space(1))) T *)p;
+}
+
+__device__ inline float bf16_low(uint32_t pair) { return __uint_as_float(pair << 16); }
+__device__ inline float bf16_high(uint32_t pair) { return __uint_as_float(pair & 0xffff0000u); }
+
+__device__ inline uint32_t bf16_pair(float low, float high) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const bf16x2 both = {__bf16(low), __bf16(high)};
+    return __builtin_bit_cast(uint32_t, both);
+}
+
+// Eight elements as they lie in memory.
+template <bool BF16>
+struct Eight {
+    uint32_t u[BF16 ? 4 : 8];
+
+    __device__ inline void get(float (&v)[8]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (BF16) {
+                v[2 * i] = bf16_low(u[i]);
+                v[2 * i + 1] = bf16_high(u[i]);
+            } else {
+                v[2 * i] = __uint_as_float(u[BF16 ? 0 : 2 * i]);
+                v[2 * i + 1] = __uint_as_float(u[BF16 ? 0 : 2 * i + 1]);
+            }
+        }
+    }
+    __device__ inline void set(const float (&v)[8]) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (BF16) {
+                u[i] = bf16_pair(v[2 * i], v[2 * i + 1]);
+            } else {
+                u[BF16 ? 0 : 2 * i] = __float_as_uint(v[2 * i]);
+                u[BF16 ? 0 : 2 * i + 1] = __float_as_uint(v[2 * i + 1]);
+            }
+        }
+    }
+};
+
+// Elements at .. at + n - 1 of `base` (n below 1: none); what is past them is 0.
+template <bool BF16>
+__device__ inline Eight<BF16> load_eight(const void *base, int64_t at, int n) {
+    Eight<BF16> e;
+    if (BF16) {
+        const uint16_t *p = (const uint16_t *)base + at;
+        if (n >= 8) {
+            __builtin_memcpy(&e, p, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                e.u[i] = (2 * i < n ? uint32_t(p[2 * i]) : 0u) |
+                         (2 * i + 1 < n ? uint32_t(p[2 * i + 1]) << 16 : 0u);
+        }
+    } else {
+        const uint32_t *p = (const uint32_t *)base + at;
+        if (n >= 8) {
+            __builtin_memcpy(&e, p, 32);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e.u[BF16 ? 0 : i] = i < n ? p[i] : 0u;
+        }
+    }
+    return e;
+}
+
+template <bool BF16>
+__device__ inline void store_eight(void *base, int64_t at, int n, const Eight<BF16> &e) {
+    if (BF16) {
+        uint16_t *p = (uint16_t *)base + at;
+        if (n >= 8) {
+            __builtin_memcpy(p, &e, 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n)
+                    p[i] = uint16_t(e.u[i / 2] >> (i % 2 * 16));
+        }
+    } else {
+        uint32_t *p = (uint32_t *)base + at;
+        if (n >= 8) {
+            __builtin_memcpy(p, &e, 32);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n)
+                    p[i] = e.u[BF16 ? 0 : i];
+        }
+    }
+}
+
+// The same with a type that is known at run time only, for what is not on a kernel's
+// longest path.
+__device__ inline void load_values(bool bf16, const void *base, int64_t at, int n,
+                                   float (&v)[8]) {
+    if (bf16)
+        load_eight<true>(base, at, n).get(v);
+    else
+        load_eight<false>(base, at, n).get(v);
+}
+
+__device__ inline void store_values(bool bf16, void *base, int64_t at, int n,
+                                    const float (&v)[8]) {
+    if (bf16) {
+        Eight<true> e;
+        e.set(v);
+        store_eight<true>(base, at, n, e);
+    } else {
+        Eight<false> e;
+        e.set(v);
+        store_eight<false>(base, at, n, e);
+    }
+}
+
+}  // namespace lamb_mi355x

@@ -5,6 +5,10 @@
   linear_cross_entropy_grad its gradients, without keeping the logits
   embedding                 rows of a token table, scaled
   embedding_grad            the table's gradient, summed in the tokens' order
+  rms_norm                  root-mean-square norm, after the residual's addition,
+  rms_norm_fp8              its result in 8 bits with scales, and
+  rms_norm_grad             its gradients
+  GradNorm                  the norm of all gradients of a model, and clipping by it
 
 PyTorch supplies device memory and the current stream only; the work is the HIP
 library's (``_ops``). Argument errors raise ``ValueError`` or ``TypeError`` here,
@@ -322,3 +326,211 @@ def embedding_grad(ids, grad_out, grad_table, *, scale: float = 1.0,
                                  grad_table.data_ptr(), stride, code,
                                  -1 if padding_id is None else padding_id, bool(accumulate),
                                  work.data_ptr(), need, _stream(device))
+
+
+def _rms(x, weight, residual, eps):
+    """(the C struct, x's device)"""
+    device = x.device
+    r = _ops.lamb_rms()
+    r.x_stride = _rows("x", x, x.dtype)
+    r.x_dtype = _float_code(x.dtype)
+    r.x = x.data_ptr() or None
+    r.tokens, r.dim = x.shape
+    r.eps = eps
+    if residual is not None:
+        r.residual_stride = _rows("residual", residual, residual.dtype, device)
+        r.residual_dtype = _float_code(residual.dtype)
+        if residual.shape != x.shape:
+            raise ValueError("residual must have x's shape")
+        r.residual = residual.data_ptr() or None
+    if weight is not None:
+        r.weight = _row("weight", weight, r.dim, device)
+        r.weight_dtype = _float_code(weight.dtype)
+    return r, device
+
+
+def _row(name, t, dim, device):
+    _on_gpu(name, t, device)
+    if t.dim() != 1 or t.shape[0] != dim:
+        raise ValueError("%s must be [%d]" % (name, dim))
+    if not t.is_contiguous():
+        raise ValueError("%s must be contiguous" % name)
+    return t.data_ptr()
+
+
+def _result(name, t, like, dtype):
+    """A result's tensor (``t``, or a new one like ``like``) and its row stride."""
+    if t is None:
+        return _torch().empty(like.shape, dtype=dtype, device=like.device), like.shape[1]
+    if t.shape != like.shape:
+        raise ValueError("%s must have x's shape" % name)
+    return t, _rows(name, t, dtype, like.device)
+
+
+def rms_norm(x, weight=None, *, residual=None, eps: float = 1e-6, out_dtype=None, out=None,
+             summed=None):
+    """``h weight / sqrt(mean(h^2) + eps)`` of every row h of ``x`` [tokens, dim], or of
+    ``x + residual``: then (the norm, the sum) is returned, the sum rounded to the
+    residual's type, and the norm is that of the rounded sum.
+
+    ``x``, ``residual`` and ``weight`` [dim] are float32 or bfloat16 each, rows contiguous;
+    the residual of a float32 x is float32. The norm has ``out_dtype`` (x's by default).
+    ``out`` and ``summed`` are written where given; each may be x or the residual itself.
+    Autograd does not see the call: tensors that require gradients are refused where grad
+    mode is on (pass them detached)."""
+    _torch()
+    _no_graph("rms_norm", *(t for t in (x, weight, residual, out, summed) if t is not None))
+    r, device = _rms(x, weight, residual, eps)
+    if out is not None:
+        out_dtype = out_dtype or out.dtype
+    out, out_stride = _result("out", out, x, out_dtype or x.dtype)
+    code = _float_code(out.dtype)
+    summed, to, stride = _summed(r, x, residual, summed)
+    with _on(device):
+        _ops.lamb_rms_forward(r, to, stride, out.data_ptr(), out_stride, code, _stream(device))
+    return out if residual is None else (out, summed)
+
+
+def _summed(r, x, residual, summed):
+    """The sum's tensor, its address and its row stride."""
+    if residual is None:
+        if summed is not None:
+            raise ValueError("summed needs a residual")
+        return None, None, 0
+    summed, stride = _result("summed", summed, x, residual.dtype)
+    return summed, summed.data_ptr(), stride
+
+
+def rms_norm_fp8(x, weight=None, *, residual=None, eps: float = 1e-6, group: int = 0, out=None,
+                 scales=None, summed=None):
+    """:func:`rms_norm` with its result in 8 bits: (out, scales), with a residual (out,
+    scales, sum). ``out`` (float8_e4m3fn, like x) times its scale is the norm; ``scales``
+    (float32 [tokens, groups]) has one for a row (``group`` 0), or one for every 32, 64, 128
+    or 256 columns, the last for what is left of a row: the largest magnitude / 448, at
+    least 2^-126."""
+    torch = _torch()
+    _no_graph("rms_norm_fp8", *(t for t in (x, weight, residual, summed) if t is not None))
+    r, device = _rms(x, weight, residual, eps)
+    out, out_stride = _result("out", out, x, torch.float8_e4m3fn)
+    groups = -(-r.dim // group) if group > 0 else 1
+    if scales is None:
+        scales = torch.empty(r.tokens, groups, dtype=torch.float32, device=device)
+    else:
+        _on_gpu("scales", scales, device)
+        if scales.dtype != torch.float32:
+            raise TypeError("scales must be float32")
+        if scales.shape != (r.tokens, groups) or not scales.is_contiguous():
+            raise ValueError("scales must be [%d, %d] and contiguous" % (r.tokens, groups))
+    summed, to, stride = _summed(r, x, residual, summed)
+    with _on(device):
+        _ops.lamb_rms_quantize(r, to, stride, out.data_ptr(), out_stride, scales.data_ptr(),
+                               group, _stream(device))
+    return (out, scales) if residual is None else (out, scales, summed)
+
+
+def rms_norm_grad(x, weight, grad_out, grad_x=None, grad_weight=None, *, eps: float = 1e-6,
+                  grad_sum=None, accumulate: bool = False) -> None:
+    """Gradients of :func:`rms_norm`, given that of its result: into ``grad_x`` [tokens, dim]
+    and ``grad_weight`` [dim], float32 or bfloat16 each and either optional; ``accumulate``
+    adds to what ``grad_weight`` holds.
+
+    ``x`` is what was normed: the sum, where there was a residual, and ``grad_x`` is the
+    gradient of both its terms. ``grad_sum`` (of grad_x's type) is added to it: the gradient
+    that the sum has from elsewhere, as the residual stream. ``grad_x`` may be ``x``,
+    ``grad_out`` or ``grad_sum`` itself."""
+    _torch()
+    r, device = _rms(x, weight, None, eps)
+    g = _ops.lamb_rms_grads(add_weight=int(bool(accumulate)))
+    g.grad_out_stride = _rows("grad_out", grad_out, grad_out.dtype, device)
+    g.grad_out_dtype = _float_code(grad_out.dtype)
+    g.grad_out = grad_out.data_ptr() or None
+    if grad_out.shape != x.shape:
+        raise ValueError("grad_out must have x's shape")
+    if grad_x is not None:
+        g.grad_x_dtype = _float_code(grad_x.dtype)
+        _, g.grad_x_stride = _result("grad_x", grad_x, x, grad_x.dtype)
+        g.grad_x = grad_x.data_ptr() or None
+    if grad_sum is not None:
+        if grad_x is None:
+            raise ValueError("grad_sum needs grad_x")
+        _, g.grad_sum_stride = _result("grad_sum", grad_sum, x, grad_x.dtype)
+        g.grad_sum = grad_sum.data_ptr() or None
+    if grad_weight is not None:
+        g.grad_weight = _row("grad_weight", grad_weight, r.dim, device)
+        g.grad_weight_dtype = _float_code(grad_weight.dtype)
+    need = _ops.lamb_rms_workspace(r)
+    work = _workspace(need, device)
+    with _on(device):
+        _ops.lamb_rms_backward(r, g, work.data_ptr() or None, need, _stream(device))
+
+
+class GradNorm:
+    """The norm of a list of gradients, tensor by tensor and over all of them, and the
+    gradients scaled so that it keeps a limit.
+
+    ``grads`` are persistent contiguous tensors, float32 or bfloat16 each, of any size;
+    ``run()`` and ``clip()`` read them as they are then. ``outputs``: where ``clip()``
+    writes, one tensor of as many elements for each, float32 or bfloat16 (default: the
+    gradients themselves). ``norm``: "l2", "l1" or "linf".
+
+    ``norms`` (float64, one per tensor), ``total`` (float64) and ``found_nonfinite`` (int32:
+    1 where the last ``clip()`` met a total that is no finite number) are on the device and
+    written by every call. Streams and captures as for :class:`Orthogonalizer`.
+    """
+
+    def __init__(self, grads: Sequence, outputs: Optional[Sequence] = None, norm: str = "l2"):
+        torch = _torch()
+        self.grads = list(grads)
+        if not self.grads:
+            raise ValueError("need at least one gradient")
+        self.outputs = self.grads if outputs is None else list(outputs)
+        if len(self.outputs) != len(self.grads):
+            raise ValueError("need one output per gradient (got %d and %d)"
+                             % (len(self.outputs), len(self.grads)))
+        if norm not in _lib.NORMS:
+            raise ValueError("norm must be one of %s" % (tuple(_lib.NORMS),))
+        self.norm = norm
+        self.device = self.grads[0].device
+        rows = []
+        for i, (a, b) in enumerate(zip(self.grads, self.outputs)):
+            for name, t in (("gradient", a), ("output", b)):
+                _on_gpu("%s %d" % (name, i), t, self.device)
+                if not t.is_contiguous():
+                    raise ValueError("%s %d is not contiguous" % (name, i))
+            if a.numel() != b.numel():
+                raise ValueError("gradient %d has %d elements, its output %d"
+                                 % (i, a.numel(), b.numel()))
+            rows.append((a.data_ptr(), b.data_ptr(), a.numel(), _float_code(a.dtype),
+                         _float_code(b.dtype)))
+        self.norms = torch.zeros(len(rows), dtype=torch.float64, device=self.device)
+        self.total = torch.zeros((), dtype=torch.float64, device=self.device)
+        self.found_nonfinite = torch.zeros(1, dtype=torch.int32, device=self.device)
+        with _on(self.device):
+            self.plan = _ops.lamb_grad_plan_create(rows, _lib.NORMS[norm])
+
+    def run(self):
+        """Enqueue the norms on the current stream; returns ``total``."""
+        _ops.lamb_grad_norm(self.plan, self.norms.data_ptr(), self.total.data_ptr(),
+                            _stream(self.device))
+        return self.total
+
+    def clip(self, max_norm: float, *, scale: float = 1.0, total=None):
+        """Write ``scale`` x the gradients, and less where their norm would pass
+        ``max_norm``, into the outputs; returns the gradients' norm before that (without
+        ``scale``). ``total``: that norm, where it is known already or is that of more
+        gradients than these (one float64 element on the device); else it is computed.
+        Gradients in place that need no change are only read. Where the norm is no finite
+        number nothing is limited and ``found_nonfinite`` is set: the step that follows can
+        see what the gradients hold (``skip_nonfinite``)."""
+        if total is None:
+            total = self.run()
+        else:
+            _on_gpu("total", total, self.device)
+            if total.dtype != _torch().float64 or total.numel() != 1:
+                raise TypeError("total must be one float64 element")
+        _ops.lamb_grad_clip(self.plan, total.data_ptr(), max_norm, scale,
+                            self.found_nonfinite.data_ptr(), _stream(self.device))
+        return total
+
+    def close(self) -> None:
+        self.plan.close()

@@ -27,7 +27,7 @@ from __future__ import annotations
 
 from typing import Optional, Sequence, Tuple
 
-from . import _lib, _ops
+from . import _lib, _ops, ops
 
 
 def _torch():
@@ -75,6 +75,28 @@ def _check_state(state, buffers) -> None:
                                  % (name, i, t.numel(), d.numel()))
 
 
+class _Clipper:
+    """The gradients of one optimizer kept to a norm before its step, in place."""
+
+    def __init__(self, grads, max_norm: Optional[float]):
+        self.norm = None
+        if max_norm is None:
+            return
+        if not max_norm > 0.0:
+            raise ValueError("max_grad_norm must be positive")
+        self.max_norm = float(max_norm)
+        self.norm = ops.GradNorm(grads)
+
+    def run(self, grad_scale: float) -> None:
+        if self.norm is not None:
+            # the step multiplies the gradients by grad_scale, so their own limit is this
+            self.norm.clip(self.max_norm / abs(grad_scale) if grad_scale else float("inf"))
+
+    def close(self) -> None:
+        if self.norm is not None:
+            self.norm.close()
+
+
 class _LayerwiseOptimizer:
     algo = _lib.LAMB_ALGO_LAMB
 
@@ -82,7 +104,7 @@ class _LayerwiseOptimizer:
                  clamp: Tuple[float, float], wd_mask: Optional[Sequence[bool]],
                  chunk_elems: int, with_v: bool, norm: str = "l2", grad_scale: float = 1.0,
                  skip_nonfinite: bool = False, schedule=None, path: str = "auto",
-                 check_every: int = 100):
+                 check_every: int = 100, max_grad_norm: Optional[float] = None):
         torch = _torch()
         if path not in _lib.PATHS:
             raise ValueError("path must be one of %s" % (tuple(_lib.PATHS),))
@@ -121,6 +143,7 @@ class _LayerwiseOptimizer:
         self.plan = None
         self.path = path
         self._build_plan()
+        self.clipper = _Clipper(self.grads, max_grad_norm)
         self._t = 0
         self._launched = 0
         # The last step's skip verdict, copied to pinned host memory behind an
@@ -190,6 +213,7 @@ class _LayerwiseOptimizer:
         hp.norm = _lib.NORMS[self.norm]
         hp.skip_nonfinite = int(self.skip_nonfinite)
         stream = self._stream()
+        self.clipper.run(hp.grad_scale)
         _lib.lamb_step_ex(self.plan, hp, stream, self.ratios.data_ptr(), self.norms.data_ptr(),
                           self.found_nonfinite.data_ptr() if self.skip_nonfinite else 0)
         if self.skip_nonfinite:
@@ -234,8 +258,15 @@ class _LayerwiseOptimizer:
         state from a checkpoint and call ``rebuild()``."""
         _lib.lamb_plan_check(self.plan, self._stream())
 
+    @property
+    def grad_norm(self):
+        """With ``max_grad_norm``: the L2 norm of all gradients that the last step met,
+        before it clipped them and without ``grad_scale`` (device, float64)."""
+        return self.clipper.norm.total if self.clipper.norm is not None else None
+
     def close(self) -> None:
         self.plan.close()
+        self.clipper.close()
 
 
 class LAMB(_LayerwiseOptimizer):
@@ -249,7 +280,8 @@ class LAMB(_LayerwiseOptimizer):
                  weight_decay: float = 0.01, clamp=(0.0, 10.0), wd_mask=None,
                  bias_correction: bool = True, chunk_elems: int = 0, variant: str = "lamb",
                  norm: str = "l2", grad_scale: float = 1.0, skip_nonfinite: bool = False,
-                 schedule=None, path: str = "auto", check_every: int = 100):
+                 schedule=None, path: str = "auto", check_every: int = 100,
+                 max_grad_norm: Optional[float] = None):
         """``variant``: "lamb" (Algorithm 2), "n-lamb" (Algorithm 3) or "nn-lamb"
         (Algorithm 4; the paper pairs both with betas=(0.975, 0.999), eps=1e-8).
         ``norm``: "l2" (default), "l1" or "linf" (Appendix F). ``grad_scale``
@@ -261,13 +293,18 @@ class LAMB(_LayerwiseOptimizer):
         ``path``: "auto" (layers of up to 8.4M elements, or 10.5M where the
         plan takes the wider tile, take the single-pass kernel) or
         "two-pass". ``check_every``: read the plan's fault word every that many
-        steps (0: only in ``check()`` and ``state_dict()``)."""
+        steps (0: only in ``check()`` and ``state_dict()``). ``max_grad_norm``: a
+        step first scales ``grads``, in place, so that the L2 norm of all of them,
+        times ``grad_scale``, is at most that (``ops.GradNorm``); a norm that is no
+        finite number scales nothing. Gradients of several optimizers that share
+        one limit are clipped by one ``ops.GradNorm`` before their steps instead."""
         if variant not in self.VARIANTS:
             raise ValueError("variant must be one of %s" % (self.VARIANTS,))
         if variant != "lamb" and not bias_correction:
             raise ValueError("N-LAMB and NN-LAMB carry their own bias correction")
         super().__init__(params, grads, lr, weight_decay, clamp, wd_mask, chunk_elems, True,
-                         norm, grad_scale, skip_nonfinite, schedule, path, check_every)
+                         norm, grad_scale, skip_nonfinite, schedule, path, check_every,
+                         max_grad_norm)
         self.beta1, self.beta2 = float(betas[0]), float(betas[1])
         self.eps = float(eps)
         self.bias_correction = bool(bias_correction)
@@ -307,9 +344,10 @@ class LARS(_LayerwiseOptimizer):
                  weight_decay: float = 0.01, clamp=(0.0, 10.0), trust_coef: float = 1e-3,
                  wd_mask=None, chunk_elems: int = 0, norm: str = "l2", grad_scale: float = 1.0,
                  skip_nonfinite: bool = False, schedule=None, path: str = "auto",
-                 check_every: int = 100):
+                 check_every: int = 100, max_grad_norm: Optional[float] = None):
         super().__init__(params, grads, lr, weight_decay, clamp, wd_mask, chunk_elems, False,
-                         norm, grad_scale, skip_nonfinite, schedule, path, check_every)
+                         norm, grad_scale, skip_nonfinite, schedule, path, check_every,
+                         max_grad_norm)
         self.momentum = float(momentum)
         self.trust_coef = float(trust_coef)
 
@@ -349,10 +387,10 @@ class Muon:
     which matrices decay (default: all). ``precision``: "split" keeps the products at
     fp32's accuracy; "half" is up to three times faster and moves the direction, as
     ``ops.Orthogonalizer`` says, by 1e-3 to 1e-1: least for independent entries, most where
-    a few singular values outweigh the rest. ``grad_scale``, ``skip_nonfinite`` and
-    ``schedule`` as for ``LAMB``; a skipped step sets ``found_nonfinite``. A step on another
-    stream than the last waits for that one; replays of a captured step are the caller's to
-    order.
+    a few singular values outweigh the rest. ``grad_scale``, ``skip_nonfinite``,
+    ``max_grad_norm`` and ``schedule`` as for ``LAMB``; a skipped step sets
+    ``found_nonfinite``. A step on another stream than the last waits for that one; replays
+    of a captured step are the caller's to order.
     """
 
     def __init__(self, params: Sequence, grads: Sequence, lr: float = 1e-3,
@@ -361,7 +399,8 @@ class Muon:
                  coefficients: Tuple[float, float, float] = (3.4445, -4.7750, 2.0315),
                  eps: float = 1e-7, precision: str = "split", m: Optional[Sequence] = None,
                  wd_mask: Optional[Sequence[bool]] = None, grad_scale: float = 1.0,
-                 skip_nonfinite: bool = False, schedule=None):
+                 skip_nonfinite: bool = False, schedule=None,
+                 max_grad_norm: Optional[float] = None):
         torch = _torch()
         self.params = list(params)
         self.grads = list(grads)
@@ -402,6 +441,7 @@ class Muon:
             self.plan = _ops.lamb_muon_plan_create(
                 rows, _ops.LAMB_DTYPE_BF16 if g_dtype == torch.bfloat16 else _ops.LAMB_DTYPE_F32,
                 _ops.PRECISIONS[precision])
+        self.clipper = _Clipper(self.grads, max_grad_norm)
         self.t = 0
 
     def step(self, lr: Optional[float] = None) -> None:
@@ -412,6 +452,7 @@ class Muon:
             lr = _lib.lamb_lr_at(self.schedule, self.t) if self.schedule else self.lr
         self.hparams.lr = lr
         stream = _torch().cuda.current_stream(self.device).cuda_stream
+        self.clipper.run(self.hparams.grad_scale)
         _ops.lamb_muon_step(self.plan, self.hparams, stream,
                             self.found_nonfinite.data_ptr() if self.hparams.skip_nonfinite else 0)
 
@@ -424,5 +465,8 @@ class Muon:
         for dst, src in zip(self.m, state["m"]):
             dst.copy_(src.reshape(dst.shape))
 
+    grad_norm = _LayerwiseOptimizer.grad_norm
+
     def close(self) -> None:
         self.plan.close()
+        self.clipper.close()
