@@ -352,7 +352,7 @@ typedef struct lamb_grad_tensor {
     int32_t in_dtype, out_dtype;
 } lamb_grad_tensor;
 
-/* A list of gradients with its workspace, 8 bytes for every 2048 to 65536 elements and
+/* A list of gradients with its workspace, 12 bytes for every 8192 to 16384 elements and
  * some for each tensor. Streams, captures and threads as for lamb_ns_plan. */
 typedef struct lamb_grad_plan lamb_grad_plan;
 
@@ -369,7 +369,7 @@ LAMB_API lamb_status lamb_grad_norm(lamb_grad_plan *plan, double *norms, double 
                                     void *stream);
 
 /*
- * out = f in, f = scale min(1, max_norm / (|scale| total)): the scaled gradients have at most
+ * Clipping by the norm: out = f in, f = scale min(1, max_norm / (|scale| total)): the scaled gradients have at most
  * the norm max_norm. total: device double, from lamb_grad_norm or from a sum over workers.
  * A total that is not finite limits nothing (f = scale), so that the NaN or the infinity
  * stays to be seen; nonfinite_out (device int32, may be NULL) receives 1 then, else 0. In
@@ -378,6 +378,11 @@ LAMB_API lamb_status lamb_grad_norm(lamb_grad_plan *plan, double *norms, double 
  */
 LAMB_API lamb_status lamb_grad_clip(lamb_grad_plan *plan, const double *total, double max_norm,
                                     double scale, int32_t *nonfinite_out, void *stream);
+
+/* lamb_grad_norm, then lamb_grad_clip by its total. */
+LAMB_API lamb_status lamb_grad_norm_clip(lamb_grad_plan *plan, double *norms, double *total,
+                                         double max_norm, double scale, int32_t *nonfinite_out,
+                                         void *stream);
 
 /* NULL is fine. Waits for the device. */
 LAMB_API lamb_status lamb_grad_plan_destroy(lamb_grad_plan *plan);

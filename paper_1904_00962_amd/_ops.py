@@ -33,7 +33,7 @@ EXPORTS = ("lamb_ns_params_init", "lamb_ortho_plan_create", "lamb_orthogonalize"
            "lamb_xent_backward", "lamb_embed_forward", "lamb_embed_workspace",
            "lamb_embed_backward", "lamb_rms_forward", "lamb_rms_quantize", "lamb_rms_workspace",
            "lamb_rms_backward", "lamb_grad_plan_create", "lamb_grad_norm", "lamb_grad_clip",
-           "lamb_grad_plan_destroy")
+           "lamb_grad_norm_clip", "lamb_grad_plan_destroy")
 
 
 class lamb_ns_params(ctypes.Structure):
@@ -139,6 +139,7 @@ def load() -> ctypes.CDLL:
     lib.lamb_grad_plan_create.argtypes = [P(lamb_grad_tensor), i32, i32, P(vp)]
     lib.lamb_grad_norm.argtypes = [vp, vp, vp, vp]
     lib.lamb_grad_clip.argtypes = [vp, vp, f64, f64, vp, vp]
+    lib.lamb_grad_norm_clip.argtypes = [vp, vp, vp, f64, f64, vp, vp]
     lib.lamb_grad_plan_destroy.argtypes = [vp]
     for name in EXPORTS:
         getattr(lib, name).restype = ctypes.c_int
@@ -319,3 +320,9 @@ def lamb_grad_clip(plan: GradPlan, total: int, max_norm: float, scale: float = 1
                    nonfinite_out: int = 0, stream: int = 0) -> None:
     _check(load().lamb_grad_clip(plan.handle, total, max_norm, scale, nonfinite_out, stream),
            "lamb_grad_clip")
+
+
+def lamb_grad_norm_clip(plan: GradPlan, norms: int, total: int, max_norm: float,
+                        scale: float = 1.0, nonfinite_out: int = 0, stream: int = 0) -> None:
+    _check(load().lamb_grad_norm_clip(plan.handle, norms, total, max_norm, scale, nonfinite_out,
+                                      stream), "lamb_grad_norm_clip")

@@ -19,18 +19,23 @@ struct lamb_grad_plan {
 
 namespace {
 
-// Chunks are as long as they can be with work for every CU: a workgroup's fixed time
-// counts in small lists, the number of parts to join in large ones.
+// Chunks are as long as a workgroup loads at once, half of that where there would be too few
+// for all CUs. (4 steps in place of 1: 11 us for the norm of 2M to 4M elements in place of
+// 13 to 14, whose time is the joins'. 8 steps in place of 16 or 32, which are further from
+// filling a last round: 979 us for 1.56 billion fp32 elements in place of 994 and 1007.)
 int32_t pick_chunk(int64_t numel) {
-    constexpr int64_t kWorkgroups = 2048, kMost = 32 * kGradStep;
+    constexpr int64_t kWorkgroups = 2048, kLeast = 4 * kGradStep, kMost = 8 * kGradStep;
     const int64_t each = round_up((numel + kWorkgroups - 1) / kWorkgroups, kGradStep);
-    return int32_t(std::min(std::max<int64_t>(each, kGradStep), kMost));
+    return int32_t(std::min(std::max(each, kLeast), kMost));
 }
 
 lamb_status build(lamb_grad_plan *plan, std::vector<GradTensor> &tensors) {
     GradList &l = plan->list;
     int64_t numel = 0, chunks = 0;
-    for (const GradTensor &t : tensors) numel += t.numel;
+    for (const GradTensor &t : tensors) {
+        numel += t.numel;
+        l.bytes += t.numel * (t.in_bf16 ? 2 : 4);
+    }
     l.chunk = pick_chunk(numel);
     for (GradTensor &t : tensors) {
         const int64_t own = (t.numel + l.chunk - 1) / l.chunk;
@@ -38,6 +43,7 @@ lamb_status build(lamb_grad_plan *plan, std::vector<GradTensor> &tensors) {
             return fail(LAMB_EINVAL, "the tensors take too many chunks for one plan");
         t.first_chunk = int32_t(chunks);
         t.chunks = int32_t(own);
+        l.filled += own > 0;
         chunks += own;
     }
     l.n = int32_t(tensors.size());
@@ -55,8 +61,9 @@ lamb_status build(lamb_grad_plan *plan, std::vector<GradTensor> &tensors) {
     };
     const size_t o_tensors = take(tensors.size() * sizeof(GradTensor));
     const size_t o_chunks = take(chunk_tensor.size() * 4);
-    const size_t o_partials = take(size_t(chunks) * 8);
+    const size_t o_partials = take(chunk_tensor.size() * 8);
     const size_t o_powers = take(tensors.size() * 8);
+    const size_t o_done = take((tensors.size() + 1) * 4);
     hipError_t err = hipGetDevice(&plan->device);
     if (err != hipSuccess)
         return fail_hip(err, "hipGetDevice");
@@ -78,12 +85,41 @@ lamb_status build(lamb_grad_plan *plan, std::vector<GradTensor> &tensors) {
     };
     up(o_tensors, tensors.data(), tensors.size() * sizeof(GradTensor));
     up(o_chunks, chunk_tensor.data(), chunk_tensor.size() * 4);
+    const std::vector<double> zeros(tensors.size(), 0.0);
+    up(o_powers, zeros.data(), zeros.size() * 8);
+    const std::vector<uint32_t> none(tensors.size() + 1, 0);
+    up(o_done, none.data(), none.size() * 4);
     if (err != hipSuccess)
         return fail_hip(err, "hipMemcpy");
     l.tensors = reinterpret_cast<const GradTensor *>(base + o_tensors);
     l.chunk_tensor = reinterpret_cast<const int32_t *>(base + o_chunks);
     l.partials = reinterpret_cast<double *>(base + o_partials);
     l.powers = reinterpret_cast<double *>(base + o_powers);
+    l.done = reinterpret_cast<uint32_t *>(base + o_done);
+    return LAMB_OK;
+}
+
+lamb_status check_totals(const lamb_grad_plan *plan, const double *norms, const double *total) {
+    if (!plan || !total)
+        return fail(LAMB_ENULL, "plan and total must not be NULL");
+    if (!aligned_to(norms, 8) || !aligned_to(total, 8))
+        return fail(LAMB_EALIGN, "norms and total must be 8-byte aligned");
+    return LAMB_OK;
+}
+
+lamb_status check_clip(const lamb_grad_plan *plan, const double *total, double max_norm,
+                       double scale, const int32_t *nonfinite_out) {
+    const lamb_status st = check_totals(plan, nullptr, total);
+    if (st != LAMB_OK)
+        return st;
+    if (!plan->clips)
+        return fail(LAMB_EPLAN, "the plan has tensors without an out");
+    if (!aligned_to(nonfinite_out, 4))
+        return fail(LAMB_EALIGN, "nonfinite_out is not aligned to its element");
+    if (!(max_norm >= 0.0))
+        return fail(LAMB_EINVAL, "max_norm = %g, need >= 0", max_norm);
+    if (!std::isfinite(scale))
+        return fail(LAMB_EINVAL, "scale = %g must be finite", scale);
     return LAMB_OK;
 }
 
@@ -125,13 +161,8 @@ lamb_status lamb_grad_plan_create(const lamb_grad_tensor *tensors, int32_t n, in
             if (t.out)
                 spans.push_back(span_of(t.out, uint64_t(t.numel * size_of(t.out_dtype)), true, i,
                                         "out"));
-            GradTensor g{};
-            g.in = t.in;
-            g.out = t.out;
-            g.numel = t.numel;
-            g.in_bf16 = t.in_dtype == LAMB_DTYPE_BF16;
-            g.out_bf16 = t.out_dtype == LAMB_DTYPE_BF16;
-            list.push_back(g);
+            list.push_back(GradTensor{t.in, t.out, t.numel, t.in_dtype == LAMB_DTYPE_BF16,
+                                      t.out_dtype == LAMB_DTYPE_BF16, 0, 0});
         }
         lamb_status s = check_spans(spans.data(), spans.size());
         if (s != LAMB_OK)
@@ -150,39 +181,45 @@ lamb_status lamb_grad_plan_create(const lamb_grad_tensor *tensors, int32_t n, in
 }
 
 lamb_status lamb_grad_norm(lamb_grad_plan *plan, double *norms, double *total, void *stream_in) {
-    if (!plan || !total)
-        return fail(LAMB_ENULL, "plan and total must not be NULL");
-    if (!aligned_to(norms, 8) || !aligned_to(total, 8))
-        return fail(LAMB_EALIGN, "norms and total must be 8-byte aligned");
+    const lamb_status st = check_totals(plan, norms, total);
+    if (st != LAMB_OK)
+        return st;
     hipStream_t stream = static_cast<hipStream_t>(stream_in);
     DeviceScope scope(plan->device);
     return ordered(plan->order, stream, [&] {
-        hipError_t err = hipSuccess;
-        if (plan->list.chunks)
-            err = launch_grad_norms(plan->list, stream);
-        if (err == hipSuccess)
-            err = launch_grad_totals(plan->list, norms, total, stream);
+        const hipError_t err = launch_grad_norms(plan->list, false, norms, total, stream);
         return err == hipSuccess ? LAMB_OK : fail_hip(err, "kernel launch");
     });
 }
 
 lamb_status lamb_grad_clip(lamb_grad_plan *plan, const double *total, double max_norm,
                            double scale, int32_t *nonfinite_out, void *stream_in) {
-    if (!plan || !total)
-        return fail(LAMB_ENULL, "plan and total must not be NULL");
-    if (!plan->clips)
-        return fail(LAMB_EPLAN, "the plan has tensors without an out");
-    if (!aligned_to(total, 8) || !aligned_to(nonfinite_out, 4))
-        return fail(LAMB_EALIGN, "total or nonfinite_out is not aligned to its element");
-    if (!(max_norm >= 0.0))
-        return fail(LAMB_EINVAL, "max_norm = %g, need >= 0", max_norm);
-    if (!std::isfinite(scale))
-        return fail(LAMB_EINVAL, "scale = %g must be finite", scale);
+    const lamb_status st = check_clip(plan, total, max_norm, scale, nonfinite_out);
+    if (st != LAMB_OK)
+        return st;
     hipStream_t stream = static_cast<hipStream_t>(stream_in);
     DeviceScope scope(plan->device);
     return ordered(plan->order, stream, [&] {
         const hipError_t err =
             launch_grad_clip(plan->list, total, max_norm, scale, nonfinite_out, stream);
+        return err == hipSuccess ? LAMB_OK : fail_hip(err, "kernel launch");
+    });
+}
+
+lamb_status lamb_grad_norm_clip(lamb_grad_plan *plan, double *norms, double *total,
+                                double max_norm, double scale, int32_t *nonfinite_out,
+                                void *stream_in) {
+    lamb_status st = check_totals(plan, norms, total);
+    if (st == LAMB_OK)
+        st = check_clip(plan, total, max_norm, scale, nonfinite_out);
+    if (st != LAMB_OK)
+        return st;
+    hipStream_t stream = static_cast<hipStream_t>(stream_in);
+    DeviceScope scope(plan->device);
+    return ordered(plan->order, stream, [&] {
+        hipError_t err = launch_grad_norms(plan->list, true, norms, total, stream);
+        if (err == hipSuccess)
+            err = launch_grad_clip(plan->list, total, max_norm, scale, nonfinite_out, stream);
         return err == hipSuccess ? LAMB_OK : fail_hip(err, "kernel launch");
     });
 }

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(rms_block(W)) void rms_kernel(RmsArgs a, RmsOut o) 
                 r[v].set(with);
                 r[v].get(h[v]);
                 if (o.summed)
-                    store_eight<RES_BF16>(o.summed, row * o.summed_stride + c, a.dim - c, r[v]);
+                    store_eight<RES_BF16, true>(o.summed, row * o.summed_stride + c, a.dim - c, r[v]);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum = fma(double(h[v][i]), double(h[v][i]), sum);
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(rms_block(W)) void rms_kernel(RmsArgs a, RmsOut o) 
                 for (int i = 0; i < 8; ++i) h[v][i] *= w[i];
             }
             if (!QUANT) {
-                store_values(o.out_bf16, o.out, row * o.out_stride + c, n, h[v]);
+                store_values<true>(o.out_bf16, o.out, row * o.out_stride + c, n, h[v]);
             } else if (o.group == 0) {
                 // columns past the row are 0 inverse, which may be NaN
 #pragma unroll
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(rms_block(W)) void rms_grad_kernel(RmsArgs a, RmsGr
             if (g.grad_x) {
                 Eight<DX_BF16> e;
                 e.set(dx);
-                store_eight<DX_BF16>(g.grad_x, row * g.grad_x_stride + c, n, e);
+                store_eight<DX_BF16, true>(g.grad_x, row * g.grad_x_stride + c, n, e);
             }
         }
         if (++rows % kRmsFoldRows == 0) {

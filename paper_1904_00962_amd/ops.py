@@ -83,7 +83,11 @@ def _on_gpu(name, t, device=None):
 def _no_graph(name, *tensors):
     """The operators record nothing for autograd: a result whose gradient would be lost
     without a word is refused."""
-    if _torch().is_grad_enabled() and any(t.requires_grad for t in tensors):
+    if not _torch().is_grad_enabled():
+        return
+    for t in tensors:
+        if t is None or not t.requires_grad:
+            continue
         raise ValueError("%s records no gradient for a tensor that requires one: pass "
                          "tensor.detach(), or call it under torch.no_grad(), and take the "
                          "gradient from %s_grad" % (name, name))
@@ -161,7 +165,8 @@ class Orthogonalizer:
 
 def _rows(name, t, dtype, device=None):
     """A 2-D tensor whose rows are contiguous: its row stride."""
-    _on_gpu(name, t, device)
+    if not t.is_cuda or (device is not None and t.device != device):
+        _on_gpu(name, t, device)
     if t.dtype is not dtype:
         raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
     if t.dim() != 2:
@@ -329,29 +334,28 @@ def embedding_grad(ids, grad_out, grad_table, *, scale: float = 1.0,
 
 
 def _rms(x, weight, residual, eps):
-    """(the C struct, x's device)"""
+    """The C struct."""
     device = x.device
-    r = _ops.lamb_rms()
-    r.x_stride = _rows("x", x, x.dtype)
-    r.x_dtype = _float_code(x.dtype)
-    r.x = x.data_ptr() or None
-    r.tokens, r.dim = x.shape
-    r.eps = eps
+    stride = _rows("x", x, x.dtype)
+    tokens, dim = x.shape
+    at = w_at = 0
+    r_stride = code = w_code = 0
     if residual is not None:
-        r.residual_stride = _rows("residual", residual, residual.dtype, device)
-        r.residual_dtype = _float_code(residual.dtype)
+        r_stride = _rows("residual", residual, residual.dtype, device)
+        code = _float_code(residual.dtype)
         if residual.shape != x.shape:
             raise ValueError("residual must have x's shape")
-        r.residual = residual.data_ptr() or None
+        at = residual.data_ptr()
     if weight is not None:
-        r.weight = _row("weight", weight, r.dim, device)
-        r.weight_dtype = _float_code(weight.dtype)
-    return r, device
+        w_at, w_code = _row("weight", weight, dim, device), _float_code(weight.dtype)
+    return _ops.lamb_rms(x.data_ptr() or None, at or None, w_at or None, stride, r_stride, tokens,
+                         dim, _float_code(x.dtype), code, w_code, eps)
 
 
 def _row(name, t, dim, device):
-    _on_gpu(name, t, device)
-    if t.dim() != 1 or t.shape[0] != dim:
+    if not t.is_cuda or t.device != device:
+        _on_gpu(name, t, device)
+    if t.shape != (dim,):
         raise ValueError("%s must be [%d]" % (name, dim))
     if not t.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
@@ -361,7 +365,9 @@ def _row(name, t, dim, device):
 def _result(name, t, like, dtype):
     """A result's tensor (``t``, or a new one like ``like``) and its row stride."""
     if t is None:
-        return _torch().empty(like.shape, dtype=dtype, device=like.device), like.shape[1]
+        torch = _torch_module
+        return (torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format),
+                like.shape[1])
     if t.shape != like.shape:
         raise ValueError("%s must have x's shape" % name)
     return t, _rows(name, t, dtype, like.device)
@@ -379,8 +385,8 @@ def rms_norm(x, weight=None, *, residual=None, eps: float = 1e-6, out_dtype=None
     Autograd does not see the call: tensors that require gradients are refused where grad
     mode is on (pass them detached)."""
     _torch()
-    _no_graph("rms_norm", *(t for t in (x, weight, residual, out, summed) if t is not None))
-    r, device = _rms(x, weight, residual, eps)
+    _no_graph("rms_norm", x, weight, residual, out, summed)
+    r, device = _rms(x, weight, residual, eps), x.device
     if out is not None:
         out_dtype = out_dtype or out.dtype
     out, out_stride = _result("out", out, x, out_dtype or x.dtype)
@@ -409,8 +415,8 @@ def rms_norm_fp8(x, weight=None, *, residual=None, eps: float = 1e-6, group: int
     or 256 columns, the last for what is left of a row: the largest magnitude / 448, at
     least 2^-126."""
     torch = _torch()
-    _no_graph("rms_norm_fp8", *(t for t in (x, weight, residual, summed) if t is not None))
-    r, device = _rms(x, weight, residual, eps)
+    _no_graph("rms_norm_fp8", x, weight, residual, summed)
+    r, device = _rms(x, weight, residual, eps), x.device
     out, out_stride = _result("out", out, x, torch.float8_e4m3fn)
     groups = -(-r.dim // group) if group > 0 else 1
     if scales is None:
@@ -439,7 +445,7 @@ def rms_norm_grad(x, weight, grad_out, grad_x=None, grad_weight=None, *, eps: fl
     that the sum has from elsewhere, as the residual stream. ``grad_x`` may be ``x``,
     ``grad_out`` or ``grad_sum`` itself."""
     _torch()
-    r, device = _rms(x, weight, None, eps)
+    r, device = _rms(x, weight, None, eps), x.device
     g = _ops.lamb_rms_grads(add_weight=int(bool(accumulate)))
     g.grad_out_stride = _rows("grad_out", grad_out, grad_out.dtype, device)
     g.grad_out_dtype = _float_code(grad_out.dtype)
@@ -523,11 +529,13 @@ class GradNorm:
         number nothing is limited and ``found_nonfinite`` is set: the step that follows can
         see what the gradients hold (``skip_nonfinite``)."""
         if total is None:
-            total = self.run()
-        else:
-            _on_gpu("total", total, self.device)
-            if total.dtype != _torch().float64 or total.numel() != 1:
-                raise TypeError("total must be one float64 element")
+            _ops.lamb_grad_norm_clip(self.plan, self.norms.data_ptr(), self.total.data_ptr(),
+                                     max_norm, scale, self.found_nonfinite.data_ptr(),
+                                     _stream(self.device))
+            return self.total
+        _on_gpu("total", total, self.device)
+        if total.dtype != _torch().float64 or total.numel() != 1:
+            raise TypeError("total must be one float64 element")
         _ops.lamb_grad_clip(self.plan, total.data_ptr(), max_norm, scale,
                             self.found_nonfinite.data_ptr(), _stream(self.device))
         return total
