@@ -59,7 +59,7 @@ __device__ inline void add_elements(Power<NORM> &power, const void *in, int64_t 
         Eight<BF16> e[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            e[k] = load_eight<BF16, STREAM>(in, at + k * kGradStep, 8);
+            e[k] = load_eight<BF16, false, STREAM>(in, at + k * kGradStep, 8);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             float v[8];
@@ -70,7 +70,7 @@ __device__ inline void add_elements(Power<NORM> &power, const void *in, int64_t 
     }
     for (; at < end; at += kGradStep) {
         float v[8];
-        load_eight<BF16>(in, at, int(end - at < 8 ? end - at : 8)).get(v);
+        load_eight<BF16, true>(in, at, int(end - at < 8 ? end - at : 8)).get(v);
 #pragma unroll
         for (int i = 0; i < 8; ++i) power.element(v[i]);  // 0 past the end
     }
@@ -227,14 +227,14 @@ __device__ inline void scale_chunk(const Chunk &c, float f) {
         Eight<IN_BF16> e[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            e[k] = load_eight<IN_BF16>(c.t.in, at + k * kGradStep, 8);
+            e[k] = load_eight<IN_BF16, false>(c.t.in, at + k * kGradStep, 8);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k)
-            store_eight<OUT_BF16, true>(c.t.out, at + k * kGradStep, 8, scaled(e[k]));
+            store_eight<OUT_BF16, false, true>(c.t.out, at + k * kGradStep, 8, scaled(e[k]));
     }
     for (; at < c.end; at += kGradStep) {
         const int n = int(c.end - at < 8 ? c.end - at : 8);
-        store_eight<OUT_BF16>(c.t.out, at, n, scaled(load_eight<IN_BF16>(c.t.in, at, n)));
+        store_eight<OUT_BF16, true>(c.t.out, at, n, scaled(load_eight<IN_BF16, true>(c.t.in, at, n)));
     }
 }
 

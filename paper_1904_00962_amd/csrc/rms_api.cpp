@@ -61,7 +61,8 @@ RmsArgs args_of(const lamb_rms &r) {
                    r.x_dtype == LAMB_DTYPE_BF16,
                    r.residual_dtype == LAMB_DTYPE_BF16,
                    r.weight_dtype == LAMB_DTYPE_BF16,
-                   r.eps};
+                   r.eps,
+                   1.0 / double(r.dim)};
 }
 
 // What a call touches, up to eight pieces of it.
@@ -129,15 +130,15 @@ lamb_status forward(const lamb_rms *rms, void *summed, int64_t summed_stride, vo
 }
 
 struct Layout {
-    int64_t columns, partials;
+    int64_t columns;
     size_t stats, bytes;
 };
 
 Layout layout_of(const lamb_rms &r) {
     Layout l{};
     l.columns = round_up(r.dim, 8);
-    l.partials = rms_partials(r.tokens, int32_t(r.dim));
-    l.stats = size_t(round_up(l.partials * l.columns * 4, 256));
+    const int64_t partials = rms_most_partials(r.tokens, int32_t(r.dim));
+    l.stats = size_t(round_up(partials * l.columns * 4, 256));
     l.bytes = l.stats + (r.dim > kRmsHeldDim ? size_t(round_up(r.tokens * 8, 256)) : 0);
     return l;
 }
@@ -244,7 +245,7 @@ lamb_status lamb_rms_backward(const lamb_rms *rms, const lamb_rms_grads *grads, 
     hipStream_t stream = static_cast<hipStream_t>(stream_in);
     const RmsArgs args = args_of(r);
     char *work = static_cast<char *>(workspace);
-    const RmsGrad grad{g.grad_out,
+    RmsGrad grad{g.grad_out,
                        g.grad_sum,
                        g.grad_x,
                        g.grad_weight,
@@ -256,9 +257,10 @@ lamb_status lamb_rms_backward(const lamb_rms *rms, const lamb_rms_grads *grads, 
                        g.grad_weight_dtype == LAMB_DTYPE_BF16,
                        g.add_weight,
                        reinterpret_cast<float *>(work),
-                       l.partials,
+                       0,
                        int32_t(l.columns),
                        reinterpret_cast<float *>(work + l.stats)};
+    grad.partials = rms_partials(args, grad);
     hipError_t err = hipSuccess;
     if (r.tokens)
         err = launch_rms_grad(args, grad, stream);

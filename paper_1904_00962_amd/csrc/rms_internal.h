@@ -7,10 +7,7 @@
 
 namespace lamb_mi355x {
 
-// A row is a team's: `waves` waves, 512 columns each time. A workgroup of at least
-// kRmsWaves waves has one or more teams.
-constexpr int kRmsWaves = 4;
-constexpr int kRmsMaxWaves = 16;
+constexpr int kRmsBlock = 256;  // threads of a workgroup, at least
 
 struct RmsArgs {
     const void *x, *residual, *weight;  // residual, weight: may be NULL
@@ -19,6 +16,7 @@ struct RmsArgs {
     int32_t dim;
     int32_t x_bf16, residual_bf16, weight_bf16;
     float eps;
+    double per_column;  // 1 / dim
 };
 
 struct RmsOut {
@@ -33,7 +31,7 @@ hipError_t launch_rms(const RmsArgs &args, const RmsOut &out, hipStream_t stream
 
 // Rows wider than this take two passes backward: a lane would have to hold more columns'
 // sums than it has registers for.
-constexpr int32_t kRmsHeldDim = 512 * kRmsMaxWaves;
+constexpr int32_t kRmsHeldDim = 8192;
 constexpr int32_t kRmsFoldRows = 32;  // rows whose terms of the weight's gradient are one sum
 constexpr int32_t kRmsWideRows = 256;  // rows of a workgroup in the second pass of wide rows
 
@@ -48,8 +46,9 @@ struct RmsGrad {
     int32_t columns;    // dim, rounded up to 8
     float *stats;       // [tokens][2], for wide rows: 1 / rms, and the mean of g x / rms
 };
-// Rows of RmsGrad::partial for these sizes.
-int64_t rms_partials(int64_t tokens, int32_t dim);
+// Rows of RmsGrad::partial in a call, and in any of these sizes.
+int64_t rms_partials(const RmsArgs &args, const RmsGrad &grad);
+int64_t rms_most_partials(int64_t tokens, int32_t dim);
 hipError_t launch_rms_grad(const RmsArgs &args, const RmsGrad &grad, hipStream_t stream);
 hipError_t launch_rms_join(const RmsArgs &args, const RmsGrad &grad, hipStream_t stream);
 

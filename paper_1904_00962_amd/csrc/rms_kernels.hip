@@ -25,177 +25,293 @@ namespace {
 constexpr float kLargestE4m3 = 448.0f;
 constexpr float kLeastScale = 0x1p-126f;
 
-template <class T>
-__device__ inline T wave_sum(T v) {
-#pragma unroll
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+// Lanes 0 to 15 of every 16 with each other, by data-parallel moves: 1 away, 2 away, then
+// eights and sixteens from their other ends. Where all lanes of a step's group hold one
+// value, its mirror image is the other half's.
+constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
+
+template <int MOVE>
+__device__ inline uint32_t moved(uint32_t v) {
+    return uint32_t(__builtin_amdgcn_update_dpp(0, int(v), MOVE, 0xF, 0xF, true));
+}
+
+template <int MOVE>
+__device__ inline double moved(double v) {
+    const uint64_t bits = uint64_t(__double_as_longlong(v));
+    const uint32_t low = moved<MOVE>(uint32_t(bits)), high = moved<MOVE>(uint32_t(bits >> 32));
+    return __longlong_as_double(int64_t(uint64_t(high) << 32 | low));
+}
+
+__device__ inline double lane_of(double v, int lane) {
+    const uint64_t bits = uint64_t(__double_as_longlong(v));
+    const uint32_t low = __builtin_amdgcn_readlane(uint32_t(bits), lane);
+    const uint32_t high = __builtin_amdgcn_readlane(uint32_t(bits >> 32), lane);
+    return __longlong_as_double(int64_t(uint64_t(high) << 32 | low));
+}
+
+// The sum over the lanes of a team (at most a wave's), on each of them. All lanes of the
+// wave must be here.
+template <int LANES>
+__device__ inline double lanes_sum(double v) {
+    v += moved<kSwap1>(v);
+    v += moved<kSwap2>(v);
+    v += moved<kMirror8>(v);
+    v += moved<kMirror16>(v);
+    if (LANES == 32)
+        v += __shfl_xor(v, 16);
+    if (LANES < 64)
+        return v;
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
+
+// The largest of `lanes` lanes (4 to 32, a power of two) that lie together, on each of them.
+__device__ inline uint32_t group_max(uint32_t v, int lanes) {
+    v = max(v, moved<kSwap1>(v));
+    v = max(v, moved<kSwap2>(v));
+    if (lanes > 4)
+        v = max(v, moved<kMirror8>(v));
+    if (lanes > 8)
+        v = max(v, moved<kMirror16>(v));
+    if (lanes > 16)
+        v = max(v, uint32_t(__shfl_xor(int(v), 16)));
     return v;
+}
+
+template <int LANES>
+__device__ inline uint32_t lanes_max(uint32_t v) {
+    if (LANES < 64)
+        return group_max(v, LANES);
+    v = group_max(v, 16);
+    const uint32_t a = max(__builtin_amdgcn_readlane(v, 0), __builtin_amdgcn_readlane(v, 16));
+    const uint32_t b = max(__builtin_amdgcn_readlane(v, 32), __builtin_amdgcn_readlane(v, 48));
+    return max(a, b);
+}
+
+// 1 / sqrt(v) to 2^-45 or so: the hardware's estimate (2^-22) and a Newton step, which
+// makes NaN of 0 and infinity, where the estimate is right.
+__device__ inline double inverse_root(double v) {
+    const double y = __builtin_amdgcn_rsq(v);
+    const double better = y * fma(-0.5 * v * y, y, 1.5);
+    return isnan(better) ? y : better;
 }
 
 // The bits of |v| as integers have the order of their values, and NaN above all.
 __device__ inline uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
-constexpr int rms_block(int waves) { return 64 * (waves < kRmsWaves ? kRmsWaves : waves); }
+// max(largest / 448, 2^-126) of the bits of a magnitude, and its inverse, both as if
+// divided: an estimate and what it leaves. Not so for infinity and NaN.
+__device__ inline void scale_of(uint32_t largest, float *scale, float *up) {
+    const float most = __uint_as_float(largest);
+    if (largest >= 0x7f800000u) {
+        *scale = most;
+        *up = 1.0f / most;
+        return;
+    }
+    constexpr float kPart = 1.0f / kLargestE4m3;
+    const float s = most * kPart;
+    *scale = fmaxf(fmaf(fmaf(-kLargestE4m3, s, most), kPart, s), kLeastScale);
+    const float u = __builtin_amdgcn_rcpf(*scale);
+    *up = fmaf(fmaf(-*scale, u, 1.0f), u, u);
+}
 
-// W waves to a row, V times 512 W columns. With QUANT the result is 8 bits wide.
-template <int W, int V, bool X_BF16, bool RES, bool RES_BF16, bool QUANT>
-__global__ __launch_bounds__(rms_block(W)) void rms_kernel(RmsArgs a, RmsOut o) {
-    constexpr int kTeams = rms_block(W) / 64 / W;
-    __shared__ double part[kTeams][W];
-    __shared__ uint32_t top[kTeams][W];
-    const int t = threadIdx.x % (64 * W), team = threadIdx.x / (64 * W), wave = t / 64;
+// L lanes to a row (16, 32 or whole waves), V times 8 L columns; a workgroup of one or more
+// rows. With QUANT the result is 8 bits wide.
+constexpr int rms_block(int lanes) { return lanes < kRmsBlock ? kRmsBlock : lanes; }
+
+template <int L, int V, bool TAIL, bool X_BF16, bool RES, bool RES_BF16, bool QUANT>
+__global__ __launch_bounds__(rms_block(L)) void rms_kernel(RmsArgs a, RmsOut o) {
+    constexpr int kTeams = rms_block(L) / L, kWaves = L < 64 ? 1 : L / 64;
+    constexpr int kInWave = L < 64 ? L : 64;
+    // registers allow all loads of a row at once, and the weight's with them
+    constexpr bool kTogether = V <= 4, kEarly = V <= 2;
+    __shared__ double part[kTeams][kWaves];
+    __shared__ uint32_t top[kTeams][kWaves];
+    const int t = threadIdx.x % L, team = threadIdx.x / L, wave = t / 64;
     const int64_t row = (int64_t(blockIdx.y) * gridDim.x + blockIdx.x) * kTeams + team;
     const bool live = row < a.tokens;
-    float h[V][8];
-    double sum = 0.0;
-    if (live) {
-        Eight<X_BF16> x[V];
-        Eight<RES_BF16> r[V];
+    int c[V], n[V];  // a lane's columns, and how many there are from there on
+    Eight<X_BF16> x[V];
+    Eight<RES_BF16> r[V];
+    float h[V][8], w[V][8];
+    auto load = [&](int v) {
+        x[v] = load_eight<X_BF16, TAIL>(a.x, row * a.x_stride + c[v], n[v], c[v] > 0);
+        if (RES)
+            r[v] = load_eight<RES_BF16, TAIL>(a.residual, row * a.residual_stride + c[v], n[v],
+                                              c[v] > 0);
+    };
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = (v * 64 * W + t) * 8;
-            x[v] = load_eight<X_BF16>(a.x, row * a.x_stride + c, a.dim - c);
-            if (RES)
-                r[v] = load_eight<RES_BF16>(a.residual, row * a.residual_stride + c, a.dim - c);
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = (v * 64 * W + t) * 8;
-            x[v].get(h[v]);
-            if (RES) {
-                float with[8];
-                r[v].get(with);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) with[i] += h[v][i];
-                r[v].set(with);
-                r[v].get(h[v]);
-                if (o.summed)
-                    store_eight<RES_BF16, true>(o.summed, row * o.summed_stride + c, a.dim - c, r[v]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sum = fma(double(h[v][i]), double(h[v][i]), sum);
-        }
-        sum = wave_sum(sum);
+    for (int v = 0; v < V; ++v) {
+        c[v] = (v * L + t) * 8;
+        n[v] = live ? a.dim - c[v] : 0;
+        if (kTogether)
+            load(v);
     }
-    if (W > 1) {
+    if (kEarly && a.weight) {
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            load_values<TAIL>(a.weight_bf16, a.weight, c[v], a.dim - c[v], c[v] > 0, w[v]);
+    }
+    double sum = 0.0;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        if (!kTogether)
+            load(v);
+        settle<TAIL>(x[v], n[v], c[v] > 0);
+        x[v].get(h[v]);
+        if (RES) {
+            float with[8];
+            settle<TAIL>(r[v], n[v], c[v] > 0);
+            r[v].get(with);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) with[i] += h[v][i];
+            r[v].set(with);
+            r[v].get(h[v]);
+            if (o.summed)
+                store_eight<RES_BF16, TAIL, true>(o.summed, row * o.summed_stride + c[v], n[v],
+                                                  r[v]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum = fma(double(h[v][i]), double(h[v][i]), sum);
+    }
+    sum = lanes_sum<kInWave>(sum);
+    if (kWaves > 1) {
         if (t % 64 == 0)
             part[team][wave] = sum;
         __syncthreads();
         sum = 0.0;
 #pragma unroll
-        for (int w = 0; w < W; ++w) sum += part[team][w];
+        for (int k = 0; k < kWaves; ++k) sum += part[team][k];
     }
-    const float inverse = float(1.0 / sqrt(sum / a.dim + double(a.eps)));
+    const float inverse = float(inverse_root(fma(sum, a.per_column, double(a.eps))));
     uint32_t largest = 0;
-    if (live) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = (v * 64 * W + t) * 8;
-            const int n = a.dim - c;
+    for (int v = 0; v < V; ++v) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) h[v][i] *= inverse;
-            if (a.weight) {
-                float w[8];
-                load_values(a.weight_bf16, a.weight, c, n, w);
+        for (int i = 0; i < 8; ++i) h[v][i] *= inverse;
+        if (a.weight) {
+            if (!kEarly)
+                load_values<TAIL>(a.weight_bf16, a.weight, c[v], n[v], c[v] > 0, w[v]);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) h[v][i] *= w[i];
-            }
-            if (!QUANT) {
-                store_values<true>(o.out_bf16, o.out, row * o.out_stride + c, n, h[v]);
-            } else if (o.group == 0) {
-                // columns past the row are 0 inverse, which may be NaN
+            for (int i = 0; i < 8; ++i) h[v][i] *= w[v][i];
+        }
+        if (!QUANT) {
+            store_values<TAIL, true>(o.out_bf16, o.out, row * o.out_stride + c[v], n[v], h[v]);
+        } else if (o.group == 0) {
+            // columns past the row are 0 inverse, which may be NaN
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
-                    if (i < n)
-                        largest = max(largest, magnitude(h[v][i]));
-            }
+            for (int i = 0; i < 8; ++i)
+                if (!TAIL ? n[v] > 0 : i < n[v])
+                    largest = max(largest, magnitude(h[v][i]));
         }
     }
     if (!QUANT)
         return;
     if (o.group == 0) {
-#pragma unroll
-        for (int d = 32; d; d >>= 1) largest = max(largest, uint32_t(__shfl_xor(int(largest), d)));
-        if (W > 1) {
+        largest = lanes_max<kInWave>(largest);
+        if (kWaves > 1) {
             if (t % 64 == 0)
                 top[team][wave] = largest;
             __syncthreads();
 #pragma unroll
-            for (int w = 0; w < W; ++w) largest = max(largest, top[team][w]);
+            for (int k = 0; k < kWaves; ++k) largest = max(largest, top[team][k]);
         }
     }
-    if (!live)
-        return;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int c = (v * 64 * W + t) * 8;
-        const int n = a.dim - c;
         if (o.group) {
             largest = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (i < n)
+                if (!TAIL ? n[v] > 0 : i < n[v])
                     largest = max(largest, magnitude(h[v][i]));
-            for (int d = 1; d < o.group / 8; d <<= 1)
-                largest = max(largest, uint32_t(__shfl_xor(int(largest), d)));
+            largest = group_max(largest, min(o.group / 8, kInWave));
         }
-        const float most = __uint_as_float(largest) / kLargestE4m3;
-        const float scale = most < kLeastScale ? kLeastScale : most;  // NaN stays
-        if (n <= 0)
+        float scale, up;
+        scale_of(largest, &scale, &up);
+        if (n[v] <= 0)
             continue;
-        if (o.group ? c % o.group == 0 : c == 0)
-            o.scales[row * o.groups + (o.group ? c / o.group : 0)] = scale;
+        if (o.group ? c[v] % o.group == 0 : c[v] == 0)
+            o.scales[row * o.groups + (o.group ? c[v] / o.group : 0)] = scale;
         uint32_t q[2] = {};
 #pragma unroll
         for (int i = 0; i < 8; i += 4) {
             int word = 0;
-            word = __builtin_amdgcn_cvt_pk_fp8_f32(h[v][i] / scale, h[v][i + 1] / scale, word,
-                                                   false);
-            word = __builtin_amdgcn_cvt_pk_fp8_f32(h[v][i + 2] / scale, h[v][i + 3] / scale, word,
-                                                   true);
+            word = __builtin_amdgcn_cvt_pk_fp8_f32(h[v][i] * up, h[v][i + 1] * up, word, false);
+            word = __builtin_amdgcn_cvt_pk_fp8_f32(h[v][i + 2] * up, h[v][i + 3] * up, word, true);
             q[i / 4] = uint32_t(word);
         }
-        uint8_t *p = (uint8_t *)o.out + row * o.out_stride + c;
-        if (n >= 8) {
+        uint8_t *p = (uint8_t *)o.out + row * o.out_stride + c[v];
+        if (n[v] >= 8) {
             __builtin_memcpy(p, q, 8);
-        } else {
+        } else if (TAIL) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (i < n)
+                if (i < n[v])
                     p[i] = uint8_t(q[i / 4] >> (i % 4 * 8));
         }
     }
 }
 
+// Writes, or adds to, a column of the weight's gradient.
+__device__ inline void finish_weight(const RmsGrad &g, int c, double sum) {
+    if (g.grad_weight_bf16) {
+        __bf16 *to = (__bf16 *)g.grad_weight + c;
+        if (g.add_weight)
+            sum += double(float(*to));
+        *to = __bf16(float(sum));
+    } else {
+        float *to = (float *)g.grad_weight + c;
+        if (g.add_weight)
+            sum += double(*to);
+        *to = float(sum);
+    }
+}
+
 // A team's columns of row after row; what a lane adds to the weight's gradient stays in
-// its registers, kRmsFoldRows rows to a sum and these sums to another, and leaves once.
-template <int W, bool X_BF16, bool DY_BF16, bool DX_BF16>
-__global__ __launch_bounds__(rms_block(W)) void rms_grad_kernel(RmsArgs a, RmsGrad g) {
-    constexpr int kTeams = rms_block(W) / 64 / W;
-    __shared__ double part[2][kTeams][W][2];
-    const int t = threadIdx.x % (64 * W), team = threadIdx.x / (64 * W), wave = t / 64;
-    const int c = t * 8, n = a.dim - c;
-    const int64_t step = int64_t(gridDim.x) * kTeams;
+// its registers, kRmsFoldRows rows to a sum and these sums to another. The teams' are
+// joined at the end, and leave as one row of parts, or finished where there is one
+// workgroup.
+template <int L, bool TAIL, bool X_BF16, bool DY_BF16, bool DX_BF16>
+__global__ __launch_bounds__(L < 1024 ? 512 : 1024) void rms_grad_kernel(RmsArgs a, RmsGrad g) {
+    constexpr int kWaves = L < 64 ? 1 : L / 64, kInWave = L < 64 ? L : 64;
+    extern __shared__ float joined[];  // [teams][8 L], where there are teams
+    __shared__ double part[2][16][2];
+    const int teams = blockDim.x / L;
+    const int t = threadIdx.x % L, team = threadIdx.x / L;
+    const int c = t * 8, columns = a.dim - c;
+    const int64_t step = int64_t(gridDim.x) * teams;
     float w[8], recent[8] = {}, dw[8] = {};
+    struct Row {
+        Eight<X_BF16> x;
+        Eight<DY_BF16> dy;
+        Eight<DX_BF16> ds;
+    };
+    auto load = [&](int64_t row, int n) {
+        Row e;
+        e.x = load_eight<X_BF16, TAIL>(a.x, row * a.x_stride + c, n, c > 0);
+        e.dy = load_eight<DY_BF16, TAIL>(g.grad_out, row * g.grad_out_stride + c, n, c > 0);
+        if (g.grad_sum)
+            e.ds = load_eight<DX_BF16, TAIL>(g.grad_sum, row * g.grad_sum_stride + c, n, c > 0);
+        else
+            e.ds = Eight<DX_BF16>{};
+        return e;
+    };
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = 1.0f;
     if (a.weight)
-        load_values(a.weight_bf16, a.weight, c, n, w);
-    int rows = 0;
+        load_values<TAIL>(a.weight_bf16, a.weight, c, columns, c > 0, w);
     // every team of a workgroup makes as many turns
-    for (int64_t first = int64_t(blockIdx.x) * kTeams; first < a.tokens; first += step) {
+    int turn = 0;
+    for (int64_t first = int64_t(blockIdx.x) * teams; first < a.tokens; first += step) {
         const int64_t row = first + team;
-        const bool live = row < a.tokens;
-        float x[8] = {}, dy[8] = {}, ds[8] = {}, gw[8];
-        if (live) {
-            const Eight<X_BF16> xe = load_eight<X_BF16>(a.x, row * a.x_stride + c, n);
-            const Eight<DY_BF16> de =
-                load_eight<DY_BF16>(g.grad_out, row * g.grad_out_stride + c, n);
-            if (g.grad_sum)
-                load_eight<DX_BF16>(g.grad_sum, row * g.grad_sum_stride + c, n).get(ds);
-            xe.get(x);
-            de.get(dy);
-        }
+        const int n = row < a.tokens ? columns : 0;
+        Row now = load(row, n);
+        float x[8], dy[8], gw[8];
+        settle<TAIL>(now.x, n, c > 0);
+        settle<TAIL>(now.dy, n, c > 0);
+        settle<TAIL>(now.ds, n, c > 0);
+        now.x.get(x);
+        now.dy.get(dy);
         double square = 0.0, along = 0.0;
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -203,26 +319,27 @@ __global__ __launch_bounds__(rms_block(W)) void rms_grad_kernel(RmsArgs a, RmsGr
             square = fma(double(x[i]), double(x[i]), square);
             along = fma(double(x[i]), double(gw[i]), along);
         }
-        square = wave_sum(square);
-        along = wave_sum(along);
-        if (W > 1) {
-            double(*to)[2] = part[rows & 1][team];
+        square = lanes_sum<kInWave>(square);
+        along = lanes_sum<kInWave>(along);
+        if (kWaves > 1) {
+            double(*to)[2] = part[turn & 1] + threadIdx.x / L * kWaves;
             if (t % 64 == 0) {
-                to[wave][0] = square;
-                to[wave][1] = along;
+                to[t / 64][0] = square;
+                to[t / 64][1] = along;
             }
             __syncthreads();
             square = along = 0.0;
 #pragma unroll
-            for (int k = 0; k < W; ++k) {
+            for (int k = 0; k < kWaves; ++k) {
                 square += to[k][0];
                 along += to[k][1];
             }
         }
-        const double r = 1.0 / sqrt(square / a.dim + double(a.eps));
-        const float inverse = float(r), mean = float(along * r / a.dim);
-        if (live) {
-            float dx[8];
+        const double r = inverse_root(fma(square, a.per_column, double(a.eps)));
+        const float inverse = float(r), mean = float(along * r * a.per_column);
+        float ds[8], dx[8];
+        now.ds.get(ds);
+        if (n > 0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 x[i] *= inverse;
@@ -232,10 +349,10 @@ __global__ __launch_bounds__(rms_block(W)) void rms_grad_kernel(RmsArgs a, RmsGr
             if (g.grad_x) {
                 Eight<DX_BF16> e;
                 e.set(dx);
-                store_eight<DX_BF16, true>(g.grad_x, row * g.grad_x_stride + c, n, e);
+                store_eight<DX_BF16, TAIL, true>(g.grad_x, row * g.grad_x_stride + c, n, e);
             }
         }
-        if (++rows % kRmsFoldRows == 0) {
+        if (++turn % kRmsFoldRows == 0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 dw[i] += recent[i];
@@ -243,12 +360,30 @@ __global__ __launch_bounds__(rms_block(W)) void rms_grad_kernel(RmsArgs a, RmsGr
             }
         }
     }
-    if (g.grad_weight && n > 0) {
-        Eight<false> e;
+    if (!g.grad_weight)
+        return;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dw[i] += recent[i];
+    for (int i = 0; i < 8; ++i) dw[i] += recent[i];
+    if (teams > 1) {
+        // element i of lane t lies at i L + t: no two lanes of a wave in one bank
+#pragma unroll
+        for (int i = 0; i < 8; ++i) joined[(team * 8 + i) * L + t] = dw[i];
+        __syncthreads();
+        if (team > 0)
+            return;
+        for (int k = 1; k < teams; ++k)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) dw[i] += joined[(k * 8 + i) * L + t];
+    }
+    if (gridDim.x == 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < columns)
+                finish_weight(g, c + i, double(dw[i]));
+    } else if (columns > 0) {
+        Eight<false> e;
         e.set(dw);
-        store_eight<false>(g.partial, (int64_t(blockIdx.x) * kTeams + team) * g.columns + c, 8, e);
+        store_eight<false, false>(g.partial, int64_t(blockIdx.x) * g.columns + c, 8, e);
     }
 }
 
@@ -262,20 +397,20 @@ __global__ __launch_bounds__(1024) void rms_stats_kernel(RmsArgs a, RmsGrad g) {
     for (int c = threadIdx.x * 8; c < a.dim; c += 8192) {
         const int n = a.dim - c;
         float x[8], dy[8], w[8];
-        load_values(a.x_bf16, a.x, row * a.x_stride + c, n, x);
-        load_values(g.grad_out_bf16, g.grad_out, row * g.grad_out_stride + c, n, dy);
+        load_values<true>(a.x_bf16, a.x, row * a.x_stride + c, n, c > 0, x);
+        load_values<true>(g.grad_out_bf16, g.grad_out, row * g.grad_out_stride + c, n, c > 0, dy);
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = 1.0f;
         if (a.weight)
-            load_values(a.weight_bf16, a.weight, c, n, w);
+            load_values<true>(a.weight_bf16, a.weight, c, n, c > 0, w);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             square = fma(double(x[i]), double(x[i]), square);
             along = fma(double(x[i]), double(dy[i] * w[i]), along);
         }
     }
-    square = wave_sum(square);
-    along = wave_sum(along);
+    square = lanes_sum<64>(square);
+    along = lanes_sum<64>(along);
     if (threadIdx.x % 64 == 0) {
         part[threadIdx.x / 64][0] = square;
         part[threadIdx.x / 64][1] = along;
@@ -287,9 +422,9 @@ __global__ __launch_bounds__(1024) void rms_stats_kernel(RmsArgs a, RmsGrad g) {
             square += part[k][0];
             along += part[k][1];
         }
-        const double r = 1.0 / sqrt(square / a.dim + double(a.eps));
+        const double r = inverse_root(fma(square, a.per_column, double(a.eps)));
         g.stats[2 * row] = float(r);
-        g.stats[2 * row + 1] = float(along * r / a.dim);
+        g.stats[2 * row + 1] = float(along * r * a.per_column);
     }
 }
 
@@ -302,15 +437,15 @@ __global__ __launch_bounds__(256) void rms_wide_grad_kernel(RmsArgs a, RmsGrad g
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = 1.0f;
     if (a.weight)
-        load_values(a.weight_bf16, a.weight, c, n, w);
+        load_values<true>(a.weight_bf16, a.weight, c, n, c > 0, w);
     const int64_t first = int64_t(blockIdx.x) * kRmsWideRows;
     const int64_t end = first + kRmsWideRows < a.tokens ? first + kRmsWideRows : a.tokens;
     for (int64_t row = first; row < end; ++row) {
         float x[8], dy[8], ds[8] = {}, dx[8];
-        load_values(a.x_bf16, a.x, row * a.x_stride + c, n, x);
-        load_values(g.grad_out_bf16, g.grad_out, row * g.grad_out_stride + c, n, dy);
+        load_values<true>(a.x_bf16, a.x, row * a.x_stride + c, n, c > 0, x);
+        load_values<true>(g.grad_out_bf16, g.grad_out, row * g.grad_out_stride + c, n, c > 0, dy);
         if (g.grad_sum)
-            load_values(g.grad_x_bf16, g.grad_sum, row * g.grad_sum_stride + c, n, ds);
+            load_values<true>(g.grad_x_bf16, g.grad_sum, row * g.grad_sum_stride + c, n, c > 0, ds);
         const float inverse = g.stats[2 * row], mean = g.stats[2 * row + 1];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -319,7 +454,7 @@ __global__ __launch_bounds__(256) void rms_wide_grad_kernel(RmsArgs a, RmsGrad g
             recent[i] = fmaf(dy[i], x[i], recent[i]);
         }
         if (g.grad_x)
-            store_values(g.grad_x_bf16, g.grad_x, row * g.grad_x_stride + c, n, dx);
+            store_values<true>(g.grad_x_bf16, g.grad_x, row * g.grad_x_stride + c, n, dx);
         if ((row - first) % kRmsFoldRows == kRmsFoldRows - 1) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
@@ -333,7 +468,7 @@ __global__ __launch_bounds__(256) void rms_wide_grad_kernel(RmsArgs a, RmsGrad g
         for (int i = 0; i < 8; ++i) dw[i] += recent[i];
         Eight<false> e;
         e.set(dw);
-        store_eight<false>(g.partial, int64_t(blockIdx.x) * g.columns + c, 8, e);
+        store_eight<false, false>(g.partial, int64_t(blockIdx.x) * g.columns + c, 8, e);
     }
 }
 
@@ -345,7 +480,7 @@ __global__ __launch_bounds__(1024) void rms_join_kernel(RmsArgs a, RmsGrad g) {
     const int c = int(blockIdx.x) * 32 + column;
     double sum = 0.0;
     if (c < a.dim) {
-#pragma unroll 8
+#pragma unroll 16
         for (int64_t k = stripe; k < g.partials; k += 32) sum += double(g.partial[k * g.columns + c]);
     }
     part[stripe][column] = sum;
@@ -353,101 +488,157 @@ __global__ __launch_bounds__(1024) void rms_join_kernel(RmsArgs a, RmsGrad g) {
     if (stripe == 0 && c < a.dim) {
         sum = 0.0;
         for (int k = 0; k < 32; ++k) sum += part[k][column];
-        if (g.grad_weight_bf16) {
-            __bf16 *to = (__bf16 *)g.grad_weight + c;
-            if (g.add_weight)
-                sum += double(float(*to));
-            *to = __bf16(float(sum));
-        } else {
-            float *to = (float *)g.grad_weight + c;
-            if (g.add_weight)
-                sum += double(*to);
-            *to = float(sum);
+        finish_weight(g, c, sum);
+    }
+}
+
+// Lanes of a row's team: the fewest that hold it, eight columns each.
+int lanes_of(int32_t dim) {
+    int lanes = 16;
+    while (lanes < 1024 && dim > 8 * lanes) lanes *= 2;
+    return lanes;
+}
+
+template <int N>
+using Constant = std::integral_constant<int, N>;
+
+template <bool TAIL, bool X_BF16, bool RES, bool RES_BF16, bool QUANT>
+hipError_t launch_rms_of(const RmsArgs &a, const RmsOut &o, hipStream_t stream) {
+    auto run = [&](auto lanes, auto times) {
+        constexpr int L = decltype(lanes)::value, V = decltype(times)::value;
+        constexpr int kTeams = rms_block(L) / L;
+        rms_kernel<L, V, TAIL, X_BF16, RES, RES_BF16, QUANT>
+            <<<grid_of((a.tokens + kTeams - 1) / kTeams), rms_block(L), 0, stream>>>(a, o);
+        return hipGetLastError();
+    };
+    const int lanes = lanes_of(a.dim);
+    // Half the lanes with twice the columns, where rows are many, a team's last lanes have no
+    // columns and a lane has little to load: a wave's fixed work counts more there.
+    if constexpr (!TAIL && (QUANT || !RES)) {
+        if (a.tokens >= 2048 && 8 * a.dim <= 7 * 8 * lanes) {
+            switch (lanes) {
+            case 128: return run(Constant<64>{}, Constant<2>{});
+            case 256: return run(Constant<128>{}, Constant<2>{});
+            case 512: return run(Constant<256>{}, Constant<2>{});
+            case 1024: return run(Constant<512>{}, Constant<2>{});
+            }
         }
     }
-}
-
-int waves_of(int32_t dim) {
-    for (int w = 1; w < kRmsMaxWaves; w *= 2)
-        if (dim <= 512 * w)
-            return w;
-    return kRmsMaxWaves;
-}
-
-template <bool X_BF16, bool RES, bool RES_BF16, bool QUANT>
-hipError_t launch_rms_of(const RmsArgs &a, const RmsOut &o, hipStream_t stream) {
-    auto run = [&](auto waves, auto times) {
-        constexpr int W = decltype(waves)::value, V = decltype(times)::value;
-        constexpr int kTeams = rms_block(W) / 64 / W;
-        rms_kernel<W, V, X_BF16, RES, RES_BF16, QUANT>
-            <<<grid_of((a.tokens + kTeams - 1) / kTeams), rms_block(W), 0, stream>>>(a, o);
-        return hipGetLastError();
-    };
-    std::integral_constant<int, 1> c1;
-    std::integral_constant<int, 2> c2;
-    std::integral_constant<int, 4> c4;
-    std::integral_constant<int, 8> c8;
-    std::integral_constant<int, 16> c16;
-    switch (waves_of(a.dim)) {
-    case 1: return run(c1, c1);
-    case 2: return run(c2, c1);
-    case 4: return run(c4, c1);
-    case 8: return run(c8, c1);
+    switch (lanes) {
+    case 16: return run(Constant<16>{}, Constant<1>{});
+    case 32: return run(Constant<32>{}, Constant<1>{});
+    case 64: return run(Constant<64>{}, Constant<1>{});
+    case 128: return run(Constant<128>{}, Constant<1>{});
+    case 256: return run(Constant<256>{}, Constant<1>{});
+    case 512: return run(Constant<512>{}, Constant<1>{});
     }
     if (a.dim <= 8192)
-        return run(c16, c1);
+        return run(Constant<1024>{}, Constant<1>{});
     if (a.dim <= 16384)
-        return run(c16, c2);
-    return a.dim <= 32768 ? run(c16, c4) : run(c16, c8);
+        return run(Constant<1024>{}, Constant<2>{});
+    return a.dim <= 32768 ? run(Constant<1024>{}, Constant<4>{})
+                          : run(Constant<1024>{}, Constant<8>{});
 }
 
-template <bool QUANT>
+template <bool TAIL, bool QUANT>
 hipError_t launch_rms_types(const RmsArgs &a, const RmsOut &o, hipStream_t stream) {
     if (!a.residual)
-        return a.x_bf16 ? launch_rms_of<true, false, true, QUANT>(a, o, stream)
-                        : launch_rms_of<false, false, false, QUANT>(a, o, stream);
+        return a.x_bf16 ? launch_rms_of<TAIL, true, false, true, QUANT>(a, o, stream)
+                        : launch_rms_of<TAIL, false, false, false, QUANT>(a, o, stream);
     if (!a.x_bf16)
-        return launch_rms_of<false, true, false, QUANT>(a, o, stream);
-    return a.residual_bf16 ? launch_rms_of<true, true, true, QUANT>(a, o, stream)
-                           : launch_rms_of<true, true, false, QUANT>(a, o, stream);
+        return launch_rms_of<TAIL, false, true, false, QUANT>(a, o, stream);
+    return a.residual_bf16 ? launch_rms_of<TAIL, true, true, true, QUANT>(a, o, stream)
+                           : launch_rms_of<TAIL, true, true, false, QUANT>(a, o, stream);
 }
 
-int64_t grad_blocks(int64_t tokens, int32_t dim) {
-    const int waves = waves_of(dim);
-    const int64_t teams = rms_block(waves) / 64 / waves;
-    const int64_t all = (tokens + teams - 1) / teams;
-    return std::min<int64_t>(all, 4096 / (rms_block(waves) / 64));
+template <bool TAIL>
+hipError_t launch_rms_tail(const RmsArgs &a, const RmsOut &o, hipStream_t stream) {
+    return o.scales ? launch_rms_types<TAIL, true>(a, o, stream)
+                    : launch_rms_types<TAIL, false>(a, o, stream);
 }
 
-template <bool X_BF16, bool DY_BF16, bool DX_BF16>
+struct GradShape {
+    int lanes, block;
+    int64_t blocks;
+};
+
+// `row_bytes`: what a row reads. Few rows go to one workgroup, which needs no second launch.
+// Else at least two rows each (a part of the weight's gradient for every row costs more),
+// and as many workgroups as keep some 8 MB of loads in flight: with more, HBM falls behind.
+// 32768 rows of 1600, fp32 with bf16 dy: 127 us with 512, 144 with 1024; 30000 of bf16: 95
+// and 78.
+GradShape grad_shape(int64_t tokens, int32_t dim, int64_t row_bytes) {
+    GradShape s;
+    s.lanes = lanes_of(dim);
+    s.block = rms_block(s.lanes);
+    const int64_t few = std::max(512, s.lanes) / s.lanes;
+    if (tokens <= 2 * few) {
+        s.block = std::max(512, s.lanes);
+        s.blocks = 1;
+        return s;
+    }
+    const int64_t teams = s.block / s.lanes, turns = (tokens + teams - 1) / teams;
+    const int64_t most = s.lanes == 1024 ? 256 : teams * row_bytes < 14336 ? 1024 : 512;
+    s.blocks = std::min((turns + 1) / 2, most);
+    return s;
+}
+
+int64_t row_bytes(const RmsArgs &a, const RmsGrad &g) {
+    const int64_t x = a.x_bf16 ? 2 : 4, dy = g.grad_out_bf16 ? 2 : 4, ds = g.grad_x_bf16 ? 2 : 4;
+    return a.dim * (x + dy + (g.grad_sum ? ds : 0));
+}
+
+template <bool TAIL, bool X_BF16, bool DY_BF16, bool DX_BF16>
 hipError_t launch_rms_grad_of(const RmsArgs &a, const RmsGrad &g, hipStream_t stream) {
-    auto run = [&](auto waves) {
-        constexpr int W = decltype(waves)::value;
-        rms_grad_kernel<W, X_BF16, DY_BF16, DX_BF16>
-            <<<uint32_t(grad_blocks(a.tokens, a.dim)), rms_block(W), 0, stream>>>(a, g);
+    const GradShape s = grad_shape(a.tokens, a.dim, row_bytes(a, g));
+    auto run = [&](auto lanes) {
+        constexpr int L = decltype(lanes)::value;
+        const size_t lds = s.block > L && g.grad_weight ? size_t(s.block) * 8 * 4 : 0;
+        rms_grad_kernel<L, TAIL, X_BF16, DY_BF16, DX_BF16>
+            <<<uint32_t(s.blocks), s.block, lds, stream>>>(a, g);
         return hipGetLastError();
     };
-    switch (waves_of(a.dim)) {
-    case 1: return run(std::integral_constant<int, 1>{});
-    case 2: return run(std::integral_constant<int, 2>{});
-    case 4: return run(std::integral_constant<int, 4>{});
-    case 8: return run(std::integral_constant<int, 8>{});
-    default: return run(std::integral_constant<int, 16>{});
+    switch (s.lanes) {
+    case 16: return run(Constant<16>{});
+    case 32: return run(Constant<32>{});
+    case 64: return run(Constant<64>{});
+    case 128: return run(Constant<128>{});
+    case 256: return run(Constant<256>{});
+    case 512: return run(Constant<512>{});
+    default: return run(Constant<1024>{});
     }
+}
+
+template <bool TAIL>
+hipError_t launch_rms_grad_types(const RmsArgs &a, const RmsGrad &g, hipStream_t stream) {
+    auto by_dx = [&](auto x, auto dy) {
+        constexpr bool X = decltype(x)::value, DY = decltype(dy)::value;
+        return g.grad_x_bf16 ? launch_rms_grad_of<TAIL, X, DY, true>(a, g, stream)
+                             : launch_rms_grad_of<TAIL, X, DY, false>(a, g, stream);
+    };
+    auto by_dy = [&](auto x) {
+        return g.grad_out_bf16 ? by_dx(x, std::true_type{}) : by_dx(x, std::false_type{});
+    };
+    return a.x_bf16 ? by_dy(std::true_type{}) : by_dy(std::false_type{});
 }
 
 }  // namespace
 
 hipError_t launch_rms(const RmsArgs &args, const RmsOut &out, hipStream_t stream) {
-    return out.scales ? launch_rms_types<true>(args, out, stream)
-                      : launch_rms_types<false>(args, out, stream);
+    return args.dim % 8 ? launch_rms_tail<true>(args, out, stream)
+                        : launch_rms_tail<false>(args, out, stream);
 }
 
-int64_t rms_partials(int64_t tokens, int32_t dim) {
+int64_t rms_partials(const RmsArgs &a, const RmsGrad &g) {
+    if (a.dim > kRmsHeldDim)
+        return (a.tokens + kRmsWideRows - 1) / kRmsWideRows;
+    return a.tokens ? grad_shape(a.tokens, a.dim, row_bytes(a, g)).blocks : 0;
+}
+
+int64_t rms_most_partials(int64_t tokens, int32_t dim) {
     if (dim > kRmsHeldDim)
         return (tokens + kRmsWideRows - 1) / kRmsWideRows;
-    const int waves = waves_of(dim);
-    return grad_blocks(tokens, dim) * (rms_block(waves) / 64 / waves);
+    return tokens ? grad_shape(tokens, dim, 0).blocks : 0;  // the fewer bytes, the more
 }
 
 hipError_t launch_rms_grad(const RmsArgs &a, const RmsGrad &g, hipStream_t stream) {
@@ -460,18 +651,13 @@ hipError_t launch_rms_grad(const RmsArgs &a, const RmsGrad &g, hipStream_t strea
         rms_wide_grad_kernel<<<grid, 256, 0, stream>>>(a, g);
         return hipGetLastError();
     }
-    auto by_dx = [&](auto x, auto dy) {
-        constexpr bool X = decltype(x)::value, DY = decltype(dy)::value;
-        return g.grad_x_bf16 ? launch_rms_grad_of<X, DY, true>(a, g, stream)
-                             : launch_rms_grad_of<X, DY, false>(a, g, stream);
-    };
-    auto by_dy = [&](auto x) {
-        return g.grad_out_bf16 ? by_dx(x, std::true_type{}) : by_dx(x, std::false_type{});
-    };
-    return a.x_bf16 ? by_dy(std::true_type{}) : by_dy(std::false_type{});
+    return a.dim % 8 ? launch_rms_grad_types<true>(a, g, stream)
+                     : launch_rms_grad_types<false>(a, g, stream);
 }
 
 hipError_t launch_rms_join(const RmsArgs &a, const RmsGrad &g, hipStream_t stream) {
+    if (a.dim <= kRmsHeldDim && g.partials == 1)
+        return hipSuccess;  // its workgroup has done it
     rms_join_kernel<<<uint32_t((a.dim + 31) / 32), 1024, 0, stream>>>(a, g);
     return hipGetLastError();
 }

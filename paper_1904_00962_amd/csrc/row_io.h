@@ -9,6 +9,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 namespace lamb_mi355x {
 
 __device__ inline float bf16_low(uint32_t pair) { return __uint_as_float(pair << 16); }
@@ -73,46 +75,73 @@ struct Eight {
     }
 };
 
-// Elements at .. at + n - 1 of `base` (n below 1: none); what is past them is 0.
-template <bool BF16, bool STREAM = false>
-__device__ inline Eight<BF16> load_eight(const void *base, int64_t at, int n) {
-    Eight<BF16> e;
+// Moves the elements `by` places (0 to 7) towards the first; zeros follow.
+template <bool BF16>
+__device__ inline void move_down(Eight<BF16> &e, int by) {
+    constexpr int kWords = BF16 ? 4 : 8;
     if (BF16) {
-        const Global<uint16_t> *p = (const Global<uint16_t> *)base + at;
-        if (n >= 8) {
-            const Bytes16 w = load_16<STREAM>(p);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) e.u[i] = w[i];
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                e.u[i] = (2 * i < n ? uint32_t(p[2 * i]) : 0u) |
-                         (2 * i + 1 < n ? uint32_t(p[2 * i + 1]) << 16 : 0u);
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t above = i < 3 ? e.u[i < 3 ? i + 1 : 3] : 0u;
+            e.u[i] = by & 1 ? above << 16 | e.u[i] >> 16 : e.u[i];
         }
-    } else {
-        const Global<uint32_t> *p = (const Global<uint32_t> *)base + at;
-        if (n >= 8) {
-            const Bytes16 a = load_16<STREAM>(p), b = load_16<STREAM>(p + 4);
+        by >>= 1;
+    }
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                e.u[i] = a[i];
-                e.u[BF16 ? 0 : i + 4] = b[i];
-            }
-        } else {
+    for (int step = 1; step < kWords; step *= 2)
 #pragma unroll
-            for (int i = 0; i < 8; ++i) e.u[BF16 ? 0 : i] = i < n ? p[i] : 0u;
+        for (int i = 0; i < kWords; ++i) {
+            const uint32_t above = i + step < kWords ? e.u[(i + step) % kWords] : 0u;
+            e.u[i] = by & step ? above : e.u[i];
         }
+}
+
+// Elements at .. at + n - 1 of `base` (n below 1: none); what is past them is 0, once
+// settled. Where the eight that end with the last of them may be read (`back`), a row's last
+// few take the same one load, of those eight, and settle() moves them to their places: later,
+// so that no load waits for another's end. TAIL false: n is at least 8, or below 1; rows of
+// whole eights go faster where nothing else is compiled in (32768 rows of 1600: the 8-bit
+// norm 62 us in place of 69, the gradients 126 in place of 157).
+template <bool BF16, bool TAIL, bool STREAM = false>
+__device__ inline Eight<BF16> load_eight(const void *base, int64_t at, int n, bool back = false) {
+    using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
+    Eight<BF16> e = {};
+    const Global<T> *p = (const Global<T> *)base + at;
+    if (n >= 8 || (TAIL && back && n > 0)) {
+        if (TAIL)
+            p -= n < 8 ? 8 - n : 0;
+        const Bytes16 a = load_16<STREAM>(p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e.u[i] = a[i];
+        if (!BF16) {
+            const Bytes16 b = load_16<STREAM>(p + 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) e.u[BF16 ? 0 : i + 4] = b[i];
+        }
+    } else if (TAIL && n > 0) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n)
+                e.u[BF16 ? i / 2 : i] |= uint32_t(p[i]) << (BF16 ? i % 2 * 16 : 0);
     }
     return e;
 }
 
-template <bool BF16, bool STREAM = false>
+template <bool TAIL, bool BF16>
+__device__ inline void settle(Eight<BF16> &e, int n, bool back) {
+    if (TAIL && back && n > 0 && n < 8) {
+        asm volatile("");  // stays a branch: as selects the moves would cost every lane
+        move_down(e, 8 - n);
+    }
+}
+
+template <bool BF16, bool TAIL, bool STREAM = false>
 __device__ inline void store_eight(void *base, int64_t at, int n, const Eight<BF16> &e) {
     if (BF16) {
         Global<uint16_t> *p = (Global<uint16_t> *)base + at;
         if (n >= 8) {
             store_16<STREAM>(p, Bytes16{e.u[0], e.u[1], e.u[2], e.u[3]});
-        } else {
+        } else if (TAIL && n > 0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (i < n)
@@ -124,7 +153,7 @@ __device__ inline void store_eight(void *base, int64_t at, int n, const Eight<BF
             store_16<STREAM>(p, Bytes16{e.u[0], e.u[1], e.u[2], e.u[3]});
             store_16<STREAM>(p + 4, Bytes16{e.u[BF16 ? 0 : 4], e.u[BF16 ? 0 : 5],
                                              e.u[BF16 ? 0 : 6], e.u[BF16 ? 0 : 7]});
-        } else {
+        } else if (TAIL && n > 0) {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
                 if (i < n)
@@ -135,25 +164,34 @@ __device__ inline void store_eight(void *base, int64_t at, int n, const Eight<BF
 
 // The same with a type that is known at run time only, for what is not on a kernel's
 // longest path.
-__device__ inline void load_values(bool bf16, const void *base, int64_t at, int n,
-                                   float (&v)[8]) {
-    if (bf16)
-        load_eight<true>(base, at, n).get(v);
-    else
-        load_eight<false>(base, at, n).get(v);
+template <bool BF16, bool TAIL>
+__device__ inline void load_values_of(const void *base, int64_t at, int n, bool back,
+                                      float (&v)[8]) {
+    Eight<BF16> e = load_eight<BF16, TAIL>(base, at, n, back);
+    settle<TAIL>(e, n, back);
+    e.get(v);
 }
 
-template <bool STREAM = false>
+template <bool TAIL>
+__device__ inline void load_values(bool bf16, const void *base, int64_t at, int n, bool back,
+                                   float (&v)[8]) {
+    if (bf16)
+        load_values_of<true, TAIL>(base, at, n, back, v);
+    else
+        load_values_of<false, TAIL>(base, at, n, back, v);
+}
+
+template <bool TAIL, bool STREAM = false>
 __device__ inline void store_values(bool bf16, void *base, int64_t at, int n,
                                     const float (&v)[8]) {
     if (bf16) {
         Eight<true> e;
         e.set(v);
-        store_eight<true, STREAM>(base, at, n, e);
+        store_eight<true, TAIL, STREAM>(base, at, n, e);
     } else {
         Eight<false> e;
         e.set(v);
-        store_eight<false, STREAM>(base, at, n, e);
+        store_eight<false, TAIL, STREAM>(base, at, n, e);
     }
 }
 

@@ -125,7 +125,7 @@ def test_norm_workspace_is_within_the_stated_bytes(lib, dim):
     for tokens in (0, 1, 7, 4096, 4097, 100000, 1 << 24):
         r = _rms(residual=None, tokens=tokens, dim=dim, x_stride=dim)
         if dim <= 8192:
-            most = 4 * columns * min(4096, tokens + 3) + 256
+            most = 4 * columns * min(1024, tokens + 3) + 256
         else:
             most = 4 * columns * (tokens // 256 + 1) + 8 * tokens + 512
         assert _ops.lamb_rms_workspace(r) <= most, tokens
