@@ -303,9 +303,9 @@ def lamb_grad_plan_create(tensors: Sequence[Tuple[int, int, int, int, int]],
     """tensors: (in_ptr, out_ptr, numel, in_dtype, out_dtype) each."""
     n = len(tensors)
     arr = (lamb_grad_tensor * max(n, 1))()
-    for i, (a, b, numel, in_dtype, out_dtype) in enumerate(tensors):
-        arr[i] = lamb_grad_tensor(int(a) or None, int(b) or None, int(numel), int(in_dtype),
-                                  int(out_dtype))
+    for t, (a, b, numel, in_dtype, out_dtype) in zip(arr, tensors):
+        t.input, t.out, t.numel = a or None, b or None, numel
+        t.in_dtype, t.out_dtype = in_dtype, out_dtype
     out = ctypes.c_void_p()
     _check(load().lamb_grad_plan_create(arr, n, int(norm), ctypes.byref(out)),
            "lamb_grad_plan_create")

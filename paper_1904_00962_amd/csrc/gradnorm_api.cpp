@@ -48,22 +48,25 @@ lamb_status build(lamb_grad_plan *plan, std::vector<GradTensor> &tensors) {
     }
     l.n = int32_t(tensors.size());
     l.chunks = int32_t(chunks);
-    std::vector<int32_t> chunk_tensor;
-    chunk_tensor.reserve(size_t(chunks));
-    for (int32_t i = 0; i < l.n; ++i)
-        chunk_tensor.insert(chunk_tensor.end(), size_t(tensors[i].chunks), i);
-
     size_t bytes = 0;
     auto take = [&](size_t size) {
         const size_t at = bytes;
         bytes += size_t(round_up(int64_t(size), 256));
         return at;
     };
+    // what the host writes comes first, so that one copy brings it
     const size_t o_tensors = take(tensors.size() * sizeof(GradTensor));
-    const size_t o_chunks = take(chunk_tensor.size() * 4);
-    const size_t o_partials = take(chunk_tensor.size() * 8);
+    const size_t o_chunks = take(size_t(chunks) * 4);
     const size_t o_powers = take(tensors.size() * 8);
     const size_t o_done = take((tensors.size() + 1) * 4);
+    const size_t written = bytes;
+    const size_t o_partials = take(size_t(chunks) * 8);
+    std::vector<char> host(written, 0);
+    std::copy_n(tensors.data(), tensors.size(),
+                reinterpret_cast<GradTensor *>(host.data() + o_tensors));
+    int32_t *chunk_tensor = reinterpret_cast<int32_t *>(host.data() + o_chunks);
+    for (int32_t i = 0; i < l.n; ++i)
+        std::fill_n(chunk_tensor + tensors[i].first_chunk, tensors[i].chunks, i);
     hipError_t err = hipGetDevice(&plan->device);
     if (err != hipSuccess)
         return fail_hip(err, "hipGetDevice");
@@ -79,16 +82,7 @@ lamb_status build(lamb_grad_plan *plan, std::vector<GradTensor> &tensors) {
         return fail(LAMB_ENOMEM, "hipMalloc of %zu bytes: %s", bytes, hipGetErrorString(err));
     }
     char *base = static_cast<char *>(plan->block);
-    auto up = [&](size_t at, const void *from, size_t size) {
-        if (err == hipSuccess && size)
-            err = hipMemcpy(base + at, from, size, hipMemcpyHostToDevice);
-    };
-    up(o_tensors, tensors.data(), tensors.size() * sizeof(GradTensor));
-    up(o_chunks, chunk_tensor.data(), chunk_tensor.size() * 4);
-    const std::vector<double> zeros(tensors.size(), 0.0);
-    up(o_powers, zeros.data(), zeros.size() * 8);
-    const std::vector<uint32_t> none(tensors.size() + 1, 0);
-    up(o_done, none.data(), none.size() * 4);
+    err = hipMemcpy(base, host.data(), written, hipMemcpyHostToDevice);
     if (err != hipSuccess)
         return fail_hip(err, "hipMemcpy");
     l.tensors = reinterpret_cast<const GradTensor *>(base + o_tensors);

@@ -497,22 +497,27 @@ class GradNorm:
             raise ValueError("norm must be one of %s" % (tuple(_lib.NORMS),))
         self.norm = norm
         self.device = self.grads[0].device
+        same = self.outputs is self.grads
         rows = []
         for i, (a, b) in enumerate(zip(self.grads, self.outputs)):
-            for name, t in (("gradient", a), ("output", b)):
-                _on_gpu("%s %d" % (name, i), t, self.device)
-                if not t.is_contiguous():
-                    raise ValueError("%s %d is not contiguous" % (name, i))
-            if a.numel() != b.numel():
-                raise ValueError("gradient %d has %d elements, its output %d"
-                                 % (i, a.numel(), b.numel()))
-            rows.append((a.data_ptr(), b.data_ptr(), a.numel(), _float_code(a.dtype),
-                         _float_code(b.dtype)))
-        self.norms = torch.zeros(len(rows), dtype=torch.float64, device=self.device)
-        self.total = torch.zeros((), dtype=torch.float64, device=self.device)
-        self.found_nonfinite = torch.zeros(1, dtype=torch.int32, device=self.device)
+            row = self._tensor("gradient", i, a)
+            to = row if same else self._tensor("output", i, b)
+            if row[1] != to[1]:
+                raise ValueError("gradient %d has %d elements, its output %d" % (i, row[1], to[1]))
+            rows.append((row[0], to[0], row[1], row[2], to[2]))
+        results = torch.zeros(len(rows) + 2, dtype=torch.float64, device=self.device)
+        self.norms, self.total = results[:-2], results[-2]
+        self.found_nonfinite = results[-1:].view(torch.int32)[:1]
         with _on(self.device):
             self.plan = _ops.lamb_grad_plan_create(rows, _lib.NORMS[norm])
+
+    def _tensor(self, name, i, t):
+        """(address, elements, type) of a tensor of the list."""
+        if not t.is_cuda or t.device != self.device:
+            _on_gpu("%s %d" % (name, i), t, self.device)
+        if not t.is_contiguous():
+            raise ValueError("%s %d is not contiguous" % (name, i))
+        return t.data_ptr(), t.numel(), _float_code(t.dtype)
 
     def run(self):
         """Enqueue the norms on the current stream; returns ``total``."""
