@@ -2,13 +2,15 @@
 with the package's optimizers and operators:
 
   lookup        ops.embedding: rows of the table's bf16 copy
-  body          residual blocks over the mean of the last few tokens (torch, autograd)
+  body          residual blocks over the mean of the last few tokens (torch, autograd),
+                with ops.rms_norm and ops.rms_norm_grad on the residual stream
   loss          ops.linear_cross_entropy against the same table, without keeping logits
   gradients     ops.linear_cross_entropy_grad writes the table's gradient buffer and the
                 hidden states' gradient; after the body's backward pass
                 ops.embedding_grad adds the lookup's share to the same buffer
-  step          Muon for the blocks' matrices, LAMB for the table, which writes the bf16
-                copy that the next lookup and loss read
+  clipping      ops.GradNorm keeps all gradients together to one norm
+  step          Muon for the blocks' matrices, LAMB for the norms' weights and for the
+                table, which writes the bf16 copy that the next lookup and loss read
 
 The data are synthetic: each token follows the one before by a fixed random rule three
 times out of four, and is random otherwise, so the loss can fall to about a third of
@@ -48,6 +50,24 @@ def batch(rule, tokens, gen):
     return ids, targets
 
 
+class Norm(torch.autograd.Function):
+    """(norm, sum) of the residual stream and a block's output, the norm in ``dtype``."""
+
+    @staticmethod
+    def forward(ctx, stream, branch, weight, dtype):
+        norm, total = ops.rms_norm(branch, weight, residual=stream, out_dtype=dtype)
+        ctx.save_for_backward(total, weight)
+        return norm, total
+
+    @staticmethod
+    def backward(ctx, grad_norm, grad_total):
+        total, weight = ctx.saved_tensors
+        grad, grad_weight = torch.empty_like(total), torch.empty_like(weight)
+        ops.rms_norm_grad(total, weight, grad_norm.contiguous(), grad, grad_weight,
+                          grad_sum=grad_total.contiguous())
+        return grad, grad, grad_weight, None
+
+
 class Body(torch.nn.Module):
     def __init__(self, dim, blocks):
         super().__init__()
@@ -55,15 +75,17 @@ class Body(torch.nn.Module):
             torch.randn(r, c, device="cuda") / math.sqrt(c))
         self.up = torch.nn.ParameterList([make(2 * dim, dim) for _ in range(blocks)])
         self.down = torch.nn.ParameterList([make(dim, 2 * dim) for _ in range(blocks)])
+        self.norms = torch.nn.ParameterList(
+            [torch.nn.Parameter(torch.ones(dim, device="cuda")) for _ in range(blocks + 1)])
 
     def forward(self, rows):
-        x = rows.float()
-        past = sum(torch.roll(x, k, 0) for k in range(1, CONTEXT)) / (CONTEXT - 1)
-        x = x + 0.1 * past
-        for up, down in zip(self.up, self.down):
-            n = x * torch.rsqrt(x.square().mean(dim=1, keepdim=True) + 1e-6)
-            x = x + torch.relu(n @ up.t()) @ down.t()
-        return (x * torch.rsqrt(x.square().mean(dim=1, keepdim=True) + 1e-6)).bfloat16()
+        stream = rows.float()
+        past = sum(torch.roll(stream, k, 0) for k in range(1, CONTEXT)) / (CONTEXT - 1)
+        branch = 0.1 * past
+        for up, down, weight in zip(self.up, self.down, self.norms):
+            n, stream = Norm.apply(stream, branch, weight, torch.float32)
+            branch = torch.relu(n @ up.t()) @ down.t()
+        return Norm.apply(stream, branch, self.norms[-1], torch.bfloat16)[0]
 
 
 def train(steps=100, vocab=2000, dim=128, blocks=2, tokens=2048, seed=0, report=None):
@@ -74,13 +96,15 @@ def train(steps=100, vocab=2000, dim=128, blocks=2, tokens=2048, seed=0, report=
     table = torch.randn(vocab, dim, generator=gen, device="cuda").mul_(0.02)
     grad_table = torch.zeros(vocab, dim, dtype=torch.bfloat16, device="cuda")
     body = Body(dim, blocks)
-    matrices = list(body.parameters())
-    for p in matrices:
+    matrices, weights = [*body.up, *body.down], list(body.norms)
+    for p in body.parameters():
         p.grad = torch.zeros_like(p)  # persistent: the plans bind the buffers
     lamb = LAMB([table], [grad_table], lr=0.02, weight_decay=0.0, clamp=(0.1, 10.0))
     copy = lamb.attach_bf16_copies()[0].view(vocab, dim)
     copy.copy_(table)
     muon = Muon([p.data for p in matrices], [p.grad for p in matrices], lr=0.01, momentum=0.9)
+    lamb_weights = LAMB([p.data for p in weights], [p.grad for p in weights], lr=0.002)
+    clipper = ops.GradNorm([grad_table] + [p.grad for p in body.parameters()])
     grad_hidden = torch.empty(tokens, dim, dtype=torch.bfloat16, device="cuda")
     scale = math.sqrt(dim)
     losses = []
@@ -92,11 +116,13 @@ def train(steps=100, vocab=2000, dim=128, blocks=2, tokens=2048, seed=0, report=
                                                 ignore_index=IGNORE)
         ops.linear_cross_entropy_grad(hidden.detach(), copy, targets, lse, grad_hidden,
                                       grad_table, ignore_index=IGNORE)
-        for p in matrices:
+        for p in body.parameters():
             p.grad.zero_()
         hidden.backward(grad_hidden)
         ops.embedding_grad(ids, rows.grad, grad_table, scale=scale, accumulate=True)
+        clipper.clip(1.0)
         muon.step()
+        lamb_weights.step()
         lamb.step()
         losses.append(mean)
         if report and (step % 10 == 0 or step + 1 == steps):
