@@ -321,7 +321,7 @@ LAMB_API lamb_status lamb_rms_quantize(const lamb_rms *rms, void *summed, int64_
  * same inputs give the same bits.
  * The workspace (256-byte aligned; lamb_rms_workspace, host only) is needed for grad_weight,
  * and for grad_x where dim is over 8192; else NULL will do. It takes 4 bytes for each of the
- * columns of at most 1024 rows (dim over 8192: of one row in 256, and 8 bytes for each row).
+ * columns of at most 1024 rows (dim over 8192: of one row in 256, and 16 bytes for each row).
  */
 typedef struct lamb_rms_grads {
     const void *grad_out;

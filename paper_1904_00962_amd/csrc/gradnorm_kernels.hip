@@ -249,8 +249,8 @@ __global__ __launch_bounds__(kGradBlock) void grad_clip_kernel(GradList l, const
         *nonfinite_out = !finite;
     if (block >= l.chunks)
         return;
-    const double scaled = fabs(scale) * norm;
-    const float f = float(finite && scaled > max_norm ? scale * (max_norm / scaled) : scale);
+    const float f = float(finite && fabs(scale) * norm > max_norm
+                              ? copysign(max_norm / norm, scale) : scale);
     const Chunk c(l, l.chunks - 1 - block);
     if (f == 1.0f && c.t.in == c.t.out)
         return;

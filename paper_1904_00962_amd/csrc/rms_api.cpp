@@ -139,7 +139,7 @@ Layout layout_of(const lamb_rms &r) {
     l.columns = round_up(r.dim, 8);
     const int64_t partials = rms_most_partials(r.tokens, int32_t(r.dim));
     l.stats = size_t(round_up(partials * l.columns * 4, 256));
-    l.bytes = l.stats + (r.dim > kRmsHeldDim ? size_t(round_up(r.tokens * 8, 256)) : 0);
+    l.bytes = l.stats + (r.dim > kRmsHeldDim ? size_t(round_up(r.tokens * 16, 256)) : 0);
     return l;
 }
 
@@ -259,7 +259,7 @@ lamb_status lamb_rms_backward(const lamb_rms *rms, const lamb_rms_grads *grads, 
                        reinterpret_cast<float *>(work),
                        0,
                        int32_t(l.columns),
-                       reinterpret_cast<float *>(work + l.stats)};
+                       reinterpret_cast<double *>(work + l.stats)};
     grad.partials = rms_partials(args, grad);
     hipError_t err = hipSuccess;
     if (r.tokens)

@@ -44,7 +44,7 @@ struct RmsGrad {
     float *partial;     // [partials][columns]: parts of the weight's gradient
     int64_t partials;   // rows of it
     int32_t columns;    // dim, rounded up to 8
-    float *stats;       // [tokens][2], for wide rows: 1 / rms, and the mean of g x / rms
+    double *stats;      // [tokens][2], for wide rows: 1 / rms, and the mean of g x / rms
 };
 // Rows of RmsGrad::partial in a call, and in any of these sizes.
 int64_t rms_partials(const RmsArgs &args, const RmsGrad &grad);

@@ -98,6 +98,26 @@ __device__ inline double inverse_root(double v) {
 // The bits of |v| as integers have the order of their values, and NaN above all.
 __device__ inline uint32_t magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
+// r as an fp32 number, and a power of two that elements take first where r is no normal one
+// (all of a row within a factor of four of fp32's ends, or below them with eps 0).
+struct Inverse {
+    float value, shift;
+    __device__ inline explicit Inverse(double r) {
+        const bool small = r > 0x1p126, large = r < 0x1p-126;
+        shift = small ? 0x1p64f : large ? 0x1p-64f : 1.0f;
+        value = float(small ? r * 0x1p-64 : large ? r * 0x1p64 : r);
+    }
+    __device__ inline void times(float (&h)[8]) const {
+        if (shift != 1.0f) {
+            asm volatile("");  // stays a branch, for a whole row
+#pragma unroll
+            for (int i = 0; i < 8; ++i) h[i] *= shift;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] *= value;
+    }
+};
+
 // max(largest / 448, 2^-126) of the bits of a magnitude, and its inverse, both as if
 // divided: an estimate and what it leaves. Not so for infinity and NaN.
 __device__ inline void scale_of(uint32_t largest, float *scale, float *up) {
@@ -182,12 +202,11 @@ __global__ __launch_bounds__(rms_block(L)) void rms_kernel(RmsArgs a, RmsOut o) 
 #pragma unroll
         for (int k = 0; k < kWaves; ++k) sum += part[team][k];
     }
-    const float inverse = float(inverse_root(fma(sum, a.per_column, double(a.eps))));
+    const Inverse inverse(inverse_root(fma(sum, a.per_column, double(a.eps))));
     uint32_t largest = 0;
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[v][i] *= inverse;
+        inverse.times(h[v]);
         if (a.weight) {
             if (!kEarly)
                 load_values<TAIL>(a.weight_bf16, a.weight, c[v], n[v], c[v] > 0, w[v]);
@@ -340,9 +359,9 @@ __global__ __launch_bounds__(L < 1024 ? 512 : 1024) void rms_grad_kernel(RmsArgs
         float ds[8], dx[8];
         now.ds.get(ds);
         if (n > 0) {
+            Inverse(r).times(x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                x[i] *= inverse;
                 dx[i] = fmaf(fmaf(-x[i], mean, gw[i]), inverse, ds[i]);
                 recent[i] = fmaf(dy[i], x[i], recent[i]);
             }
@@ -423,8 +442,8 @@ __global__ __launch_bounds__(1024) void rms_stats_kernel(RmsArgs a, RmsGrad g) {
             along += part[k][1];
         }
         const double r = inverse_root(fma(square, a.per_column, double(a.eps)));
-        g.stats[2 * row] = float(r);
-        g.stats[2 * row + 1] = float(along * r * a.per_column);
+        g.stats[2 * row] = r;
+        g.stats[2 * row + 1] = along * r * a.per_column;
     }
 }
 
@@ -446,10 +465,11 @@ __global__ __launch_bounds__(256) void rms_wide_grad_kernel(RmsArgs a, RmsGrad g
         load_values<true>(g.grad_out_bf16, g.grad_out, row * g.grad_out_stride + c, n, c > 0, dy);
         if (g.grad_sum)
             load_values<true>(g.grad_x_bf16, g.grad_sum, row * g.grad_sum_stride + c, n, c > 0, ds);
-        const float inverse = g.stats[2 * row], mean = g.stats[2 * row + 1];
+        const double r = g.stats[2 * row];
+        const float inverse = float(r), mean = float(g.stats[2 * row + 1]);
+        Inverse(r).times(x);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            x[i] *= inverse;
             dx[i] = fmaf(fmaf(-x[i], mean, dy[i] * w[i]), inverse, ds[i]);
             recent[i] = fmaf(dy[i], x[i], recent[i]);
         }

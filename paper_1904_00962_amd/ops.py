@@ -510,6 +510,8 @@ class GradNorm:
         self.found_nonfinite = results[-1:].view(torch.int32)[:1]
         with _on(self.device):
             self.plan = _ops.lamb_grad_plan_create(rows, _lib.NORMS[norm])
+            # the zeros come before any call's results, whatever its stream
+            torch.cuda.current_stream(self.device).synchronize()
 
     def _tensor(self, name, i, t):
         """(address, elements, type) of a tensor of the list."""

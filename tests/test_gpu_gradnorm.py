@@ -48,8 +48,8 @@ def _near(a, b, kind):
 
 
 def _factor(torch, total, max_norm, scale=1.0):
-    scaled = abs(scale) * total
-    f = scale * (max_norm / scaled) if math.isfinite(total) and scaled > max_norm else scale
+    over = math.isfinite(total) and abs(scale) * total > max_norm
+    f = math.copysign(max_norm / total, scale) if over else scale
     return torch.tensor(f, dtype=torch.float64).float().cuda()
 
 
@@ -123,6 +123,33 @@ def test_clipped_gradients_keep_the_limit():
         assert before > 0.5
         # the factor's rounding to fp32 and the products'
         assert abs(float(plan.run()) - 0.5) <= 0.5 * 2.0 ** -22
+
+
+def test_a_scale_whose_norm_passes_every_type():
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    grads, _ = _grads(torch, [3000], gen, "f32", sigma=1e10)
+    before = grads[0].double()
+    plan = ops.GradNorm(grads)
+    total = float(plan.clip(2.0, scale=-1e305))
+    assert float(torch.linalg.vector_norm(grads[0].double() + before * (2.0 / total))) <= 2.0 ** -22
+
+
+def test_results_of_a_plan_made_on_a_busy_stream():
+    """A call on another stream than the one that made the plan's results."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    g = torch.ones(5000, device="cuda")
+    torch.cuda.synchronize()
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    with torch.cuda.stream(a):
+        torch.cuda._sleep(5_000_000)
+        plan = ops.GradNorm([g], norm="l1")
+    with torch.cuda.stream(b):
+        plan.run()
+    torch.cuda.synchronize()
+    assert float(plan.total) == 5000.0 and float(plan.norms[0]) == 5000.0
 
 
 def test_totals_that_are_no_number():

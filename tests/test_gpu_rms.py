@@ -178,6 +178,28 @@ def test_rows_of_zeros_infinities_and_nan():
         assert torch.equal(ops.rms_norm(clean, w, eps=EPS)[7:], ops.rms_norm(x, w, eps=EPS)[7:])
 
 
+@pytest.mark.parametrize("dim", [6, 100, 700, 9000])
+def test_rows_at_the_ends_of_fp32(dim):
+    """Whose 1 / rms no fp32 number holds to its precision, or at all."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    gen = torch.Generator(device="cuda").manual_seed(dim)
+    signs = torch.where(torch.rand(5, dim, generator=gen, device="cuda") < 0.5, -1.0, 1.0)
+    sizes = torch.tensor([3.3e38, 1e38, 1e-38, 1e-41, 2.0], device="cuda")[:, None]
+    x = signs * sizes * (0.5 + 0.5 * torch.rand(5, dim, generator=gen, device="cuda"))
+    w = torch.randn(dim, generator=gen, device="cuda")
+    R.check_norm(ops.rms_norm(x, w, eps=0.0), x, w, 0.0)
+    q, scales = ops.rms_norm_fp8(x, w, eps=0.0, group=32)
+    R.check_fp8(q, scales, x, w, 0.0, 32)
+    dy = torch.randn(5, dim, generator=gen, device="cuda")
+    gx, gw = torch.empty_like(x), torch.empty_like(w)
+    big = torch.tensor([0, 1, 4], device="cuda")  # the others' gradients pass fp32's range
+    ops.rms_norm_grad(x[big], w, dy[big], gx[big], gw, eps=0.0)
+    R.check_grads(None, gw, x[big], w, dy[big], None, 0.0)
+    ops.rms_norm_grad(x, w, dy, None, gw, eps=0.0)
+    R.check_grads(None, gw, x, w, dy, None, 0.0)
+
+
 def test_an_infinite_weight():
     torch = torch_cuda()
     from paper_1904_00962_amd import ops
