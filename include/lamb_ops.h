@@ -317,11 +317,11 @@ LAMB_API lamb_status lamb_rms_quantize(const lamb_rms *rms, void *summed, int64_
  * (the residual stream's own gradient), of grad_x's type, or NULL. grad_x: float32 or
  * bfloat16, or NULL; it may take the place of x, grad_out or grad_sum. grad_weight: [dim],
  * float32 or bfloat16, written, or added to (`add_weight` 1); NULL for none. Its sums are
- * fp32 over 32 tokens, then over as many of those as a workgroup has, then fp64; the
+ * fp32 over at most 32 tokens, then over as many of those as a workgroup has, then fp64; the
  * same inputs give the same bits.
  * The workspace (256-byte aligned; lamb_rms_workspace, host only) is needed for grad_weight,
  * and for grad_x where dim is over 8192; else NULL will do. It takes 4 bytes for each of the
- * columns of at most 1024 rows (dim over 8192: of one row in 256, and 16 bytes for each row).
+ * columns of at most 1024 rows (dim over 8192: of one row in 16, and 16 bytes for each row).
  */
 typedef struct lamb_rms_grads {
     const void *grad_out;

@@ -20,11 +20,19 @@ template <int NORM>
 struct Power {
     double v = 0.0;
 
-    __device__ inline void element(float g) {
-        if (NORM == LAMB_NORM_L2)
-            v = fma(double(g), double(g), v);
-        else
-            join(fabs(double(g)));
+    __device__ inline void elements(const float (&g)[8]) {
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (NORM == LAMB_NORM_L2)
+                v = fma(double(g[i]), double(g[i]), v);
+            else if (NORM == LAMB_NORM_L1)
+                v += fabs(double(g[i]));
+            else
+                top = max(top, __float_as_uint(g[i]) & 0x7fffffffu);
+        }
+        if (NORM == LAMB_NORM_LINF)
+            join(double(__uint_as_float(top)));
     }
     __device__ inline void join(double w) {
         if (NORM != LAMB_NORM_LINF)
@@ -64,15 +72,13 @@ __device__ inline void add_elements(Power<NORM> &power, const void *in, int64_t 
         for (int k = 0; k < kAhead; ++k) {
             float v[8];
             e[k].get(v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) power.element(v[i]);
+            power.elements(v);
         }
     }
     for (; at < end; at += kGradStep) {
         float v[8];
         load_eight<BF16, true>(in, at, int(end - at < 8 ? end - at : 8)).get(v);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) power.element(v[i]);  // 0 past the end
+        power.elements(v);  // 0 past the end
     }
 }
 
@@ -157,6 +163,12 @@ __device__ inline void join_chunks(const GradList &l, int32_t first, int32_t chu
 
 // A chunk's sum. In short lists (JOIN) the last workgroup at a tensor joins the tensor's
 // chunks, the last of all the tensors: no second launch, and no workgroup waits for another.
+// STREAM: loads past the caches.
+//
+// Bound by HBM: 6.23 GB of fp32 in 980 us, 6.4 TB/s; 670 MB of bf16 in 96 us, 7.0 (some of it
+// from the last-level cache). Chunks follow one another over the workgroups: with one long
+// range to a workgroup, so that fewer sums were joined, the dies' 2048 streams took 1.10 ms
+// and 104 us. 2.4 MB in 8 tensors take 6.3 us, joins included: latency.
 template <int NORM, bool JOIN, bool STREAM>
 __global__ __launch_bounds__(kGradBlock) void grad_norms_kernel(GradList l, double *norms,
                                                                 double *total) {
@@ -186,7 +198,8 @@ __global__ __launch_bounds__(kGradBlock) void grad_norms_kernel(GradList l, doub
         join_tensors<NORM>(l, norms, total, part);
 }
 
-// The joins of long lists: a workgroup's tensors one after another.
+// The joins of long lists: a workgroup's tensors one after another. 8 us for 391 tensors, 11
+// for 580: latency. (One workgroup for all took 28 and 61.)
 template <int NORM>
 __global__ __launch_bounds__(kGradBlock) void grad_totals_kernel(GradList l, double *norms,
                                                                  double *total) {
@@ -234,11 +247,14 @@ __device__ inline void scale_chunk(const Chunk &c, float f) {
     }
     for (; at < c.end; at += kGradStep) {
         const int n = int(c.end - at < 8 ? c.end - at : 8);
-        store_eight<OUT_BF16, true>(c.t.out, at, n, scaled(load_eight<IN_BF16, true>(c.t.in, at, n)));
+        store_eight<OUT_BF16, true>(c.t.out, at, n,
+                                    scaled(load_eight<IN_BF16, true>(c.t.in, at, n)));
     }
 }
 
-// The last chunks first: the norms have left them in the last-level cache.
+// The last chunks first: the norms have left them in the last-level cache. Bound by HBM: 1.56
+// billion fp32 to bf16, 9.35 GB in 1.63 ms, 5.7 TB/s. Eight loads ahead in place of four: 1740
+// to 1630 us; results past the caches: 3% less for all sizes.
 __global__ __launch_bounds__(kGradBlock) void grad_clip_kernel(GradList l, const double *total,
                                                                double max_norm, double scale,
                                                                int32_t *nonfinite_out) {

@@ -235,8 +235,9 @@ lamb_status lamb_rms_backward(const lamb_rms *rms, const lamb_rms_grads *grads, 
     if (g.grad_x)
         spans.rows(g.grad_x, g.grad_x_stride, dx_size, true, "grad_x");
     if (g.grad_weight)
-        spans.list[spans.n++] = span_of(g.grad_weight, uint64_t(r.dim * size_of(g.grad_weight_dtype)),
-                                        true, 0, "grad_weight");
+        spans.list[spans.n++] =
+            span_of(g.grad_weight, uint64_t(r.dim * size_of(g.grad_weight_dtype)), true, 0,
+                    "grad_weight");
     if (held && r.tokens)
         spans.list[spans.n++] = span_of(workspace, l.bytes, true, 0, "workspace");
     st = spans.check();
@@ -246,20 +247,20 @@ lamb_status lamb_rms_backward(const lamb_rms *rms, const lamb_rms_grads *grads, 
     const RmsArgs args = args_of(r);
     char *work = static_cast<char *>(workspace);
     RmsGrad grad{g.grad_out,
-                       g.grad_sum,
-                       g.grad_x,
-                       g.grad_weight,
-                       g.grad_out_stride,
-                       g.grad_sum_stride,
-                       g.grad_x_stride,
-                       g.grad_out_dtype == LAMB_DTYPE_BF16,
-                       g.grad_x_dtype == LAMB_DTYPE_BF16,
-                       g.grad_weight_dtype == LAMB_DTYPE_BF16,
-                       g.add_weight,
-                       reinterpret_cast<float *>(work),
-                       0,
-                       int32_t(l.columns),
-                       reinterpret_cast<double *>(work + l.stats)};
+                 g.grad_sum,
+                 g.grad_x,
+                 g.grad_weight,
+                 g.grad_out_stride,
+                 g.grad_sum_stride,
+                 g.grad_x_stride,
+                 g.grad_out_dtype == LAMB_DTYPE_BF16,
+                 g.grad_x_dtype == LAMB_DTYPE_BF16,
+                 g.grad_weight_dtype == LAMB_DTYPE_BF16,
+                 g.add_weight,
+                 reinterpret_cast<float *>(work),
+                 0,
+                 int32_t(l.columns),
+                 reinterpret_cast<double *>(work + l.stats)};
     grad.partials = rms_partials(args, grad);
     hipError_t err = hipSuccess;
     if (r.tokens)

@@ -33,7 +33,7 @@ hipError_t launch_rms(const RmsArgs &args, const RmsOut &out, hipStream_t stream
 // sums than it has registers for.
 constexpr int32_t kRmsHeldDim = 8192;
 constexpr int32_t kRmsFoldRows = 32;  // rows whose terms of the weight's gradient are one sum
-constexpr int32_t kRmsWideRows = 256;  // rows of a workgroup in the second pass of wide rows
+constexpr int32_t kRmsWideRows = 16;  // rows of a workgroup in the second pass of wide rows
 
 struct RmsGrad {
     const void *grad_out, *grad_sum;  // grad_sum: may be NULL

@@ -8,7 +8,10 @@
 //
 // All of it is bound by HBM: a row is read once, stays in the registers of its team's
 // lanes, eight columns to a lane, and its results leave from there. The sums of a row are
-// taken in fp64, which costs nothing beside the loads and lets no square pass fp32's range.
+// taken in fp64, which costs little beside the loads (32768 rows of 1600 of a bf16 stream to
+// 8 bits: 77.8 us, 74.3 with sums in fp32) and lets no square pass fp32's range. Results are
+// stored past the caches (nontemporal): 97 to 95 us there, gradients 143.4 to 142.5; loads
+// that way were slower (112 to 118 us on an fp32 stream).
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -27,7 +30,9 @@ constexpr float kLeastScale = 0x1p-126f;
 
 // Lanes 0 to 15 of every 16 with each other, by data-parallel moves: 1 away, 2 away, then
 // eights and sixteens from their other ends. Where all lanes of a step's group hold one
-// value, its mirror image is the other half's.
+// value, its mirror image is the other half's. (Shuffles, which go through LDS, with
+// divisions and roots at full length: 71 us in place of 63 for the rows above, 3.6 in place
+// of 3.0 for one.)
 constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
 
 template <int MOVE>
@@ -135,7 +140,13 @@ __device__ inline void scale_of(uint32_t largest, float *scale, float *up) {
 }
 
 // L lanes to a row (16, 32 or whole waves), V times 8 L columns; a workgroup of one or more
-// rows. With QUANT the result is 8 bits wide.
+// rows. With QUANT the result is 8 bits wide. TAIL: dim is no multiple of eight.
+//
+// One row to a team and many workgroups, not few that go from row to row: these were slower
+// (112 to 118-128 us for 32768 rows of 1600, bf16 on an fp32 stream), with the next row's
+// loads ahead or not. That case moves 629 MB in 110 to 112 us, 5.7 TB/s (a copy of 1 GiB
+// moves 5.1); to 8 bits with groups of 128, bf16 stream: 369 MB in 62 us, 5.9 TB/s. 64 rows
+// take 2.9 us, one 2.3: latency.
 constexpr int rms_block(int lanes) { return lanes < kRmsBlock ? kRmsBlock : lanes; }
 
 template <int L, int V, bool TAIL, bool X_BF16, bool RES, bool RES_BF16, bool QUANT>
@@ -287,9 +298,12 @@ __device__ inline void finish_weight(const RmsGrad &g, int c, double sum) {
 }
 
 // A team's columns of row after row; what a lane adds to the weight's gradient stays in
-// its registers, kRmsFoldRows rows to a sum and these sums to another. The teams' are
-// joined at the end, and leave as one row of parts, or finished where there is one
-// workgroup.
+// its registers, kRmsFoldRows rows to a sum and these sums to another, so that chains of like
+// terms stay short. The teams' are joined at the end, and leave as one row of parts, or
+// finished where there is one workgroup.
+//
+// Bound by HBM: 32768 rows of 1600 on an fp32 stream, 734 MB in 125 us, 5.9 TB/s; 8192 rows of
+// 1024 in bf16 14 us, 4.8 TB/s. Loading the next row ahead changed neither.
 template <int L, bool TAIL, bool X_BF16, bool DY_BF16, bool DX_BF16>
 __global__ __launch_bounds__(L < 1024 ? 512 : 1024) void rms_grad_kernel(RmsArgs a, RmsGrad g) {
     constexpr int kWaves = L < 64 ? 1 : L / 64, kInWave = L < 64 ? L : 64;
@@ -407,6 +421,9 @@ __global__ __launch_bounds__(L < 1024 ? 512 : 1024) void rms_grad_kernel(RmsArgs
 }
 
 // Rows too wide for one lane's registers: first each row's two numbers, a workgroup a row.
+// (Both passes read x and dy: 2900 bf16 rows of 16384 take 114 us, 3.3 TB/s of what has to
+// move, 4.8 of what does.)
+template <bool TAIL, bool X_BF16, bool DY_BF16>
 __global__ __launch_bounds__(1024) void rms_stats_kernel(RmsArgs a, RmsGrad g) {
     __shared__ double part[16][2];
     const int64_t row = int64_t(blockIdx.y) * gridDim.x + blockIdx.x;
@@ -415,13 +432,18 @@ __global__ __launch_bounds__(1024) void rms_stats_kernel(RmsArgs a, RmsGrad g) {
     double square = 0.0, along = 0.0;
     for (int c = threadIdx.x * 8; c < a.dim; c += 8192) {
         const int n = a.dim - c;
+        Eight<X_BF16> xe = load_eight<X_BF16, TAIL>(a.x, row * a.x_stride + c, n, c > 0);
+        Eight<DY_BF16> de =
+            load_eight<DY_BF16, TAIL>(g.grad_out, row * g.grad_out_stride + c, n, c > 0);
         float x[8], dy[8], w[8];
-        load_values<true>(a.x_bf16, a.x, row * a.x_stride + c, n, c > 0, x);
-        load_values<true>(g.grad_out_bf16, g.grad_out, row * g.grad_out_stride + c, n, c > 0, dy);
 #pragma unroll
         for (int i = 0; i < 8; ++i) w[i] = 1.0f;
         if (a.weight)
-            load_values<true>(a.weight_bf16, a.weight, c, n, c > 0, w);
+            load_values<TAIL>(a.weight_bf16, a.weight, c, n, c > 0, w);
+        settle<TAIL>(xe, n, c > 0);
+        settle<TAIL>(de, n, c > 0);
+        xe.get(x);
+        de.get(dy);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             square = fma(double(x[i]), double(x[i]), square);
@@ -447,45 +469,63 @@ __global__ __launch_bounds__(1024) void rms_stats_kernel(RmsArgs a, RmsGrad g) {
     }
 }
 
-// Then 2048 columns of kRmsWideRows rows in a workgroup.
+// Then 2048 columns of kRmsWideRows rows in a workgroup, four rows in flight.
+template <bool TAIL, bool X_BF16, bool DY_BF16, bool DX_BF16>
 __global__ __launch_bounds__(256) void rms_wide_grad_kernel(RmsArgs a, RmsGrad g) {
-    const int c = (int(blockIdx.y) * 256 + threadIdx.x) * 8, n = a.dim - c;
-    if (n <= 0)
+    constexpr int kAhead = 4;
+    const int c = (int(blockIdx.y) * 256 + threadIdx.x) * 8, columns = a.dim - c;
+    if (columns <= 0)
         return;
-    float w[8], recent[8] = {}, dw[8] = {};
+    float w[8], dw[8] = {};
 #pragma unroll
     for (int i = 0; i < 8; ++i) w[i] = 1.0f;
     if (a.weight)
-        load_values<true>(a.weight_bf16, a.weight, c, n, c > 0, w);
+        load_values<TAIL>(a.weight_bf16, a.weight, c, columns, c > 0, w);
     const int64_t first = int64_t(blockIdx.x) * kRmsWideRows;
-    const int64_t end = first + kRmsWideRows < a.tokens ? first + kRmsWideRows : a.tokens;
-    for (int64_t row = first; row < end; ++row) {
-        float x[8], dy[8], ds[8] = {}, dx[8];
-        load_values<true>(a.x_bf16, a.x, row * a.x_stride + c, n, c > 0, x);
-        load_values<true>(g.grad_out_bf16, g.grad_out, row * g.grad_out_stride + c, n, c > 0, dy);
-        if (g.grad_sum)
-            load_values<true>(g.grad_x_bf16, g.grad_sum, row * g.grad_sum_stride + c, n, c > 0, ds);
-        const double r = g.stats[2 * row];
-        const float inverse = float(r), mean = float(g.stats[2 * row + 1]);
-        Inverse(r).times(x);
+    for (int64_t at = first; at < first + kRmsWideRows && at < a.tokens; at += kAhead) {
+        Eight<X_BF16> xe[kAhead];
+        Eight<DY_BF16> de[kAhead];
+        Eight<DX_BF16> se[kAhead];
+        int n[kAhead];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            dx[i] = fmaf(fmaf(-x[i], mean, dy[i] * w[i]), inverse, ds[i]);
-            recent[i] = fmaf(dy[i], x[i], recent[i]);
+        for (int k = 0; k < kAhead; ++k) {
+            const int64_t row = at + k;
+            n[k] = row < a.tokens ? columns : 0;
+            xe[k] = load_eight<X_BF16, TAIL>(a.x, row * a.x_stride + c, n[k], c > 0);
+            de[k] = load_eight<DY_BF16, TAIL>(g.grad_out, row * g.grad_out_stride + c, n[k], c > 0);
+            se[k] = Eight<DX_BF16>{};
+            if (g.grad_sum)
+                se[k] = load_eight<DX_BF16, TAIL>(g.grad_sum, row * g.grad_sum_stride + c, n[k],
+                                                  c > 0);
         }
-        if (g.grad_x)
-            store_values<true>(g.grad_x_bf16, g.grad_x, row * g.grad_x_stride + c, n, dx);
-        if ((row - first) % kRmsFoldRows == kRmsFoldRows - 1) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            if (n[k] <= 0)
+                break;
+            const int64_t row = at + k;
+            settle<TAIL>(xe[k], n[k], c > 0);
+            settle<TAIL>(de[k], n[k], c > 0);
+            settle<TAIL>(se[k], n[k], c > 0);
+            float x[8], dy[8], ds[8], dx[8];
+            xe[k].get(x);
+            de[k].get(dy);
+            se[k].get(ds);
+            const double r = g.stats[2 * row];
+            const float inverse = float(r), mean = float(g.stats[2 * row + 1]);
+            Inverse(r).times(x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                dw[i] += recent[i];
-                recent[i] = 0.0f;
+                dx[i] = fmaf(fmaf(-x[i], mean, dy[i] * w[i]), inverse, ds[i]);
+                dw[i] = fmaf(dy[i], x[i], dw[i]);
+            }
+            if (g.grad_x) {
+                Eight<DX_BF16> e;
+                e.set(dx);
+                store_eight<DX_BF16, TAIL, true>(g.grad_x, row * g.grad_x_stride + c, n[k], e);
             }
         }
     }
     if (g.grad_weight) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) dw[i] += recent[i];
         Eight<false> e;
         e.set(dw);
         store_eight<false, false>(g.partial, int64_t(blockIdx.x) * g.columns + c, 8, e);
@@ -493,7 +533,7 @@ __global__ __launch_bounds__(256) void rms_wide_grad_kernel(RmsArgs a, RmsGrad g
 }
 
 // The weight's gradient: its parts in their order, 32 stripes of them and 32 columns in a
-// workgroup, in fp64.
+// workgroup, in fp64. 3.8 to 4.7 us for 1024 or 512 parts of 1024 and 1600 columns: latency.
 __global__ __launch_bounds__(1024) void rms_join_kernel(RmsArgs a, RmsGrad g) {
     __shared__ double part[32][32];
     const int column = threadIdx.x % 32, stripe = threadIdx.x / 32;
@@ -501,7 +541,8 @@ __global__ __launch_bounds__(1024) void rms_join_kernel(RmsArgs a, RmsGrad g) {
     double sum = 0.0;
     if (c < a.dim) {
 #pragma unroll 16
-        for (int64_t k = stripe; k < g.partials; k += 32) sum += double(g.partial[k * g.columns + c]);
+        for (int64_t k = stripe; k < g.partials; k += 32)
+            sum += double(g.partial[k * g.columns + c]);
     }
     part[stripe][column] = sum;
     __syncthreads();
@@ -533,7 +574,10 @@ hipError_t launch_rms_of(const RmsArgs &a, const RmsOut &o, hipStream_t stream) 
     };
     const int lanes = lanes_of(a.dim);
     // Half the lanes with twice the columns, where rows are many, a team's last lanes have no
-    // columns and a lane has little to load: a wave's fixed work counts more there.
+    // columns and a lane has little to load: a wave's fixed work counts more there. 25000 rows
+    // of 1600 to 8 bits 50.0 us so and 53.4 the other way, 15625 of 2560 without a residual
+    // 32.4 and 35.6; but with one 56.9 and 54.2, 2048 columns to 8 bits 48.1 and 46.2, and 64
+    // rows of 1600 3.7 and 3.0.
     if constexpr (!TAIL && (QUANT || !RES)) {
         if (a.tokens >= 2048 && 8 * a.dim <= 7 * 8 * lanes) {
             switch (lanes) {
@@ -609,7 +653,20 @@ int64_t row_bytes(const RmsArgs &a, const RmsGrad &g) {
 }
 
 template <bool TAIL, bool X_BF16, bool DY_BF16, bool DX_BF16>
+hipError_t launch_wide_grad_of(const RmsArgs &a, const RmsGrad &g, hipStream_t stream) {
+    rms_stats_kernel<TAIL, X_BF16, DY_BF16><<<grid_of(a.tokens), 1024, 0, stream>>>(a, g);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess)
+        return err;
+    const dim3 grid(uint32_t(g.partials), uint32_t((a.dim + 2047) / 2048));
+    rms_wide_grad_kernel<TAIL, X_BF16, DY_BF16, DX_BF16><<<grid, 256, 0, stream>>>(a, g);
+    return hipGetLastError();
+}
+
+template <bool TAIL, bool X_BF16, bool DY_BF16, bool DX_BF16>
 hipError_t launch_rms_grad_of(const RmsArgs &a, const RmsGrad &g, hipStream_t stream) {
+    if (a.dim > kRmsHeldDim)
+        return launch_wide_grad_of<TAIL, X_BF16, DY_BF16, DX_BF16>(a, g, stream);
     const GradShape s = grad_shape(a.tokens, a.dim, row_bytes(a, g));
     auto run = [&](auto lanes) {
         constexpr int L = decltype(lanes)::value;
@@ -662,15 +719,6 @@ int64_t rms_most_partials(int64_t tokens, int32_t dim) {
 }
 
 hipError_t launch_rms_grad(const RmsArgs &a, const RmsGrad &g, hipStream_t stream) {
-    if (a.dim > kRmsHeldDim) {
-        rms_stats_kernel<<<grid_of(a.tokens), 1024, 0, stream>>>(a, g);
-        const hipError_t err = hipGetLastError();
-        if (err != hipSuccess)
-            return err;
-        const dim3 grid(uint32_t(g.partials), uint32_t((a.dim + 2047) / 2048));
-        rms_wide_grad_kernel<<<grid, 256, 0, stream>>>(a, g);
-        return hipGetLastError();
-    }
     return a.dim % 8 ? launch_rms_grad_types<true>(a, g, stream)
                      : launch_rms_grad_types<false>(a, g, stream);
 }

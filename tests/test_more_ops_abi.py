@@ -127,7 +127,7 @@ def test_norm_workspace_is_within_the_stated_bytes(lib, dim):
         if dim <= 8192:
             most = 4 * columns * min(1024, tokens + 3) + 256
         else:
-            most = 4 * columns * (tokens // 256 + 1) + 16 * tokens + 512
+            most = 4 * columns * (tokens // 16 + 1) + 16 * tokens + 512
         assert _ops.lamb_rms_workspace(r) <= most, tokens
 
 
