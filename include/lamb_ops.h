@@ -3,8 +3,9 @@
  * Instinct MI355X (gfx950): Newton-Schulz orthogonalization and the Muon step
  * for a model's matrices, softmax cross entropy against a vocabulary table with
  * its gradients, a token table's lookup with its gradient, the root-mean-square
- * norm of rows with the residual's addition, its gradients and its result in 8 bits, and
- * the norm of all gradients with clipping by it. Same library, status codes and conventions as lamb_mi355x.h: pointers are device pointers
+ * norm of rows with the residual's addition, its gradients and its result in 8
+ * bits, and the norm of all gradients with clipping by it. Same library, status
+ * codes and conventions as lamb_mi355x.h: pointers are device pointers
  * unless marked host; the caller owns every tensor; arguments are validated on
  * the host before any HIP call; work is enqueued on `stream` and nothing is
  * synchronised, allocated or copied to the host (plan creation and destruction
@@ -369,8 +370,8 @@ LAMB_API lamb_status lamb_grad_norm(lamb_grad_plan *plan, double *norms, double 
                                     void *stream);
 
 /*
- * Clipping by the norm: out = f in, f = scale min(1, max_norm / (|scale| total)): the scaled gradients have at most
- * the norm max_norm. total: device double, from lamb_grad_norm or from a sum over workers.
+ * Clipping by the norm: out = f in, f = scale min(1, max_norm / (|scale| total)): the
+ * scaled gradients have at most the norm max_norm. total: device double, from lamb_grad_norm or from a sum over workers.
  * A total that is not finite limits nothing (f = scale), so that the NaN or the infinity
  * stays to be seen; nonfinite_out (device int32, may be NULL) receives 1 then, else 0. In
  * place nothing is written where f is 1. max_norm >= 0 (infinity: no limit), scale finite;

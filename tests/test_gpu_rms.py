@@ -13,9 +13,16 @@ pytestmark = pytest.mark.gpu
 EPS = 1e-6
 DIMS = [1, 2, 7, 8, 9, 63, 64, 65, 250, 511, 512, 513, 1000, 1024, 1025, 1600, 2048, 2049, 4096,
         4097, 8192, 8193, 16384, 16385, 40000, 65536]
-FORWARD = [("bfloat16", None, "bfloat16", "bfloat16"), ("bfloat16", "bfloat16", "bfloat16", "bfloat16"),
+FORWARD = [("bfloat16", None, "bfloat16", "bfloat16"),
+           ("bfloat16", "bfloat16", "bfloat16", "bfloat16"),
            ("bfloat16", "float32", "float32", "bfloat16"), ("float32", "float32", None, "float32"),
            ("float32", None, "float32", "bfloat16"), ("bfloat16", None, None, "float32")]
+
+TYPES = {"f": "float32", "h": "bfloat16", "-": None}
+# rows, and the types of x, the result's gradient, the stream's and x's, the weight, and its
+# gradient
+GRADIENTS = [(1, *"fffff"), (7, *"hhhff"), (70, *"fhfhh"), (5, *"hff-f"), (33, *"ffhff"),
+             (3, *"hhfff"), (2, *"hfh--"), (9, *"fhhf-")]
 
 
 def _t(torch, name):
@@ -79,14 +86,8 @@ def test_fp8(dim):
 def test_gradients(dim):
     torch = torch_cuda()
     from paper_1904_00962_amd import ops
-    for tokens, xt, yt, gt, wt, dwt in ((1, "float32", "float32", "float32", "float32", "float32"),
-                                        (7, "bfloat16", "bfloat16", "bfloat16", "float32", "float32"),
-                                        (70, "float32", "bfloat16", "float32", "bfloat16", "bfloat16"),
-                                        (5, "bfloat16", "float32", "float32", None, "float32"),
-                                        (33, "float32", "float32", "bfloat16", "float32", "float32"),
-                                        (3, "bfloat16", "bfloat16", "float32", "float32", "float32"),
-                                        (2, "bfloat16", "float32", "bfloat16", None, None),
-                                        (9, "float32", "bfloat16", "bfloat16", "float32", None)):
+    for tokens, xt, yt, gt, wt, dwt in GRADIENTS:
+        xt, yt, gt, wt, dwt = (TYPES[k] for k in (xt, yt, gt, wt, dwt))
         x, _, w, gen = _case(torch, tokens, dim, xt, None, wt)
         dy = _rows(torch, gen, tokens, dim, _t(torch, yt), 1e-3)
         for ds in (None, _rows(torch, gen, tokens, dim, _t(torch, gt), 1e-3)):
@@ -137,7 +138,8 @@ def test_gradient_against_differences():
     gen = torch.Generator(device="cuda").manual_seed(5)
     for tokens, dim in ((1, 3), (6, 200), (4, 1500)):
         rand = lambda *s: torch.randn(*s, generator=gen, device="cuda")  # noqa: E731
-        x, w, c, d, dw = rand(tokens, dim), rand(dim), rand(tokens, dim), rand(tokens, dim), rand(dim)
+        x, c, d = rand(tokens, dim), rand(tokens, dim), rand(tokens, dim)
+        w, dw = rand(dim), rand(dim)
         value = lambda t: float((c.double() * R.norm(  # noqa: E731
             x.double() + t * d.double(), w.double() + t * dw.double(), EPS)[0]).sum())
         slope = (value(1e-4) - value(-1e-4)) / 2e-4
@@ -386,7 +388,8 @@ def test_refusals():
             call()
     for call in (lambda: ops.rms_norm(x.cpu()), lambda: ops.rms_norm(x, w.cpu()),
                  lambda: ops.rms_norm(x[0]), lambda: ops.rms_norm(x.t()),
-                 lambda: ops.rms_norm(x, w[:8]), lambda: ops.rms_norm(x, torch.ones(32, device="cuda")[::2]),
+                 lambda: ops.rms_norm(x, w[:8]),
+                 lambda: ops.rms_norm(x, torch.ones(32, device="cuda")[::2]),
                  lambda: ops.rms_norm(x, residual=x[:3]), lambda: ops.rms_norm(x, summed=x.clone()),
                  lambda: ops.rms_norm(x, out=x[:3]),
                  lambda: ops.rms_norm_fp8(x, scales=torch.zeros(4, 2, device="cuda")),

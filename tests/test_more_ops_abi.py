@@ -136,7 +136,8 @@ def _tensor(base=A, out=None, numel=100, types=(F32, F32)):
 
 
 @pytest.mark.parametrize("rows,norm,status", [
-    ([], 0, _lib.LAMB_EINVAL), ([_tensor()], 3, _lib.LAMB_EINVAL), ([_tensor()], -1, _lib.LAMB_EINVAL),
+    ([], 0, _lib.LAMB_EINVAL), ([_tensor()], 3, _lib.LAMB_EINVAL),
+    ([_tensor()], -1, _lib.LAMB_EINVAL),
     ([_tensor(numel=-1)], 0, _lib.LAMB_EINVAL),
     ([_tensor(numel=(1 << 40) + 1)], 0, _lib.LAMB_EINVAL),
     ([_tensor(types=(2, 0))], 0, _lib.LAMB_EINVAL), ([_tensor(types=(0, 3))], 0, _lib.LAMB_EINVAL),
