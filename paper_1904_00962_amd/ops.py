@@ -27,12 +27,19 @@ COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 _torch_module = None
 _FLOAT_CODES = {}
 _ID_CODES = {}
+# what a call asks torch for each time: the current device's index, and a stream's raw handle
+_current_device = _raw_stream = None
 
 
 def _torch():
-    global _torch_module
+    global _torch_module, _current_device, _raw_stream
     if _torch_module is None:
         import torch
+        # without torch's look whether CUDA is there (a tensor lies on a device), and without a
+        # Stream object, which costs 4 us a call; where torch has them
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
+                              lambda index: torch.cuda.current_stream(index).cuda_stream)
         _FLOAT_CODES.update({torch.float32: _ops.LAMB_DTYPE_F32,
                              torch.bfloat16: _ops.LAMB_DTYPE_BF16})
         _ID_CODES.update({torch.int32: _ops.LAMB_DTYPE_I32, torch.int64: _ops.LAMB_DTYPE_I64})
@@ -41,12 +48,8 @@ def _torch():
 
 
 def _stream(device) -> int:
-    torch = _torch()
-    # the raw handle by itself, where torch has it: a Stream object costs 4 us a call
-    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
-    if raw is not None:
-        return raw(device.index)
-    return torch.cuda.current_stream(device).cuda_stream
+    _torch()
+    return _raw_stream(device.index)
 
 
 class _NoSwitch:
@@ -62,8 +65,8 @@ _NO_SWITCH = _NoSwitch()
 
 def _on(device):
     """A context on ``device``; nothing where it is current already."""
-    cuda = _torch().cuda
-    return _NO_SWITCH if cuda.current_device() == device.index else cuda.device(device)
+    torch = _torch()
+    return _NO_SWITCH if _current_device() == device.index else torch.cuda.device(device)
 
 
 def _float_code(dtype) -> int:
@@ -335,21 +338,29 @@ def embedding_grad(ids, grad_out, grad_table, *, scale: float = 1.0,
 
 def _rms(x, weight, residual, eps):
     """The C struct."""
-    device = x.device
-    stride = _rows("x", x, x.dtype)
-    tokens, dim = x.shape
-    at = w_at = 0
-    r_stride = code = w_code = 0
+    device, shape, dtype = x.device, x.shape, x.dtype
+    stride = _like("x", x, shape, device)
+    code = _float_code(dtype)
+    at = w_at = None
+    r_stride = r_code = w_code = 0
     if residual is not None:
-        r_stride = _rows("residual", residual, residual.dtype, device)
-        code = _float_code(residual.dtype)
-        if residual.shape != x.shape:
-            raise ValueError("residual must have x's shape")
-        at = residual.data_ptr()
+        r_stride = _like("residual", residual, shape, device)
+        r_code = _float_code(residual.dtype)
+        at = residual.data_ptr() or None
     if weight is not None:
-        w_at, w_code = _row("weight", weight, dim, device), _float_code(weight.dtype)
-    return _ops.lamb_rms(x.data_ptr() or None, at or None, w_at or None, stride, r_stride, tokens,
-                         dim, _float_code(x.dtype), code, w_code, eps)
+        w_at, w_code = _row("weight", weight, shape[1], device), _float_code(weight.dtype)
+    return _ops.lamb_rms(x.data_ptr() or None, at, w_at, stride, r_stride, *shape, code, r_code,
+                         w_code, eps)
+
+
+def _like(name, t, shape, device):
+    """The row stride of a 2-D tensor of x's shape."""
+    if t.shape != shape:
+        raise ValueError("%s must have x's shape" % name)
+    # most are contiguous: nothing else to look at
+    if len(shape) == 2 and t.is_contiguous() and t.is_cuda and t.device == device:
+        return shape[1]
+    return _rows(name, t, t.dtype, device)
 
 
 def _row(name, t, dim, device):
@@ -368,9 +379,9 @@ def _result(name, t, like, dtype):
         torch = _torch_module
         return (torch.empty_like(like, dtype=dtype, memory_format=torch.contiguous_format),
                 like.shape[1])
-    if t.shape != like.shape:
-        raise ValueError("%s must have x's shape" % name)
-    return t, _rows(name, t, dtype, like.device)
+    if t.dtype is not dtype:
+        raise TypeError("%s must be %s, got %s" % (name, dtype, t.dtype))
+    return t, _like(name, t, like.shape, like.device)
 
 
 def rms_norm(x, weight=None, *, residual=None, eps: float = 1e-6, out_dtype=None, out=None,
@@ -447,11 +458,9 @@ def rms_norm_grad(x, weight, grad_out, grad_x=None, grad_weight=None, *, eps: fl
     _torch()
     r, device = _rms(x, weight, None, eps), x.device
     g = _ops.lamb_rms_grads(add_weight=int(bool(accumulate)))
-    g.grad_out_stride = _rows("grad_out", grad_out, grad_out.dtype, device)
+    g.grad_out_stride = _like("grad_out", grad_out, x.shape, device)
     g.grad_out_dtype = _float_code(grad_out.dtype)
     g.grad_out = grad_out.data_ptr() or None
-    if grad_out.shape != x.shape:
-        raise ValueError("grad_out must have x's shape")
     if grad_x is not None:
         g.grad_x_dtype = _float_code(grad_x.dtype)
         _, g.grad_x_stride = _result("grad_x", grad_x, x, grad_x.dtype)
