@@ -31,7 +31,8 @@ struct GradList {
 };
 
 constexpr int kGradBlock = 256;
-constexpr int kGradStep = kGradBlock * 8;  // elements that a workgroup loads at once
+constexpr int kGradStep = kGradBlock * 8;  // elements that a chunk is a multiple of
+constexpr int kGradTurn = 8 * kGradStep;   // those that a workgroup has in flight
 
 // Lists of up to this many chunks are joined by the launch that sums them: 10 to 11 us for
 // the norm of 0.1M to 4M elements, where two launches take 13 (the second costs the host

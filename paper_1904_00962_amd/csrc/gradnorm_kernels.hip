@@ -6,6 +6,8 @@
 #include <hip/hip_runtime.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "gradnorm_internal.h"
 #include "ops_host.h"
 #include "row_io.h"
@@ -20,10 +22,11 @@ template <int NORM>
 struct Power {
     double v = 0.0;
 
-    __device__ inline void elements(const float (&g)[8]) {
+    template <int N>
+    __device__ inline void elements(const float (&g)[N]) {
         uint32_t top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < N; ++i) {
             if (NORM == LAMB_NORM_L2)
                 v = fma(double(g[i]), double(g[i]), v);
             else if (NORM == LAMB_NORM_L1)
@@ -56,29 +59,72 @@ __device__ inline void join_block(Power<NORM> &power, double *shared) {
         for (int w = 1; w < kGradBlock / 64; ++w) power.join(shared[w]);
 }
 
-constexpr int kAhead = 8;  // times eight elements a thread has in flight: a whole chunk
+// A lane's 16 bytes of a gradient tensor, which follow one another over the lanes.
+template <bool BF16>
+struct Part {
+    static constexpr int kElements = BF16 ? 8 : 4;
+    Bytes16 u;
 
-// Adds the elements from `first` to `end`.
+    __device__ inline void get(float (&v)[kElements]) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (BF16) {
+                v[2 * i] = bf16_low(u[i]);
+                v[2 * i + 1] = bf16_high(u[i]);
+            } else {
+                v[i] = __uint_as_float(u[i]);
+            }
+        }
+    }
+};
+
+template <bool BF16, bool STREAM>
+__device__ inline Part<BF16> load_part(const void *base, int64_t at) {
+    using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
+    return Part<BF16>{load_16<STREAM>((const Global<T> *)base + at)};
+}
+
+// The first n elements of one; 0 past them.
+template <bool BF16>
+__device__ inline Part<BF16> load_some(const void *base, int64_t at, int n) {
+    using T = typename std::conditional<BF16, uint16_t, uint32_t>::type;
+    const Global<T> *p = (const Global<T> *)base + at;
+    Part<BF16> e = {};
+#pragma unroll
+    for (int i = 0; i < Part<BF16>::kElements; ++i)
+        if (i < n)
+            e.u[BF16 ? i / 2 : i] |= uint32_t(p[i]) << (BF16 ? i % 2 * 16 : 0);
+    return e;
+}
+
+// Adds the elements from `first` to `end`: a whole chunk's, or half of one's, in flight at
+// once (short lists have chunks of half the length and more).
 template <int NORM, bool BF16, bool STREAM>
 __device__ inline void add_elements(Power<NORM> &power, const void *in, int64_t first,
                                     int64_t end) {
-    int64_t at = first + threadIdx.x * 8;
-    for (; at + (kAhead - 1) * kGradStep + 8 <= end; at += kAhead * kGradStep) {
-        Eight<BF16> e[kAhead];
+    constexpr int kEach = Part<BF16>::kElements, kAcross = kGradBlock * kEach;
+    float v[kEach];
+    int64_t at = first + threadIdx.x * kEach;
+    auto turns = [&](auto size) {
+        constexpr int kTurn = decltype(size)::value, kParts = kTurn / kAcross;
+        for (; first + kTurn <= end; first += kTurn, at += kTurn) {
+            Part<BF16> e[kParts];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            e[k] = load_eight<BF16, false, STREAM>(in, at + k * kGradStep, 8);
+            for (int k = 0; k < kParts; ++k) e[k] = load_part<BF16, STREAM>(in, at + k * kAcross);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            float v[8];
-            e[k].get(v);
-            power.elements(v);
+            for (int k = 0; k < kParts; ++k) {
+                e[k].get(v);
+                power.elements(v);
+            }
         }
-    }
-    for (; at < end; at += kGradStep) {
-        float v[8];
-        load_eight<BF16, true>(in, at, int(end - at < 8 ? end - at : 8)).get(v);
-        power.elements(v);  // 0 past the end
+    };
+    turns(std::integral_constant<int, kGradTurn>{});
+    turns(std::integral_constant<int, kGradTurn / 2>{});
+    turns(std::integral_constant<int, kGradTurn / 8>{});
+    for (; at < end; at += kAcross) {
+        const int64_t n = end - at;
+        (n < kEach ? load_some<BF16>(in, at, int(n)) : load_part<BF16, false>(in, at)).get(v);
+        power.elements(v);
     }
 }
 
@@ -165,8 +211,8 @@ __device__ inline void join_chunks(const GradList &l, int32_t first, int32_t chu
 // chunks, the last of all the tensors: no second launch, and no workgroup waits for another.
 // STREAM: loads past the caches.
 //
-// Bound by HBM: 6.23 GB of fp32 in 980 us, 6.4 TB/s; 670 MB of bf16 in 96 us, 7.0 (some of it
-// from the last-level cache). Chunks follow one another over the workgroups: with one long
+// Bound by HBM: 6.23 GB of fp32 in 930 us, 6.7 TB/s (980 with eight elements a lane); 670 MB of bf16 in 96 to 98 us, 6.9 (some of
+// it from the last-level cache). Chunks follow one another over the workgroups: with one long
 // range to a workgroup, so that fewer sums were joined, the dies' 2048 streams took 1.10 ms
 // and 104 us. 2.4 MB in 8 tensors take 6.3 us, joins included: latency.
 template <int NORM, bool JOIN, bool STREAM>
@@ -224,6 +270,8 @@ __global__ __launch_bounds__(kGradBlock) void grad_zeros_kernel(int32_t n, doubl
         for (int i = threadIdx.x; i < n; i += kGradBlock) norms[i] = 0.0;
 }
 
+// Eight elements a lane, whatever the types: with 16 bytes of fp32 a lane, as the norms have
+// it, their four bf16 results took 1750 us in place of 1630 for the case below.
 template <bool IN_BF16, bool OUT_BF16>
 __device__ inline void scale_chunk(const Chunk &c, float f) {
     auto scaled = [&](const Eight<IN_BF16> &e) {
@@ -235,16 +283,21 @@ __device__ inline void scale_chunk(const Chunk &c, float f) {
         to.set(v);
         return to;
     };
-    int64_t at = c.first + threadIdx.x * 8;
-    for (; at + (kAhead - 1) * kGradStep + 8 <= c.end; at += kAhead * kGradStep) {
-        Eight<IN_BF16> e[kAhead];
+    int64_t first = c.first, at = first + threadIdx.x * 8;
+    auto turns = [&](auto size) {
+        constexpr int kTurn = decltype(size)::value, kParts = kTurn / kGradStep;
+        for (; first + kTurn <= c.end; first += kTurn, at += kTurn) {
+            Eight<IN_BF16> e[kParts];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            e[k] = load_eight<IN_BF16, false>(c.t.in, at + k * kGradStep, 8);
+            for (int k = 0; k < kParts; ++k)
+                e[k] = load_eight<IN_BF16, false>(c.t.in, at + k * kGradStep, 8);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            store_eight<OUT_BF16, false, true>(c.t.out, at + k * kGradStep, 8, scaled(e[k]));
-    }
+            for (int k = 0; k < kParts; ++k)
+                store_eight<OUT_BF16, false, true>(c.t.out, at + k * kGradStep, 8, scaled(e[k]));
+        }
+    };
+    turns(std::integral_constant<int, kGradTurn>{});
+    turns(std::integral_constant<int, kGradTurn / 2>{});
     for (; at < c.end; at += kGradStep) {
         const int n = int(c.end - at < 8 ? c.end - at : 8);
         store_eight<OUT_BF16, true>(c.t.out, at, n,
