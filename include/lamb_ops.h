@@ -371,7 +371,8 @@ LAMB_API lamb_status lamb_grad_norm(lamb_grad_plan *plan, double *norms, double 
 
 /*
  * Clipping by the norm: out = f in, f = scale min(1, max_norm / (|scale| total)): the
- * scaled gradients have at most the norm max_norm. total: device double, from lamb_grad_norm or from a sum over workers.
+ * scaled gradients have at most the norm max_norm. total: device double, from
+ * lamb_grad_norm or from a sum over workers.
  * A total that is not finite limits nothing (f = scale), so that the NaN or the infinity
  * stays to be seen; nonfinite_out (device int32, may be NULL) receives 1 then, else 0. In
  * place nothing is written where f is 1. max_norm >= 0 (infinity: no limit), scale finite;

@@ -211,10 +211,11 @@ __device__ inline void join_chunks(const GradList &l, int32_t first, int32_t chu
 // chunks, the last of all the tensors: no second launch, and no workgroup waits for another.
 // STREAM: loads past the caches.
 //
-// Bound by HBM: 6.23 GB of fp32 in 930 us, 6.7 TB/s (980 with eight elements a lane); 670 MB of bf16 in 96 to 98 us, 6.9 (some of
-// it from the last-level cache). Chunks follow one another over the workgroups: with one long
-// range to a workgroup, so that fewer sums were joined, the dies' 2048 streams took 1.10 ms
-// and 104 us. 2.4 MB in 8 tensors take 6.3 us, joins included: latency.
+// Bound by HBM: 6.23 GB of fp32 in 930 us, 6.7 TB/s (980 with eight elements a lane); 670 MB
+// of bf16 in 96 to 98 us, 6.9 (some of it from the last-level cache). Chunks follow one
+// another over the workgroups: with one long range to a workgroup, so that fewer sums were
+// joined, the dies' 2048 streams took 1.10 ms and 104 us. 2.4 MB in 8 tensors take 6.3 us,
+// joins included: latency.
 template <int NORM, bool JOIN, bool STREAM>
 __global__ __launch_bounds__(kGradBlock) void grad_norms_kernel(GradList l, double *norms,
                                                                 double *total) {

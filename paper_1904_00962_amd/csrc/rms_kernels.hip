@@ -92,7 +92,7 @@ __device__ inline uint32_t lanes_max(uint32_t v) {
     return max(a, b);
 }
 
-// 1 / sqrt(v) to 2^-45 or so: the hardware's estimate (2^-22) and a Newton step, which
+// 1 / sqrt(v) to 2^-43: the hardware's estimate (2^-22) and a Newton step, which
 // makes NaN of 0 and infinity, where the estimate is right.
 __device__ inline double inverse_root(double v) {
     const double y = __builtin_amdgcn_rsq(v);
