@@ -121,6 +121,10 @@ struct Inverse {
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[i] *= value;
     }
+    // v r + add; no branch here, which would hold more registers
+    __device__ inline float times_add(float v, float add) const {
+        return fmaf(v * shift, value, add);
+    }
 };
 
 // max(largest / 448, 2^-126) of the bits of a magnitude, and its inverse, both as if
@@ -369,14 +373,15 @@ __global__ __launch_bounds__(L < 1024 ? 512 : 1024) void rms_grad_kernel(RmsArgs
             }
         }
         const double r = inverse_root(fma(square, a.per_column, double(a.eps)));
-        const float inverse = float(r), mean = float(along * r * a.per_column);
+        const Inverse inverse(r);
+        const float mean = float(along * r * a.per_column);
         float ds[8], dx[8];
         now.ds.get(ds);
         if (n > 0) {
-            Inverse(r).times(x);
+            inverse.times(x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                dx[i] = fmaf(fmaf(-x[i], mean, gw[i]), inverse, ds[i]);
+                dx[i] = inverse.times_add(fmaf(-x[i], mean, gw[i]), ds[i]);
                 recent[i] = fmaf(dy[i], x[i], recent[i]);
             }
             if (g.grad_x) {
@@ -510,12 +515,12 @@ __global__ __launch_bounds__(256) void rms_wide_grad_kernel(RmsArgs a, RmsGrad g
             xe[k].get(x);
             de[k].get(dy);
             se[k].get(ds);
-            const double r = g.stats[2 * row];
-            const float inverse = float(r), mean = float(g.stats[2 * row + 1]);
-            Inverse(r).times(x);
+            const Inverse inverse(g.stats[2 * row]);
+            const float mean = float(g.stats[2 * row + 1]);
+            inverse.times(x);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                dx[i] = fmaf(fmaf(-x[i], mean, dy[i] * w[i]), inverse, ds[i]);
+                dx[i] = inverse.times_add(fmaf(-x[i], mean, dy[i] * w[i]), ds[i]);
                 dw[i] = fmaf(dy[i], x[i], dw[i]);
             }
             if (g.grad_x) {
