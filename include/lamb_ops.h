@@ -376,7 +376,8 @@ LAMB_API lamb_status lamb_grad_norm(lamb_grad_plan *plan, double *norms, double 
  * A total that is not finite limits nothing (f = scale), so that the NaN or the infinity
  * stays to be seen; nonfinite_out (device int32, may be NULL) receives 1 then, else 0. In
  * place nothing is written where f is 1. max_norm >= 0 (infinity: no limit), scale finite;
- * f is rounded to fp32, the products once more to their type.
+ * f is rounded to fp32, the products once more to their type; an f outside fp32's normal
+ * range (of gradients near the end of theirs) is a double, and so are its products.
  */
 LAMB_API lamb_status lamb_grad_clip(lamb_grad_plan *plan, const double *total, double max_norm,
                                     double scale, int32_t *nonfinite_out, void *stream);

@@ -273,13 +273,14 @@ __global__ __launch_bounds__(kGradBlock) void grad_zeros_kernel(int32_t n, doubl
 
 // Eight elements a lane, whatever the types: with 16 bytes of fp32 a lane, as the norms have
 // it, their four bf16 results took 1750 us in place of 1630 for the case below.
-template <bool IN_BF16, bool OUT_BF16>
-__device__ inline void scale_chunk(const Chunk &c, float f) {
+// F: float, or double for factors that fp32 does not hold.
+template <bool IN_BF16, bool OUT_BF16, class F>
+__device__ inline void scale_chunk(const Chunk &c, F f) {
     auto scaled = [&](const Eight<IN_BF16> &e) {
         float v[8];
         e.get(v);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] *= f;
+        for (int i = 0; i < 8; ++i) v[i] = float(F(v[i]) * f);
         Eight<OUT_BF16> to;
         to.set(v);
         return to;
@@ -297,12 +298,29 @@ __device__ inline void scale_chunk(const Chunk &c, float f) {
                 store_eight<OUT_BF16, false, true>(c.t.out, at + k * kGradStep, 8, scaled(e[k]));
         }
     };
-    turns(std::integral_constant<int, kGradTurn>{});
-    turns(std::integral_constant<int, kGradTurn / 2>{});
+    if constexpr (std::is_same<F, float>::value) {
+        turns(std::integral_constant<int, kGradTurn>{});
+        turns(std::integral_constant<int, kGradTurn / 2>{});
+    }
     for (; at < c.end; at += kGradStep) {
         const int n = int(c.end - at < 8 ? c.end - at : 8);
         store_eight<OUT_BF16, true>(c.t.out, at, n,
                                     scaled(load_eight<IN_BF16, true>(c.t.in, at, n)));
+    }
+}
+
+template <class F>
+__device__ inline void scale_chunk(const Chunk &c, F f) {
+    if (c.t.in_bf16) {
+        if (c.t.out_bf16)
+            scale_chunk<true, true>(c, f);
+        else
+            scale_chunk<true, false>(c, f);
+    } else {
+        if (c.t.out_bf16)
+            scale_chunk<false, true>(c, f);
+        else
+            scale_chunk<false, false>(c, f);
     }
 }
 
@@ -319,22 +337,18 @@ __global__ __launch_bounds__(kGradBlock) void grad_clip_kernel(GradList l, const
         *nonfinite_out = !finite;
     if (block >= l.chunks)
         return;
-    const float f = float(finite && fabs(scale) * norm > max_norm
-                              ? copysign(max_norm / norm, scale) : scale);
+    const double f = finite && fabs(scale) * norm > max_norm ? copysign(max_norm / norm, scale)
+                                                             : scale;
+    const float rounded = float(f);
     const Chunk c(l, l.chunks - 1 - block);
-    if (f == 1.0f && c.t.in == c.t.out)
+    if (rounded == 1.0f && c.t.in == c.t.out)
         return;
-    if (c.t.in_bf16) {
-        if (c.t.out_bf16)
-            scale_chunk<true, true>(c, f);
-        else
-            scale_chunk<true, false>(c, f);
-    } else {
-        if (c.t.out_bf16)
-            scale_chunk<false, true>(c, f);
-        else
-            scale_chunk<false, false>(c, f);
-    }
+    // Outside its normal range fp32 would round f by more than its half step, to 0 or to
+    // infinity: gradients of 1e38 have norms of 1e43.
+    if (f == 0.0 || (fabs(f) >= 0x1p-126 && isfinite(rounded)))
+        scale_chunk(c, rounded);
+    else
+        scale_chunk(c, f);
 }
 
 template <int NORM>
