@@ -311,6 +311,13 @@ LAMB_API lamb_status lamb_step_ex(lamb_plan *plan, const lamb_hparams *hp, void 
                          double *ratio_out, double *norms_out, int32_t *nonfinite_out);
 
 /*
+ * What lamb_step_ex says of its plan and hyperparameters before any HIP call (host only):
+ * for callers that enqueue something of their own before a step, as the clipping of its
+ * gradients, and want none of it where the step is refused.
+ */
+LAMB_API lamb_status lamb_step_check(const lamb_plan *plan, const lamb_hparams *hp);
+
+/*
  * One LAMB step (Algorithm 2) over every block of the plan, at step t = step:
  *   m <- beta1 m + (1 - beta1) g ;  v <- beta2 v + (1 - beta2) g^2
  *   r  = (m / c1) / (sqrt(v / c2) + eps),  c1 = 1 - beta1^t, c2 = 1 - beta2^t

@@ -155,6 +155,10 @@ LAMB_API lamb_status lamb_muon_hparams_init(lamb_muon_hparams *hp);
 LAMB_API lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void *stream,
                                     int32_t *nonfinite_out);
 
+/* What lamb_muon_step says of its plan and hyperparameters before any HIP call (host
+ * only), for callers that enqueue something of their own before a step. */
+LAMB_API lamb_status lamb_muon_check(const lamb_ns_plan *plan, const lamb_muon_hparams *hp);
+
 /* Frees either kind of plan; NULL is fine. Waits for the device. */
 LAMB_API lamb_status lamb_ns_plan_destroy(lamb_ns_plan *plan);
 

@@ -53,7 +53,7 @@ PATHS = {"auto": LAMB_PATH_AUTO, "two-pass": LAMB_PATH_TWO_PASS}
 # Every symbol the header declares (checked by the test suite).
 EXPORTS = ("lamb_plan_create", "lamb_plan_destroy", "lamb_plan_info",
            "lamb_plan_set_bf16_copies", "lamb_hparams_init",
-           "lamb_step_ex", "lamb_step", "nlamb_step", "lars_step", "lamb_lr_at",
+           "lamb_step_check", "lamb_step_ex", "lamb_step", "nlamb_step", "lars_step", "lamb_lr_at",
            "lamb_sqrt_scaled_lr", "lamb_chunk_table", "lamb_plan_set_timing", "lamb_plan_timing",
            "lamb_plan_set_path", "lamb_plan_tiles", "lamb_plan_check", "lamb_tile_schedule",
            "lamb_step_partials", "lamb_step_finish", "lamb_plan_set_u_check",
@@ -117,6 +117,7 @@ def load(path: Optional[str] = None) -> ctypes.CDLL:
     lib.lamb_hparams_init.argtypes = [P(lamb_hparams), i32]
     lib.lamb_lr_at.argtypes = [P(lamb_lr_stage), i32, i64, P(ctypes.c_double)]
     lib.lamb_sqrt_scaled_lr.argtypes = [ctypes.c_double, i64, i64, P(ctypes.c_double)]
+    lib.lamb_step_check.argtypes = [vp, P(lamb_hparams)]
     lib.lamb_step_ex.argtypes = [vp, P(lamb_hparams), vp, vp, vp, vp]
     lib.lars_step.argtypes = [vp, f32, f32, f32, f32, f32, f32, vp, vp, vp]
     lib.lamb_chunk_table.argtypes = [P(i64), i32, i32, i32, P(i32), P(i64), P(i32), P(i32)]
@@ -235,6 +236,11 @@ def lamb_hparams_init(variant="lamb", **fields) -> lamb_hparams:
             raise AttributeError("lamb_hparams has no field %r" % k)
         setattr(hp, k, val)
     return hp
+
+
+def lamb_step_check(plan: Plan, hp: lamb_hparams) -> None:
+    """Raise what ``lamb_step_ex`` would of these before any HIP call (host only)."""
+    _check(load().lamb_step_check(_vp(plan.handle), ctypes.byref(hp)), "lamb_step_check")
 
 
 def lamb_step_ex(plan: Plan, hp: lamb_hparams, stream: int = 0, ratio_out: int = 0,

@@ -28,7 +28,7 @@ SCALES = {"rms": LAMB_MUON_RMS, "spectral": LAMB_MUON_SPECTRAL, "unit": LAMB_MUO
 
 # Every symbol include/lamb_ops.h declares (checked by the test suite).
 EXPORTS = ("lamb_ns_params_init", "lamb_ortho_plan_create", "lamb_orthogonalize",
-           "lamb_muon_plan_create", "lamb_muon_hparams_init", "lamb_muon_step",
+           "lamb_muon_plan_create", "lamb_muon_hparams_init", "lamb_muon_check", "lamb_muon_step",
            "lamb_ns_plan_destroy", "lamb_xent_workspace", "lamb_xent_forward",
            "lamb_xent_backward", "lamb_embed_forward", "lamb_embed_workspace",
            "lamb_embed_backward", "lamb_rms_forward", "lamb_rms_quantize", "lamb_rms_workspace",
@@ -121,6 +121,7 @@ def load() -> ctypes.CDLL:
     lib.lamb_orthogonalize.argtypes = [vp, P(lamb_ns_params), vp]
     lib.lamb_muon_plan_create.argtypes = [P(lamb_muon_tensor), i32, i32, i32, P(vp)]
     lib.lamb_muon_hparams_init.argtypes = [P(lamb_muon_hparams)]
+    lib.lamb_muon_check.argtypes = [vp, P(lamb_muon_hparams)]
     lib.lamb_muon_step.argtypes = [vp, P(lamb_muon_hparams), vp, vp]
     lib.lamb_ns_plan_destroy.argtypes = [vp]
     lib.lamb_xent_workspace.argtypes = [P(lamb_xent), P(size), P(size)]
@@ -214,6 +215,11 @@ def lamb_muon_plan_create(tensors: Sequence[Tuple[int, int, int, int, int, int]]
     _check(load().lamb_muon_plan_create(arr, n, int(g_dtype), int(precision), ctypes.byref(out)),
            "lamb_muon_plan_create")
     return NsPlan(out.value)
+
+
+def lamb_muon_check(plan: NsPlan, hp: lamb_muon_hparams) -> None:
+    """Raise what ``lamb_muon_step`` would of these before any HIP call (host only)."""
+    _check(load().lamb_muon_check(_vp(plan.handle), ctypes.byref(hp)), "lamb_muon_check")
 
 
 def lamb_muon_step(plan: NsPlan, hp: lamb_muon_hparams, stream: int = 0,

@@ -1147,6 +1147,12 @@ lamb_status lamb_hparams_init(lamb_hparams *hp, int32_t variant) {
     return LAMB_OK;
 }
 
+lamb_status lamb_step_check(const lamb_plan *plan, const lamb_hparams *hp) {
+    if (!plan)
+        return fail(LAMB_ENULL, "plan must not be NULL");
+    return check_hparams(plan, hp, nullptr);
+}
+
 lamb_status lamb_step_ex(lamb_plan *plan, const lamb_hparams *hp, void *stream,
                          double *ratio_out, double *norms_out, int32_t *nonfinite_out) {
     if (!plan)

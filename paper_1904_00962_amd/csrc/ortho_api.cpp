@@ -533,8 +533,7 @@ lamb_status lamb_orthogonalize(lamb_ns_plan *plan, const lamb_ns_params *params,
                    [&] { return run(plan, *params, NsStep{}, nullptr, nullptr, on); });
 }
 
-lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void *stream_in,
-                           int32_t *nonfinite_out) {
+lamb_status lamb_muon_check(const lamb_ns_plan *plan, const lamb_muon_hparams *hp) {
     if (!plan || !hp)
         return fail(LAMB_ENULL, "plan and hparams must not be NULL");
     if (!plan->muon)
@@ -557,6 +556,14 @@ lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void
         return fail(LAMB_EINVAL, "unknown scale %d", hp->scale);
     if (hp->reserved != 0)
         return fail(LAMB_EINVAL, "hparams.reserved must be 0");
+    return LAMB_OK;
+}
+
+lamb_status lamb_muon_step(lamb_ns_plan *plan, const lamb_muon_hparams *hp, void *stream_in,
+                           int32_t *nonfinite_out) {
+    const lamb_status st = lamb_muon_check(plan, hp);
+    if (st != LAMB_OK)
+        return st;
     hipStream_t stream = static_cast<hipStream_t>(stream_in);
     DeviceScope scope(plan->device);
     NsStep step{};

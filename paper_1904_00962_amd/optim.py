@@ -87,10 +87,15 @@ class _Clipper:
         self.max_norm = float(max_norm)
         self.norm = ops.GradNorm(grads)
 
-    def run(self, grad_scale: float) -> None:
-        if self.norm is not None:
-            # the step multiplies the gradients by grad_scale, so their own limit is this
-            self.norm.clip(self.max_norm / abs(grad_scale) if grad_scale else float("inf"))
+    def run(self, check, plan, hp) -> None:
+        """Before the step of ``plan`` with ``hp``; nothing, and the step's own error, where
+        ``check`` refuses that."""
+        if self.norm is None:
+            return
+        check(plan, hp)
+        scale = abs(hp.grad_scale)
+        # the step multiplies the gradients by grad_scale, so their own limit is this
+        self.norm.clip(self.max_norm / scale if scale else float("inf"))
 
     def close(self) -> None:
         if self.norm is not None:
@@ -213,7 +218,7 @@ class _LayerwiseOptimizer:
         hp.norm = _lib.NORMS[self.norm]
         hp.skip_nonfinite = int(self.skip_nonfinite)
         stream = self._stream()
-        self.clipper.run(hp.grad_scale)
+        self.clipper.run(_lib.lamb_step_check, self.plan, hp)
         _lib.lamb_step_ex(self.plan, hp, stream, self.ratios.data_ptr(), self.norms.data_ptr(),
                           self.found_nonfinite.data_ptr() if self.skip_nonfinite else 0)
         if self.skip_nonfinite:
@@ -452,7 +457,7 @@ class Muon:
             lr = _lib.lamb_lr_at(self.schedule, self.t) if self.schedule else self.lr
         self.hparams.lr = lr
         stream = _torch().cuda.current_stream(self.device).cuda_stream
-        self.clipper.run(self.hparams.grad_scale)
+        self.clipper.run(_ops.lamb_muon_check, self.plan, self.hparams)
         _ops.lamb_muon_step(self.plan, self.hparams, stream,
                             self.found_nonfinite.data_ptr() if self.hparams.skip_nonfinite else 0)
 
