@@ -140,21 +140,34 @@ struct Inverse {
     }
 };
 
-// max(largest / 448, 2^-126) of the bits of a magnitude, and its inverse, both as if
-// divided: an estimate and what it leaves. Not so for infinity and NaN.
-__device__ inline void scale_of(uint32_t largest, float *scale, float *up) {
-    const float most = __uint_as_float(largest);
-    if (largest >= 0x7f800000u) {
-        *scale = most;
-        *up = 1.0f / most;
-        return;
+// max(largest / 448, 2^-126) of the bits of a magnitude, and quotients by it, both as if
+// divided: an estimate and what it leaves. Products with the inverse alone fall to the other
+// side of ties of e4m3, which quotients of bf16 products often are (3 in 100000 values of a
+// bf16 stream); they are up to 3% faster (32768 rows of 1600, groups of 128: 71.8 us and 73.2).
+struct Scale {
+    float value, up;
+    float left;  // value; 0 of an infinite or NaN scale, which leaves nothing
+
+    __device__ inline explicit Scale(uint32_t largest) {
+        const float most = __uint_as_float(largest);
+        if (largest >= 0x7f800000u) {
+            value = most;
+            up = 1.0f / most;
+            left = 0.0f;
+            return;
+        }
+        constexpr float kPart = 1.0f / kLargestE4m3;
+        const float s = most * kPart;
+        value = left = fmaxf(fmaf(fmaf(-kLargestE4m3, s, most), kPart, s), kLeastScale);
+        const float u = __builtin_amdgcn_rcpf(value);
+        up = fmaf(fmaf(-value, u, 1.0f), u, u);
     }
-    constexpr float kPart = 1.0f / kLargestE4m3;
-    const float s = most * kPart;
-    *scale = fmaxf(fmaf(fmaf(-kLargestE4m3, s, most), kPart, s), kLeastScale);
-    const float u = __builtin_amdgcn_rcpf(*scale);
-    *up = fmaf(fmaf(-*scale, u, 1.0f), u, u);
-}
+    // signs so that a zero keeps its own
+    __device__ inline float quotient(float y) const {
+        const float q = y * up;
+        return fmaf(-fmaf(q, left, -y), up, q);
+    }
+};
 
 // L lanes to a row (16, 32 or whole waves), V times 8 L columns; a workgroup of one or more
 // rows. With QUANT the result is 8 bits wide. TAIL: dim is no multiple of eight.
@@ -273,18 +286,19 @@ __global__ __launch_bounds__(rms_block(L)) void rms_kernel(RmsArgs a, RmsOut o) 
                     largest = max(largest, magnitude(h[v][i]));
             largest = group_max(largest, min(o.group / 8, kInWave));
         }
-        float scale, up;
-        scale_of(largest, &scale, &up);
+        const Scale scale(largest);
         if (n[v] <= 0)
             continue;
         if (o.group ? c[v] % o.group == 0 : c[v] == 0)
-            o.scales[row * o.groups + (o.group ? c[v] / o.group : 0)] = scale;
+            o.scales[row * o.groups + (o.group ? c[v] / o.group : 0)] = scale.value;
         uint32_t q[2] = {};
 #pragma unroll
         for (int i = 0; i < 8; i += 4) {
             int word = 0;
-            word = __builtin_amdgcn_cvt_pk_fp8_f32(h[v][i] * up, h[v][i + 1] * up, word, false);
-            word = __builtin_amdgcn_cvt_pk_fp8_f32(h[v][i + 2] * up, h[v][i + 3] * up, word, true);
+            word = __builtin_amdgcn_cvt_pk_fp8_f32(scale.quotient(h[v][i]),
+                                                   scale.quotient(h[v][i + 1]), word, false);
+            word = __builtin_amdgcn_cvt_pk_fp8_f32(scale.quotient(h[v][i + 2]),
+                                                   scale.quotient(h[v][i + 3]), word, true);
             q[i / 4] = uint32_t(word);
         }
         uint8_t *p = (uint8_t *)o.out + row * o.out_stride + c[v];
