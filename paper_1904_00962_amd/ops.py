@@ -93,7 +93,7 @@ def _no_graph(name, *tensors):
             continue
         raise ValueError("%s records no gradient for a tensor that requires one: pass "
                          "tensor.detach(), or call it under torch.no_grad(), and take the "
-                         "gradient from %s_grad" % (name, name))
+                         "gradient from %s_grad" % (name, name.removesuffix("_fp8")))
 
 
 class Orthogonalizer:
@@ -426,7 +426,7 @@ def rms_norm_fp8(x, weight=None, *, residual=None, eps: float = 1e-6, group: int
     or 256 columns, the last for what is left of a row: the largest magnitude / 448, at
     least 2^-126."""
     torch = _torch()
-    _no_graph("rms_norm_fp8", x, weight, residual, summed)
+    _no_graph("rms_norm_fp8", x, weight, residual, out, scales, summed)
     r, device = _rms(x, weight, residual, eps), x.device
     out, out_stride = _result("out", out, x, torch.float8_e4m3fn)
     groups = -(-r.dim // group) if group > 0 else 1
