@@ -483,14 +483,18 @@ class GradNorm:
     """The norm of a list of gradients, tensor by tensor and over all of them, and the
     gradients scaled so that it keeps a limit.
 
-    ``grads`` are persistent contiguous tensors, float32 or bfloat16 each, of any size;
-    ``run()`` and ``clip()`` read them as they are then. ``outputs``: where ``clip()``
-    writes, one tensor of as many elements for each, float32 or bfloat16 (default: the
-    gradients themselves). ``norm``: "l2", "l1" or "linf".
+    ``grads`` are persistent contiguous tensors, float32 or bfloat16 each, of any size, none
+    of them twice; ``run()`` and ``clip()`` read them as they are then. ``outputs``: where
+    ``clip()`` writes, one tensor of as many elements for each, float32 or bfloat16 (default:
+    the gradients themselves). ``norm``: "l2", "l1" or "linf".
 
-    ``norms`` (float64, one per tensor), ``total`` (float64) and ``found_nonfinite`` (int32:
-    1 where the last ``clip()`` met a total that is no finite number) are on the device and
-    written by every call. Streams and captures as for :class:`Orthogonalizer`.
+    The results are on the device: ``norms`` (float64, one per tensor) and ``total`` (float64),
+    which ``run()`` and ``clip()`` without a ``total`` write, and ``found_nonfinite`` (int32: 1
+    where the last ``clip()`` met a total that is no finite number), which every ``clip()``
+    writes. Streams and captures as for :class:`Orthogonalizer`.
+
+    To be made once for tensors that stay: that takes an allocation, a copy and a wait for the
+    stream, 0.3 ms for 391 tensors.
     """
 
     def __init__(self, grads: Sequence, outputs: Optional[Sequence] = None, norm: str = "l2"):
