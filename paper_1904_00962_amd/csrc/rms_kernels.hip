@@ -7,11 +7,17 @@
 //   backward, with g = dy w: dh = r (g - h r mean(g h r)) + ds,  dw = sum of dy h r
 //
 // All of it is bound by HBM: a row is read once, stays in the registers of its team's
-// lanes, eight columns to a lane, and its results leave from there. The sums of a row are
-// taken in fp64, which costs little beside the loads (32768 rows of 1600 of a bf16 stream to
-// 8 bits: 77.8 us, 74.3 with sums in fp32) and lets no square pass fp32's range. Results are
-// stored past the caches (nontemporal): 97 to 95 us there, gradients 143.4 to 142.5; loads
-// that way were slower (112 to 118 us on an fp32 stream).
+// lanes, eight columns to a lane, and its results leave from there.
+//
+// Both sides of what was chosen, calls one after another in a graph, in us. Norms: bf16 to 8
+// bits with a bf16 residual and groups of 128; gradients: of bf16 rows on an fp32 stream; both
+// of 32768 rows of 1600 where no other size stands.
+//   sums of a row in fp64 (no square passes fp32's range)  63.9, 133.4; in fp32 62.6, 132.1
+//     (25000 rows: 57.4 and 53.5, the most that it costs)
+//   results, but for the 8-bit ones, stored past the caches (nontemporal)  63.9, 133.4;
+//     through them 71.9, 134.6
+//   loads through the caches  133.4, norms of bf16 on an fp32 stream 112.8; past them 142.3,
+//     117.0 (bf16 gradients of 11718 rows of 4096 gain: 77.4 and 73.3)
 #include <hip/hip_runtime.h>
 #include <math.h>
 
@@ -30,9 +36,9 @@ constexpr float kLeastScale = 0x1p-126f;
 
 // Lanes 0 to 15 of every 16 with each other, by data-parallel moves: 1 away, 2 away, then
 // eights and sixteens from their other ends. Where all lanes of a step's group hold one
-// value, its mirror image is the other half's. (Shuffles, which go through LDS, with
-// divisions and roots at full length: 71 us in place of 63 for the rows above, 3.6 in place
-// of 3.0 for one.)
+// value, its mirror image is the other half's. (Shuffles, which go through LDS: 66.3 us in
+// place of 63.9 for the norms above, 4.1 in place of 3.6 for one row, gradients 141.6 in place
+// of 133.4.)
 constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
 
 template <int MOVE>
@@ -143,7 +149,8 @@ struct Inverse {
 // max(largest / 448, 2^-126) of the bits of a magnitude, and quotients by it, both as if
 // divided: an estimate and what it leaves. Products with the inverse alone fall to the other
 // side of ties of e4m3, which quotients of bf16 products often are (3 in 100000 values of a
-// bf16 stream); they are up to 3% faster (32768 rows of 1600, groups of 128: 71.8 us and 73.2).
+// bf16 stream); they are up to 4% faster (25000 rows of 1600: 55.0 us and 57.4; 32768 rows 64.1
+// and 63.9).
 struct Scale {
     float value, up;
     float left;  // value; 0 of an infinite or NaN scale, which leaves nothing
@@ -175,7 +182,7 @@ struct Scale {
 // One row to a team and many workgroups, not few that go from row to row: these were slower
 // (112 to 118-128 us for 32768 rows of 1600, bf16 on an fp32 stream), with the next row's
 // loads ahead or not. That case moves 629 MB in 110 to 112 us, 5.7 TB/s (a copy of 1 GiB
-// moves 5.1); to 8 bits with groups of 128, bf16 stream: 369 MB in 62 us, 5.9 TB/s. 64 rows
+// moves 5.1); to 8 bits with groups of 128, bf16 stream: 369 MB in 61 us, 6.0 TB/s. 64 rows
 // take 2.9 us, one 2.3: latency.
 constexpr int rms_block(int lanes) { return lanes < kRmsBlock ? kRmsBlock : lanes; }
 
@@ -334,7 +341,11 @@ __device__ inline void finish_weight(const RmsGrad &g, int c, double sum) {
 // finished where there is one workgroup.
 //
 // Bound by HBM: 32768 rows of 1600 on an fp32 stream, 734 MB in 125 us, 5.9 TB/s; 8192 rows of
-// 1024 in bf16 14 us, 4.8 TB/s. Loading the next row ahead changed neither.
+// 1024 in bf16 14 us, 4.8 TB/s. Loading the next row ahead changed neither. L = 1024 (4097 to
+// 8192 columns) has 128 registers a lane, 2 to 11 fewer than the loop takes: 12 to 36 bytes a
+// lane go to scratch; and one workgroup fills a CU, so that nothing loads while it joins a
+// row's sums: 9600 bf16 rows of 5000 with the stream's 99 us, 3.9 TB/s, 5859 of 8192 82 us,
+// 4.7. The weight loaded again for each row, in place of its registers: 6 us more for both.
 template <int L, bool TAIL, bool X_BF16, bool DY_BF16, bool DX_BF16>
 __global__ __launch_bounds__(L < 1024 ? 512 : 1024) void rms_grad_kernel(RmsArgs a, RmsGrad g) {
     constexpr int kWaves = L < 64 ? 1 : L / 64, kInWave = L < 64 ? L : 64;
@@ -607,9 +618,9 @@ hipError_t launch_rms_of(const RmsArgs &a, const RmsOut &o, hipStream_t stream) 
     const int lanes = lanes_of(a.dim);
     // Half the lanes with twice the columns, where rows are many, a team's last lanes have no
     // columns and a lane has little to load: a wave's fixed work counts more there. 25000 rows
-    // of 1600 to 8 bits 50.0 us so and 53.4 the other way, 15625 of 2560 without a residual
-    // 32.4 and 35.6; but with one 56.9 and 54.2, 2048 columns to 8 bits 48.1 and 46.2, and 64
-    // rows of 1600 3.7 and 3.0.
+    // of 1600 to 8 bits 57.4 us so and 64.6 the other way, 2100 rows 9.3 and 8.7; 15625 bf16 rows
+    // of 2560 without a residual 28.6 and 33.0 (fp32 63.0 and 61.4). But with one 56.9 and 54.2,
+    // 2048 columns to 8 bits 48.1 and 46.2, and 64 rows of 1600 3.7 and 3.0.
     if constexpr (!TAIL && (QUANT || !RES)) {
         if (a.tokens >= 2048 && 8 * a.dim <= 7 * 8 * lanes) {
             switch (lanes) {
@@ -659,10 +670,11 @@ struct GradShape {
 };
 
 // `row_bytes`: what a row reads. Few rows go to one workgroup, which needs no second launch.
-// Else at least two rows each (a part of the weight's gradient for every row costs more),
-// and as many workgroups as keep some 8 MB of loads in flight: with more, HBM falls behind.
-// 32768 rows of 1600, fp32 with bf16 dy: 127 us with 512, 144 with 1024; 30000 of bf16: 95
-// and 78.
+// Else at least two rows each (a part of the weight's gradient for every row costs more), in
+// 1024 workgroups where a turn of one reads less than 14 KB, else in 512: with more in flight
+// HBM falls behind. The border lies between what was measured on its sides, 32768 rows of
+// 1600 on an fp32 stream (16 KB) 133.6 us with 512 and 149.9 with 1024, 30000 of bf16 (9.6 KB)
+// 96.0 and 77.6; ragged rows want more further up (192000 fp32 rows of 250, 24 KB: 175 and 149).
 GradShape grad_shape(int64_t tokens, int32_t dim, int64_t row_bytes) {
     GradShape s;
     s.lanes = lanes_of(dim);
