@@ -306,9 +306,10 @@ LAMB_API lamb_status lamb_rms_forward(const lamb_rms *rms, void *summed, int64_t
  * infinities, up to 448), rows out_stride bytes apart, that stand for out times scale.
  * group 0: one scale for a row; 32, 64, 128 or 256: one for as many columns, the last of a
  * row for what is left. scales: float [tokens][groups], max(max |y| / 448, 2^-126) over its
- * columns; out = y / scale, the quotient rounded to fp32 and from there to nearest even. NaN
- * where y holds a NaN or an infinity: in the scale and the columns that share it, or, of an
- * infinity, as y / scale has it.
+ * columns; out = y (1 / scale), the inverse and the product rounded to fp32 and from there to
+ * nearest even: y / scale, but for ties, which may fall to either side. NaN where y holds a NaN
+ * or an infinity: in the scale and the columns that share it, or, of an infinity, as y / scale
+ * has it.
  */
 LAMB_API lamb_status lamb_rms_quantize(const lamb_rms *rms, void *summed, int64_t summed_stride,
                                        void *out, int64_t out_stride, float *scales, int32_t group,

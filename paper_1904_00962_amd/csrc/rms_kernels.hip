@@ -146,35 +146,26 @@ struct Inverse {
     }
 };
 
-// max(largest / 448, 2^-126) of the bits of a magnitude, and quotients by it, both as if
-// divided: an estimate and what it leaves. Products with the inverse alone fall to the other
-// side of ties of e4m3, which quotients of bf16 products often are (3 in 100000 values of a
-// bf16 stream); they are up to 4% faster (25000 rows of 1600: 55.0 us and 57.4; 32768 rows 64.1
-// and 63.9).
-struct Scale {
-    float value, up;
-    float left;  // value; 0 of an infinite or NaN scale, which leaves nothing
-
-    __device__ inline explicit Scale(uint32_t largest) {
-        const float most = __uint_as_float(largest);
-        if (largest >= 0x7f800000u) {
-            value = most;
-            up = 1.0f / most;
-            left = 0.0f;
-            return;
-        }
-        constexpr float kPart = 1.0f / kLargestE4m3;
-        const float s = most * kPart;
-        value = left = fmaxf(fmaf(fmaf(-kLargestE4m3, s, most), kPart, s), kLeastScale);
-        const float u = __builtin_amdgcn_rcpf(value);
-        up = fmaf(fmaf(-value, u, 1.0f), u, u);
+// max(largest / 448, 2^-126) of the bits of a magnitude, and its inverse, both as if
+// divided: an estimate and what it leaves. Not so for infinity and NaN.
+//
+// Values take the inverse, where a division would take the scale: 3 in 100000 of a bf16
+// stream, whose quotients lie at ties of e4m3, then fall to the other side, no further off.
+// Quotients with what the product leaves cost up to 6%: 25600 rows of 3584 60.8 us so and 64.3,
+// 32768 of 1600 64.8 and 65.2; 5% more where it is below fp32's normal numbers.
+__device__ inline void scale_of(uint32_t largest, float *scale, float *up) {
+    const float most = __uint_as_float(largest);
+    if (largest >= 0x7f800000u) {
+        *scale = most;
+        *up = 1.0f / most;
+        return;
     }
-    // signs so that a zero keeps its own
-    __device__ inline float quotient(float y) const {
-        const float q = y * up;
-        return fmaf(-fmaf(q, left, -y), up, q);
-    }
-};
+    constexpr float kPart = 1.0f / kLargestE4m3;
+    const float s = most * kPart;
+    *scale = fmaxf(fmaf(fmaf(-kLargestE4m3, s, most), kPart, s), kLeastScale);
+    const float u = __builtin_amdgcn_rcpf(*scale);
+    *up = fmaf(fmaf(-*scale, u, 1.0f), u, u);
+}
 
 // L lanes to a row (16, 32 or whole waves), V times 8 L columns; a workgroup of one or more
 // rows. With QUANT the result is 8 bits wide. TAIL: dim is no multiple of eight.
@@ -293,19 +284,18 @@ __global__ __launch_bounds__(rms_block(L)) void rms_kernel(RmsArgs a, RmsOut o) 
                     largest = max(largest, magnitude(h[v][i]));
             largest = group_max(largest, min(o.group / 8, kInWave));
         }
-        const Scale scale(largest);
+        float scale, up;
+        scale_of(largest, &scale, &up);
         if (n[v] <= 0)
             continue;
         if (o.group ? c[v] % o.group == 0 : c[v] == 0)
-            o.scales[row * o.groups + (o.group ? c[v] / o.group : 0)] = scale.value;
+            o.scales[row * o.groups + (o.group ? c[v] / o.group : 0)] = scale;
         uint32_t q[2] = {};
 #pragma unroll
         for (int i = 0; i < 8; i += 4) {
             int word = 0;
-            word = __builtin_amdgcn_cvt_pk_fp8_f32(scale.quotient(h[v][i]),
-                                                   scale.quotient(h[v][i + 1]), word, false);
-            word = __builtin_amdgcn_cvt_pk_fp8_f32(scale.quotient(h[v][i + 2]),
-                                                   scale.quotient(h[v][i + 3]), word, true);
+            word = __builtin_amdgcn_cvt_pk_fp8_f32(h[v][i] * up, h[v][i + 1] * up, word, false);
+            word = __builtin_amdgcn_cvt_pk_fp8_f32(h[v][i + 2] * up, h[v][i + 3] * up, word, true);
             q[i / 4] = uint32_t(word);
         }
         uint8_t *p = (uint8_t *)o.out + row * o.out_stride + c[v];

@@ -1,6 +1,6 @@
-"""The 8-bit norm's numbers are the quotients of the norm in fp32 and its scale, rounded to
-nearest even, and the scales those of its magnitudes, bit for bit: also at ties, where
-quotients of bf16 products often lie. Divided here on the CPU."""
+"""The 8-bit norm's numbers are the norm in fp32 times its scale's inverse, rounded to nearest
+even, and the scales those of its magnitudes, bit for bit: also at ties, where quotients of
+bf16 products often lie. Computed here on the CPU; but at ties they are the quotients too."""
 
 import math
 
@@ -15,14 +15,20 @@ def _want(torch, y, group):
     n, d = y.shape
     parts = torch.nn.functional.pad(y, (0, -d % (group or d))).view(n, -1, group or d)
     scales = (parts.abs().amax(dim=2) / 448.0).clamp(min=2.0 ** -126)
-    q = (parts / scales[:, :, None]).view(n, -1)[:, :d]
-    return q.to(torch.float8_e4m3fn), scales
+    q = (parts * (1.0 / scales[:, :, None])).view(n, -1)[:, :d].to(torch.float8_e4m3fn)
+    # where a quotient in 64 bits is more than 2^-23 of it from the middle of two numbers
+    exact = (parts.double() / scales.double()[:, :, None]).view(n, -1)[:, :d]
+    divided = exact.float().to(torch.float8_e4m3fn)
+    other = (q.view(torch.uint8) != divided.view(torch.uint8)).nonzero(as_tuple=True)
+    middle = (q.double()[other] + divided.double()[other]) / 2
+    assert bool(((exact[other] - middle).abs() <= 2.0 ** -23 * middle.abs()).all())
+    return q, scales
 
 
 @pytest.mark.parametrize("tokens,dim", [(300, 100), (2500, 1600), (40, 1001), (30, 9000),
                                         (7, 40000)])
 @pytest.mark.parametrize("group", [0, 32, 128])
-def test_quotients(tokens, dim, group):
+def test_values(tokens, dim, group):
     torch = torch_cuda()
     from paper_1904_00962_amd import ops
     gen = torch.Generator(device="cuda").manual_seed(dim)
@@ -58,3 +64,22 @@ def test_every_tie():
         want, want_scales = _want(torch, y, 0)
         assert torch.equal(scales.cpu(), want_scales)
         assert torch.equal(q.cpu().view(torch.uint8), want.view(torch.uint8))
+
+
+@pytest.mark.parametrize("size", [1e-30, 1e-34, 1e-36, 1e-37, 1e-38, 1e-40, 1e-44, 1e34])
+@pytest.mark.parametrize("group", [0, 32])
+def test_small_and_large_norms(size, group):
+    """Whose scales lie near the least one, and norms near fp32's largest."""
+    torch = torch_cuda()
+    from paper_1904_00962_amd import ops
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    tokens, dim = 3000, 776
+    x = torch.randn(tokens, dim, generator=gen, device="cuda").bfloat16()
+    # many values on ties, and far below the row's largest
+    x = x * torch.exp2(-torch.randint(0, 16, (tokens, dim), generator=gen, device="cuda"))
+    w = (1.0 + 0.2 * torch.randn(dim, generator=gen, device="cuda")).bfloat16().float() * size
+    y = ops.rms_norm(x, w, out_dtype=torch.float32).cpu()
+    q, scales = ops.rms_norm_fp8(x, w, group=group)
+    want, want_scales = _want(torch, y, group)
+    assert torch.equal(scales.cpu(), want_scales)
+    assert torch.equal(q.cpu().view(torch.uint8), want.view(torch.uint8))
