@@ -12,10 +12,10 @@
 // Both sides of what was chosen, calls one after another in a graph, in us. Norms: bf16 to 8
 // bits with a bf16 residual and groups of 128; gradients: of bf16 rows on an fp32 stream; both
 // of 32768 rows of 1600 where no other size stands.
-//   sums of a row in fp64 (no square passes fp32's range)  63.9, 133.4; in fp32 62.6, 132.1
-//     (25000 rows: 57.4 and 53.5, the most that it costs)
-//   results, but for the 8-bit ones, stored past the caches (nontemporal)  63.9, 133.4;
-//     through them 71.9, 134.6
+//   sums of a row in fp64 (no square passes fp32's range)  64.3, 133.4; in fp32 61.9, 132.1
+//     (25000 rows: 56.9 and 51.3, the most that it costs)
+//   results, but for the 8-bit ones, stored past the caches (nontemporal)  64.3, 133.4;
+//     through them 73.7, 134.6
 //   loads through the caches  133.4, norms of bf16 on an fp32 stream 112.8; past them 142.3,
 //     117.0 (bf16 gradients of 11718 rows of 4096 gain: 77.4 and 73.3)
 #include <hip/hip_runtime.h>
@@ -36,9 +36,9 @@ constexpr float kLeastScale = 0x1p-126f;
 
 // Lanes 0 to 15 of every 16 with each other, by data-parallel moves: 1 away, 2 away, then
 // eights and sixteens from their other ends. Where all lanes of a step's group hold one
-// value, its mirror image is the other half's. (Shuffles, which go through LDS: 66.3 us in
-// place of 63.9 for the norms above, 4.1 in place of 3.6 for one row, gradients 141.6 in place
-// of 133.4.)
+// value, its mirror image is the other half's. (Shuffles, which go through LDS: 65.8 us in
+// place of 64.3 for the norms above, 64.3 in place of 60.3 for 25600 rows of 3584, 4.0 in place
+// of 3.7 for one row, gradients 141.6 in place of 133.4.)
 constexpr int kSwap1 = 0xB1, kSwap2 = 0x4E, kMirror8 = 0x141, kMirror16 = 0x140;
 
 template <int MOVE>
@@ -608,7 +608,7 @@ hipError_t launch_rms_of(const RmsArgs &a, const RmsOut &o, hipStream_t stream) 
     const int lanes = lanes_of(a.dim);
     // Half the lanes with twice the columns, where rows are many, a team's last lanes have no
     // columns and a lane has little to load: a wave's fixed work counts more there. 25000 rows
-    // of 1600 to 8 bits 57.4 us so and 64.6 the other way, 2100 rows 9.3 and 8.7; 15625 bf16 rows
+    // of 1600 to 8 bits 56.9 us so and 61.9 the other way, 2100 rows 9.1 and 8.7; 15625 bf16 rows
     // of 2560 without a residual 28.6 and 33.0 (fp32 63.0 and 61.4). But with one 56.9 and 54.2,
     // 2048 columns to 8 bits 48.1 and 46.2, and 64 rows of 1600 3.7 and 3.0.
     if constexpr (!TAIL && (QUANT || !RES)) {
