@@ -318,6 +318,7 @@ LAMB_API lamb_status lamb_rms_quantize(const lamb_rms *rms, void *summed, int64_
 /*
  * Gradients, given that of y: with r = (mean(h^2) + eps)^-1/2 and g = grad_out w,
  *   grad_x = r (g - h r mean(g h r)) + grad_sum,   grad_weight = sum of grad_out h r.
+ * g is formed in fp32: past its range it is infinite, and the row with it.
  * rms.x is the normed h (summed, where there was a residual) and rms.residual NULL: the
  * gradients of x and of the residual are both grad_x. grad_sum: what reaches h from elsewhere
  * (the residual stream's own gradient), of grad_x's type, or NULL. grad_x: float32 or
